@@ -443,6 +443,144 @@ int ptstore_lookup_gather_noalloc(ptstore_t *store, const int32_t *tokens, const
                                   void *cache, int64_t cache_blocks, void *stream);
 
 /* ======================================================================
+ * Operators of the paged cache: what a serving program does with the
+ * caller's cache between a load and the next one. They need no store.
+ *
+ * Conventions of these calls: as above (device pointers, CSR batches, nothing
+ * but kernels enqueued on `stream`, so that every call may be captured in a
+ * graph), on the current device, which has to be the pointers' and the
+ * stream's. They keep no state and allocate nothing: calls on different
+ * streams and host threads are independent. `offsets` must rise from 0 to
+ * n_tokens; a request whose offsets are decreasing, negative or beyond
+ * n_tokens is treated as empty, and what is written for tokens that no
+ * request, or more than one, has is unspecified. Nothing outside the arrays is
+ * touched whatever the device arrays hold.
+ * ====================================================================== */
+
+/* What a paged cache holds. BF16, FP16: a slab is [head][slot][dim] values.
+ * MXFP4 (OCP microscaling 4-bit floats, 4.25 bits an element): a slab is
+ * [head][slot][dim/2] bytes of codes, then [head][slot][dim/32] bytes of
+ * exponents, padded to a multiple of 16 bytes. 32 elements along dim share an
+ * exponent byte b; element 2i is in the low half of byte i; a code is a sign and
+ * one of the levels 0, 0.5, 1, 1.5, 2, 3, 4, 6, and stands for level * 2^(b-127);
+ * b = 255 is NaN. A store holds such blocks when it is made with
+ * layer_chunk_bytes of ptstore_kv_slab_bytes: gather and scatter copy slabs
+ * whatever they hold. The calls below take and give bf16 for BF16 and MXFP4
+ * caches and fp16 for FP16. */
+enum { PTSTORE_KV_BF16 = 0, PTSTORE_KV_FP16 = 1, PTSTORE_KV_MXFP4 = 2 };
+
+/* One layer of a paged cache: its K and V planes, [cache_blocks][slab] each,
+ * 16-byte aligned. Layer l of a cache laid out as above begins at byte
+ * 2 * cache_blocks * (slabs of the earlier layers); its V plane follows its K
+ * plane. */
+typedef struct {
+    void *k;
+    void *v;
+    int64_t cache_blocks;  /* 0 .. 2^26 */
+    int32_t kv_heads;
+    int32_t head_dim;      /* 64 or 128 */
+    int32_t block_tokens;  /* 1 .. 64 */
+    int32_t kind;          /* PTSTORE_KV_* */
+} ptstore_kv_t;
+
+/* Bytes of a (layer, K|V) slab of one block. Host only. Errors: INVALID (a shape
+ * or kind these calls do not take, a slab over 1 GiB, NULL). */
+int ptstore_kv_slab_bytes(int32_t kind, int32_t kv_heads, int32_t head_dim, int32_t block_tokens,
+                          int64_t *bytes);
+
+/*
+ * Block tables, slot map and positions of a batch. Request r has context[r]
+ * tokens in the cache, held[r] entries of its row of block_table [R][max_blocks]
+ * in use (held NULL: none), and offsets[r+1] - offsets[r] new tokens. It needs
+ * ceil((context[r] + new) / block_tokens) blocks, at most max_blocks; those
+ * beyond held[r] are taken, requests in order, from free_blocks[*first],
+ * free_blocks[*first + 1], ... (first NULL: 0) up to free_blocks[n_free - 1], and
+ * written to its row; an entry for which no free block is left gets -1. Other
+ * entries are not touched. held_out[r] = held[r] plus the blocks it got; *next =
+ * *first plus all that were taken. Token t of request r is at position
+ * context[r] + t - offsets[r]: positions[t] (NULL: not wanted), and slots[t] =
+ * block * block_tokens + position % block_tokens, or -1 where its block is
+ * beyond max_blocks or its entry is negative. A held block is reused first: the
+ * entry of a position below held[r] * block_tokens is read from block_table.
+ * held_out must not be held, nor next first (outputs may not overlap inputs).
+ * Errors: INVALID (sizes out of range, R * max_blocks > 2^29, tokens without
+ * requests, a NULL pointer), HIP.
+ */
+int ptstore_block_tables(const int64_t *offsets, int64_t n_tokens, const int32_t *context,
+                         const int32_t *held, int32_t R, int32_t max_blocks, int32_t block_tokens,
+                         const int32_t *free_blocks, int64_t n_free, const int64_t *first,
+                         int32_t *block_table, int64_t *slots, int32_t *positions,
+                         int32_t *held_out, int64_t *next, void *stream);
+
+/*
+ * Write new tokens' K and V into their pages: row (token t, head h) of k and v
+ * goes to slot slots[t] of head h (block slots[t] / block_tokens). Slots below 0
+ * or past the cache are skipped; two tokens of one slot race. k and v are
+ * [token][head][dim] with strides in elements (multiples of 8; 16-byte aligned
+ * bases), dim contiguous. MXFP4: 32 elements get the smallest exponent e for
+ * which their largest magnitude is at most 7 * 2^e (-126 <= e <= 125), and each the
+ * level nearest to its magnitude / 2^e, ties to the even code, above 6 to 6; a
+ * group that holds an infinity or a NaN reads as NaN.
+ * Errors: INVALID, HIP.
+ */
+int ptstore_kv_append(const ptstore_kv_t *kv, const void *k, int64_t k_token_stride,
+                      int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                      int64_t v_head_stride, const int64_t *slots, int64_t n_tokens, void *stream);
+
+/* The reverse: the values that the rows of `slots` hold, into k and v; zeros
+ * for a slot below 0 or past the cache. Errors as ptstore_kv_append. */
+int ptstore_kv_read(const ptstore_kv_t *kv, void *k, int64_t k_token_stride, int64_t k_head_stride,
+                    void *v, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots,
+                    int64_t n_tokens, void *stream);
+
+/*
+ * Causal attention of a batch's new tokens over their requests' pages. Token t
+ * of request r, at position i = context[r] + t - offsets[r], sees the keys of
+ * positions 0 .. i (its own K and V have been appended) whose block_table entry
+ * names a block of the cache; keys on other pages, and positions past
+ * max_blocks * block_tokens, do not exist. Query head h reads KV head
+ * h / (q_heads / kv_heads):
+ *   out[t][h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q[t][h] . k_j),
+ *   lse[t][h] = log(sum_j w_j).
+ * A row that sees no key, or only keys of weight zero (scores of minus
+ * infinity), gets zeros and minus infinity. What lies in keys a row does not see,
+ * NaN included, never reaches it. One token a request, whole prompts, prompts
+ * behind a loaded prefix and mixes of them are all this call. Products take
+ * 16-bit factors and sum in 32 bits; maxima, sums and the output are kept in 32
+ * bits until they are written. The same inputs give the same bits.
+ */
+typedef struct {
+    ptstore_kv_t kv;
+    const void *q;              /* [n_tokens][q_heads][head_dim], 16-byte aligned rows */
+    int64_t q_token_stride;     /* in elements, multiples of 8 */
+    int64_t q_head_stride;
+    void *out;                  /* as q; not q itself */
+    int64_t out_token_stride;
+    int64_t out_head_stride;
+    float *lse;                 /* [n_tokens][q_heads], or NULL */
+    const int64_t *offsets;     /* [R + 1] */
+    const int32_t *context;     /* [R] tokens in the cache before the new ones */
+    const int32_t *block_table; /* [R][max_blocks] */
+    int64_t n_tokens;
+    int32_t R;
+    int32_t max_blocks;
+    int32_t q_heads;            /* a multiple of kv.kv_heads */
+    float scale;                /* positive, usually 1 / sqrt(head_dim) */
+    void *workspace;            /* the call's own until it is done; need not be cleared */
+    int64_t workspace_bytes;
+} ptstore_attention_t;
+
+/* Bytes of workspace an attention of these sizes needs (0: none), 16-byte
+ * aligned; it follows from the arguments and the device alone. Host only.
+ * Errors: INVALID, HIP. */
+int ptstore_attention_workspace(const ptstore_kv_t *kv, int32_t q_heads, int64_t n_tokens, int32_t R,
+                                int32_t max_blocks, int64_t *bytes);
+
+/* Errors: INVALID (shapes, sizes, strides or alignment as stated; max_blocks *
+ * block_tokens > 2^30; no cache blocks; a workspace too small), HIP. */
+int ptstore_attention(const ptstore_attention_t *args, void *stream);
+
+/* ======================================================================
  * Tuning and diagnostics: not store operations. Counters, timing, the
  * store's buffers for tests, copy launch shapes, and a bandwidth probe.
  * ====================================================================== */

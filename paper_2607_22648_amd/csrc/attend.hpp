@@ -1,0 +1,164 @@
+// Device parts that the attention kernels share.
+//
+// Scores are computed transposed, S^T = K Q^T, and so is the output, O^T =
+// V^T P^T: a query is a column of both, a lane holds one query's scores, and
+// its share of P^T is in the registers where the second product wants it. The
+// matrix instructions sum over 8 consecutive keys per lane; which key a row of
+// K stands for is free, and is chosen (key_of_row) so that a lane's scores are
+// those of 8 consecutive keys.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "paged.hpp"
+#include "ptstore.h"
+
+namespace ptsd {
+
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+// A 16-bit type's vectors and matrix instructions. The 4-bit cache is widened
+// to bf16, which holds its values exactly.
+template <bool kHalf>
+struct Elem;
+
+template <>
+struct Elem<false> {
+    typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    static constexpr uint32_t kExpMask = 0x7F807F80u;  // all ones: infinity or NaN
+    static __device__ float wide(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ v4f mma16(v8 a, v8 b, v4f c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ v16f mma32(v8 a, v8 b, v16f c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <>
+struct Elem<true> {
+    typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    static constexpr uint32_t kExpMask = 0x7C007C00u;
+    static __device__ float wide(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
+    static __device__ v4f mma16(v8 a, v8 b, v4f c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+    static __device__ v16f mma32(v8 a, v8 b, v16f c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+// Two floats to two 16-bit values, nearest even.
+template <bool kHalf>
+__device__ inline uint32_t pack2(float a, float b) {
+    const v2f x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, typename Elem<kHalf>::v2));
+}
+
+// Whether one of a lane's eight values is an infinity or a NaN.
+template <bool kHalf>
+__device__ inline bool not_finite(v4u x) {
+    constexpr uint32_t m = Elem<kHalf>::kExpMask, lo = m & 0xFFFFu, hi = m & 0xFFFF0000u;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (x[i] & lo) == lo || (x[i] & hi) == hi;
+    return bad;
+}
+
+// Four 16-bit rows' values of one column: lane i of 16 gives the address of 4
+// values of row i / 4 and gets column i of the 4 x 16 piece.
+__device__ inline v2u read_transposed(const uint8_t* lds) {
+    typedef __attribute__((address_space(3))) v4s lds_v4s;
+    return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)lds));
+}
+
+__device__ inline v4u join(v2u a, v2u b) { return v4u{a[0], a[1], b[0], b[1]}; }
+
+// The 32 codes of a lane's 16 bytes: piece `i` of four, 8 elements.
+__device__ inline v4u widen8(uint32_t code, float step) {
+    v4u x;
+    x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 0));
+    x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 1));
+    x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 2));
+    x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 3));
+    return x;
+}
+
+// Lowest score kept: what a row starts from instead of minus infinity, so that
+// the differences of two such rows stay numbers.
+constexpr float kLowest = -3.0e38f;
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A request's tile: its number among the request's tiles, and the request's
+// numbers. `tile` < 0: no work.
+struct Tile {
+    int r, tile;
+    int64_t begin;  // first token
+    int32_t n;      // new tokens
+    int64_t past;
+};
+
+// Finds tile number t of the batch. Every wave looks for itself, 64 requests at
+// a time: request r's tiles start at offsets[r] * group / rows + r, which
+// rises with r, so the lanes that start at or before t are counted.
+__device__ inline Tile find_tile(const AttendPlan& p, int64_t t, int rows) {
+    const int lane = threadIdx.x & 63;
+    Tile f;
+    f.tile = -1;
+    int lo = 0, span = p.R;  // the request is in [lo, lo + span)
+    while (span > 64) {
+        const int step = (span + 63) / 64;
+        const int r = lo + lane * step;
+        const bool at = r < lo + span && p.offsets[r] * p.group / rows + r <= t;
+        const int n = __popcll(__ballot(at));
+        const int from = lo + (n > 0 ? n - 1 : 0) * step;
+        span = lo + span - from < step ? lo + span - from : step;
+        lo = from;
+    }
+    const int r = lo + lane;
+    int64_t a = 0, b = 0;
+    int32_t past = 0;
+    const bool in = lane < span;
+    if (in) {
+        a = p.offsets[r];
+        b = p.offsets[r + 1];
+        past = p.context[r];
+    }
+    const int n = __popcll(__ballot(in && a * p.group / rows + r <= t));
+    const int src = __builtin_amdgcn_readfirstlane(n > 0 ? n - 1 : 0);
+    f.r = lo + src;
+    const int64_t begin = ((int64_t)__builtin_amdgcn_readlane((int)(a >> 32), src) << 32) |
+                          (uint32_t)__builtin_amdgcn_readlane((int)a, src);
+    const int64_t end = ((int64_t)__builtin_amdgcn_readlane((int)(b >> 32), src) << 32) |
+                        (uint32_t)__builtin_amdgcn_readlane((int)b, src);
+    f.past = __builtin_amdgcn_readlane(past, src);
+    if (begin < 0 || end < begin || end > p.n_tokens) return f;
+    f.begin = begin;
+    f.n = (int32_t)(end - begin);
+    const int64_t tile = t - (begin * p.group / rows + f.r);
+    if (tile < 0 || tile * rows >= (int64_t)f.n * p.group) return f;
+    f.tile = (int)tile;
+    return f;
+}
+
+// The place of key `key` of a request's pages: cache block << 6 | slot, or -1 if
+// it is at or past `end` or its page does not exist.
+__device__ inline int32_t page_entry(const AttendPlan& p, const int32_t* table, int32_t key, int32_t end) {
+    return key < end ? table[div_page((uint32_t)key, p.kv.div)] : -1;
+}
+
+__device__ inline uint32_t place_of(const AttendPlan& p, int32_t entry, int32_t key, bool& there) {
+    there = entry >= 0 && entry < (int32_t)p.kv.blocks;
+    const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
+    return there ? ((uint32_t)entry << kSlotBits) | slot : 0u;
+}
+
+}  // namespace ptsd

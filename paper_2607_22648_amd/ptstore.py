@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -24,6 +24,7 @@ PTSTORE_FLAG_WEAK_TAGS = 16
 PTSTORE_NOALLOC_MAX_ENTRIES = 1 << 20
 KIND_GATHER, KIND_LOOKUP, KIND_SCATTER, KIND_INSERT, KIND_SELECT, KIND_EVICT = 0, 1, 2, 3, 4, 5
 KIND_REPLICATE = 6
+PTSTORE_KV_BF16, PTSTORE_KV_FP16, PTSTORE_KV_MXFP4 = 0, 1, 2
 
 
 class ptstore_config_t(C.Structure):
@@ -50,6 +51,21 @@ class ptstore_buffers_t(C.Structure):
                 ("host_blocks", C.c_int64), ("device_blocks", C.c_int64), ("replica_of", C.c_void_p)]
 
 
+class ptstore_kv_t(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cache_blocks", C.c_int64),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block_tokens", C.c_int32),
+                ("kind", C.c_int32)]
+
+
+class ptstore_attention_t(C.Structure):
+    _fields_ = [("kv", ptstore_kv_t), ("q", C.c_void_p), ("q_token_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("out", C.c_void_p), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("lse", C.c_void_p), ("offsets", C.c_void_p),
+                ("context", C.c_void_p), ("block_table", C.c_void_p), ("n_tokens", C.c_int64),
+                ("R", C.c_int32), ("max_blocks", C.c_int32), ("q_heads", C.c_int32),
+                ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 class PTStoreError(RuntimeError):
     def __init__(self, fn: str, code: int, detail: str):
         super().__init__(f"{fn} failed: code {code} ({detail})")
@@ -64,7 +80,9 @@ EXPORTS = ("ptstore_create", "ptstore_destroy", "ptstore_lookup", "ptstore_gathe
            "ptstore_scatter_layers", "ptstore_gather_prepare", "ptstore_gather_prepared",
            "ptstore_set_counters", "ptstore_set_timing", "ptstore_lookup_gather_noalloc",
            "ptstore_set_timing_kinds",
-           "ptstore_insert_sync")
+           "ptstore_insert_sync", "ptstore_kv_slab_bytes", "ptstore_block_tables",
+           "ptstore_kv_append", "ptstore_kv_read", "ptstore_attention_workspace",
+           "ptstore_attention")
 
 
 def _load() -> C.CDLL:
@@ -97,6 +115,12 @@ def _load() -> C.CDLL:
         "ptstore_scatter_layers": [p, p, p, p, i32, i32, i32, i32, p, i64, p],
         "ptstore_gather_prepare": [p, p, p, p, i32, i32, i64, p],
         "ptstore_gather_prepared": [p, i32, i32, p, i64, p],
+        "ptstore_kv_slab_bytes": [i32, i32, i32, i32, C.POINTER(i64)],
+        "ptstore_block_tables": [p, i64, p, p, i32, i32, i32, p, i64, p, p, p, p, p, p, p],
+        "ptstore_kv_append": [C.POINTER(ptstore_kv_t), p, i64, i64, p, i64, i64, p, i64, p],
+        "ptstore_kv_read": [C.POINTER(ptstore_kv_t), p, i64, i64, p, i64, i64, p, i64, p],
+        "ptstore_attention_workspace": [C.POINTER(ptstore_kv_t), i32, i64, i32, i32, C.POINTER(i64)],
+        "ptstore_attention": [C.POINTER(ptstore_attention_t), p],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -152,6 +176,13 @@ def _requests(offsets: torch.Tensor) -> int:
     if offsets.dim() != 1 or offsets.numel() < 1:
         raise ValueError("offsets must be a 1-D tensor of R + 1 entries")
     return offsets.numel() - 1
+
+
+def _table(offsets: torch.Tensor, block_table: torch.Tensor) -> Tuple[int, int]:
+    R, maxb = _rows(block_table, "block_table")
+    if _requests(offsets) != R:
+        raise ValueError(f"block_table has {R} rows, the batch {_requests(offsets)} requests")
+    return R, maxb
 
 
 # The current stream's handle alone: building a torch.cuda.Stream to read it
@@ -373,8 +404,104 @@ def ptstore_last_error() -> str:
     return _lib.ptstore_last_error().decode()
 
 
+def ptstore_kv_slab_bytes(kind: int, kv_heads: int, head_dim: int, block_tokens: int) -> int:
+    n = C.c_int64()
+    _check("ptstore_kv_slab_bytes", _lib.ptstore_kv_slab_bytes(kind, kv_heads, head_dim, block_tokens,
+                                                               C.byref(n)))
+    return n.value
+
+
+def ptstore_block_tables(offsets, context, held, block_tokens, free_blocks, first, block_table, slots,
+                         positions, held_out, next_free, stream=None) -> None:
+    """n_tokens is the length of `slots`; `held`, `first` and `positions` may be None."""
+    R, maxb = _table(offsets, block_table)
+    n = slots.numel()
+    _need(context, R, "context")
+    if held is not None:
+        _need(held, R, "held")
+    _need(held_out, R, "held_out")
+    _need(next_free, 1, "next_free")
+    if first is not None:
+        _need(first, 1, "first")
+    if positions is not None:
+        _need(positions, n, "positions")
+    _check("ptstore_block_tables", _lib.ptstore_block_tables(
+        _dev(offsets, torch.int64, "offsets"), n, _dev(context, torch.int32, "context"),
+        _dev(held, torch.int32, "held"), R, maxb, block_tokens,
+        _dev(free_blocks, torch.int32, "free_blocks"), free_blocks.numel(),
+        _dev(first, torch.int64, "first"), _dev(block_table, torch.int32, "block_table"),
+        _dev(slots, torch.int64, "slots"), _dev(positions, torch.int32, "positions"),
+        _dev(held_out, torch.int32, "held_out"), _dev(next_free, torch.int64, "next_free"),
+        _stream(stream)))
+
+
+_KV_DTYPES = {PTSTORE_KV_BF16: torch.bfloat16, PTSTORE_KV_FP16: torch.float16,
+              PTSTORE_KV_MXFP4: torch.bfloat16}
+
+
+def _token_rows(t: torch.Tensor, kv: ptstore_kv_t, heads: Optional[int], name: str) -> Tuple[int, int, int]:
+    """Address and strides of a [tokens, heads, head_dim] tensor whose rows are contiguous."""
+    want = _KV_DTYPES[kv.kind]
+    if not t.is_cuda or t.dtype != want or t.dim() != 3:
+        raise ValueError(f"{name} must be a [tokens, heads, head_dim] device tensor of {want}")
+    if t.shape[2] != kv.head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the cache {kv.kv_heads} heads of "
+                         f"{kv.head_dim}")
+    token, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    # a dimension of one row may have any stride: none of its others is reached
+    return t.data_ptr(), token if t.shape[0] > 1 else 0, head if t.shape[1] > 1 else 0
+
+
+def _rows_of(kv, k, v, slots):
+    n = slots.numel()
+    kr, vr = _token_rows(k, kv, kv.kv_heads, "k"), _token_rows(v, kv, kv.kv_heads, "v")
+    if k.shape[0] != n or v.shape[0] != n:
+        raise ValueError(f"k and v hold {k.shape[0]} and {v.shape[0]} tokens, slots {n}")
+    return (*kr, *vr, _dev(slots, torch.int64, "slots"), n)
+
+
+def ptstore_kv_append(kv: ptstore_kv_t, k, v, slots, stream=None) -> None:
+    _check("ptstore_kv_append", _lib.ptstore_kv_append(C.byref(kv), *_rows_of(kv, k, v, slots),
+                                                       _stream(stream)))
+
+
+def ptstore_kv_read(kv: ptstore_kv_t, k, v, slots, stream=None) -> None:
+    _check("ptstore_kv_read", _lib.ptstore_kv_read(C.byref(kv), *_rows_of(kv, k, v, slots),
+                                                   _stream(stream)))
+
+
+def ptstore_attention_workspace(kv: ptstore_kv_t, q_heads: int, n_tokens: int, R: int,
+                                max_blocks: int) -> int:
+    n = C.c_int64()
+    _check("ptstore_attention_workspace", _lib.ptstore_attention_workspace(
+        C.byref(kv), q_heads, n_tokens, R, max_blocks, C.byref(n)))
+    return n.value
+
+
+def ptstore_attention(kv: ptstore_kv_t, q, out, lse, offsets, context, block_table, scale: float,
+                      workspace=None, stream=None) -> None:
+    """`lse` may be None, and `workspace` where the call needs none."""
+    R, maxb = _table(offsets, block_table)
+    _need(context, R, "context")
+    qr = _token_rows(q, kv, None, "q")
+    outr = _token_rows(out, kv, q.shape[1], "out")
+    n, heads = q.shape[0], q.shape[1]
+    if out.shape[0] != n:
+        raise ValueError(f"out holds {out.shape[0]} tokens, q {n}")
+    if lse is not None:
+        _need(lse, n * heads, "lse")
+    a = ptstore_attention_t(kv, *qr, *outr, _dev(lse, torch.float32, "lse"),
+                            _dev(offsets, torch.int64, "offsets"), _dev(context, torch.int32, "context"),
+                            _dev(block_table, torch.int32, "block_table"), n, R, maxb, heads, scale,
+                            _dev(workspace, torch.uint8, "workspace"),
+                            workspace.numel() if workspace is not None else 0)
+    _check("ptstore_attention", _lib.ptstore_attention(C.byref(a), _stream(stream)))
+
+
 # ---------------------------------------------------------------------------
-# Convenience wrapper
+# Convenience wrappers
 # ---------------------------------------------------------------------------
 
 @dataclass
@@ -592,6 +719,100 @@ class PrefixStore:
             raise ValueError("store created without PTSTORE_FLAG_EVICT")
         return (_wrap_device(b.freq, b.capacity, torch.int64),
                 _wrap_device(b.prio, b.capacity, torch.int64))
+
+
+_KV_KINDS = {"bf16": PTSTORE_KV_BF16, "fp16": PTSTORE_KV_FP16, "mxfp4": PTSTORE_KV_MXFP4}
+
+
+class PagedCache:
+    """A paged cache [layer][K|V][cache block][slab] on the current device, and the
+    operators on it. ``data`` is what the store's loads and ``scatter`` take; a store
+    for its blocks is made with ``shape``. ``kv_heads`` is a number, or one per layer.
+
+    Outputs and workspaces that a call makes are made for the stream it runs on."""
+
+    def __init__(self, layers: int, kv_heads: Union[int, Sequence[int]], head_dim: int, cache_blocks: int,
+                 block_tokens: int = 16, kind: str = "bf16", data: Optional[torch.Tensor] = None,
+                 device="cuda"):
+        if kind not in _KV_KINDS:
+            raise ValueError(f"kind must be one of {sorted(_KV_KINDS)}, got {kind!r}")
+        heads = [kv_heads] * layers if isinstance(kv_heads, int) else [int(h) for h in kv_heads]
+        if layers < 1 or len(heads) != layers or cache_blocks < 0:
+            raise ValueError("a cache has layers, a number of KV heads for each, and 0 or more blocks")
+        self.kind, self.cache_blocks, self.block_tokens = kind, cache_blocks, block_tokens
+        slabs = [ptstore_kv_slab_bytes(_KV_KINDS[kind], h, head_dim, block_tokens) for h in heads]
+        # slabs of values only, all alike: the uniform store shape; else sizes by layer
+        uniform = kind != "mxfp4" and len(set(heads)) == 1
+        self.shape = StoreShape(layers, heads[0], head_dim, block_tokens, 2,
+                                None if uniform else tuple(slabs))
+        nbytes = 2 * cache_blocks * sum(slabs)
+        if data is None:
+            data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if not data.is_cuda or not data.is_contiguous() or data.numel() * data.element_size() != nbytes:
+            raise ValueError(f"data must be a contiguous device tensor of {nbytes} bytes")
+        self.data = data
+        self.dtype = _KV_DTYPES[_KV_KINDS[kind]]
+        self._planes = []
+        at = data.data_ptr()
+        for h, slab in zip(heads, slabs):
+            self._planes.append(ptstore_kv_t(at, at + cache_blocks * slab, cache_blocks, h, head_dim,
+                                             block_tokens, _KV_KINDS[kind]))
+            at += 2 * cache_blocks * slab
+
+    def layer(self, layer: int) -> ptstore_kv_t:
+        """The K and V planes of a layer, as the C calls take them."""
+        return self._planes[layer]
+
+    @staticmethod
+    def _on(stream):
+        """A context in which tensors are allocated for `stream` (a torch stream or a raw handle)."""
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream))
+        return torch.cuda.stream(stream)  # no change where it is None
+
+    def tables(self, offsets, context, block_table, free_blocks, n_tokens: int, held=None, first=None,
+               stream=None):
+        """Give the batch's requests their blocks: fills the new entries of `block_table` and
+        returns (slots, positions, held after, next free entry)."""
+        dev = offsets.device
+        with self._on(stream):
+            slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
+            positions = torch.empty(n_tokens, dtype=torch.int32, device=dev)
+            held_out = torch.empty(block_table.shape[0], dtype=torch.int32, device=dev)
+            next_free = torch.empty(1, dtype=torch.int64, device=dev)
+        ptstore_block_tables(offsets, context, held, self.block_tokens, free_blocks, first, block_table,
+                             slots, positions, held_out, next_free, stream)
+        return slots, positions, held_out, next_free
+
+    def append(self, layer: int, k, v, slots, stream=None) -> None:
+        """Write k, v [tokens, kv_heads, head_dim] to `slots` of a layer."""
+        ptstore_kv_append(self._planes[layer], k, v, slots, stream)
+
+    def read(self, layer: int, slots, stream=None):
+        """The K and V that `slots` of a layer hold, [tokens, kv_heads, head_dim] each."""
+        kv = self._planes[layer]
+        with self._on(stream):
+            k, v = (torch.empty((slots.numel(), kv.kv_heads, kv.head_dim), dtype=self.dtype,
+                                device=slots.device) for _ in range(2))
+        ptstore_kv_read(kv, k, v, slots, stream)
+        return k, v
+
+    def attend(self, layer: int, q, offsets, context, block_table, scale: Optional[float] = None, out=None,
+               lse: bool = False, workspace=None, stream=None):
+        """Causal attention of q [tokens, q_heads, head_dim] over a layer: out, or (out, lse).
+        scale: 1 / sqrt(head_dim) unless given. A `workspace` (uint8) is used if it is large enough."""
+        kv = self._planes[layer]
+        n, heads = q.shape[0], q.shape[1]
+        need = ptstore_attention_workspace(kv, heads, n, *_table(offsets, block_table))
+        with self._on(stream):
+            if out is None:
+                out = torch.empty((n, heads, kv.head_dim), dtype=q.dtype, device=q.device)
+            sums = torch.empty((n, heads), dtype=torch.float32, device=q.device) if lse else None
+            if need and (workspace is None or workspace.numel() < need):
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ptstore_attention(kv, q, out, sums, offsets, context, block_table,
+                          kv.head_dim ** -0.5 if scale is None else scale, workspace, stream)
+        return (out, sums) if lse else out
 
 
 class _CudaArray:
