@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libptstore.so")
 SOURCES = ["api.hip", "lookup.hip", "copy.hip", "insert.hip", "evict.hip", "probe.hip",
-           "paged_api.hip", "tables.hip", "append.hip", "decode.hip"]
+           "paged_api.hip", "tables.hip", "append.hip", "decode.hip", "prompt.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

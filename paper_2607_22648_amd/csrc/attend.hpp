@@ -1,4 +1,4 @@
-// Device parts that the attention kernels share.
+// Device parts that the attention kernels share (decode.hip, prompt.hip).
 //
 // Scores are computed transposed, S^T = K Q^T, and so is the output, O^T =
 // V^T P^T: a query is a column of both, a lane holds one query's scores, and
@@ -32,7 +32,6 @@ struct Elem<false> {
     typedef __bf16 v2 __attribute__((ext_vector_type(2)));
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExpMask = 0x7F807F80u;  // all ones: infinity or NaN
-    static __device__ float wide(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
     static __device__ v4f mma16(v8 a, v8 b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
@@ -46,7 +45,6 @@ struct Elem<true> {
     typedef _Float16 v2 __attribute__((ext_vector_type(2)));
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExpMask = 0x7C007C00u;
-    static __device__ float wide(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
     static __device__ v4f mma16(v8 a, v8 b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
@@ -62,14 +60,21 @@ __device__ inline uint32_t pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, typename Elem<kHalf>::v2));
 }
 
-// Whether one of a lane's eight values is an infinity or a NaN.
+// A weight of zero times an infinity would be a NaN. So in V's rows that some
+// row of a tile must not see, values that are not finite are replaced by zeros
+// before the product (true if there were any), and added at the end, by
+// add_endless, to the rows that do see them.
 template <bool kHalf>
-__device__ inline bool not_finite(v4u x) {
-    constexpr uint32_t m = Elem<kHalf>::kExpMask, lo = m & 0xFFFFu, hi = m & 0xFFFF0000u;
-    bool bad = false;
+__device__ inline bool drop_endless(v4u& x) {
+    constexpr uint32_t lo = Elem<kHalf>::kExpMask & 0xFFFFu, hi = Elem<kHalf>::kExpMask & 0xFFFF0000u;
+    bool any = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad |= (x[i] & lo) == lo || (x[i] & hi) == hi;
-    return bad;
+    for (int i = 0; i < 4; ++i) {
+        const bool a = (x[i] & lo) == lo, b = (x[i] & hi) == hi;
+        any |= a || b;
+        x[i] &= (a ? 0u : 0xFFFFu) | (b ? 0u : 0xFFFF0000u);
+    }
+    return any;
 }
 
 // Four 16-bit rows' values of one column: lane i of 16 gives the address of 4
@@ -159,6 +164,27 @@ __device__ inline uint32_t place_of(const AttendPlan& p, int32_t entry, int32_t 
     there = entry >= 0 && entry < (int32_t)p.kv.blocks;
     const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
     return there ? ((uint32_t)entry << kSlotBits) | slot : 0u;
+}
+
+// The value at dimension d of the V row at `place` of a head.
+template <int D, bool kHalf, bool kFour>
+__device__ inline float v_value(const Planes& kv, uint32_t place, uint64_t head_row, int d) {
+    const uint8_t* page = kv.v + (uint64_t)(place >> kSlotBits) * kv.slab;
+    const uint64_t line = head_row + (place & 63u);
+    if constexpr (kFour) {
+        const float step = __uint_as_float((uint32_t)page[kv.exponents + line * (D / kGroup) + d / kGroup] << 23);
+        const uint32_t code = page[line * (D / 2) + d / 2] >> (4 * (d & 1));
+        const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 0));
+        return __uint_as_float(two << 16);
+    } else {
+        const uint16_t x = *(const uint16_t*)(page + (line * D + d) * 2);
+        return kHalf ? (float)__builtin_bit_cast(_Float16, x) : __uint_as_float((uint32_t)x << 16);
+    }
+}
+
+// Adds to a sum what drop_endless took from it.
+__device__ inline float add_endless(float sum, float x) {
+    return __builtin_isfinite(x) ? sum : sum + x;
 }
 
 }  // namespace ptsd

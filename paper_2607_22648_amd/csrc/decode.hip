@@ -176,6 +176,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         entry = page_entry(p, table, at + stride + step_key, k1);
     }
     uint8_t* const lds = s_mem.v[wave];
+    bool endless = false;  // a V value that is not finite lies behind the first row's last key
 
     while (at < k1) {
         // scores of column n: keys 32 b + 8 h4 + 4 (g & 1) + i in s[g][i], b = g >> 1
@@ -204,7 +205,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         }
 
         constexpr uint64_t kAll = kKeys == 64 ? ~0ull : 0xFFFFFFFFull;
-        const bool some_hidden = (ok & kAll) != kAll || at + kKeys - 1 > all_see;
+        const bool edge = k1 - 1 > all_see && at + kKeys - 1 > all_see;
+        const bool some_hidden = (ok & kAll) != kAll || edge;
         if (some_hidden) {
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -256,6 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
                     for (int c = 0; c < kWords; ++c) {
                         v4u x = widen8(vreg[j][c], step);
+                        if (edge && at + 32 * b + key > all_see && in) endless |= drop_endless<kHalf>(x);
                         if (!in) x = v4u{0u, 0u, 0u, 0u};
                         const int col = (lane & 3) * kWords + c;
                         *(v4u*)(lds + key * kRow + ((col ^ turn<D>(key)) * 16)) = x;
@@ -266,6 +269,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 for (int i = 0; i < kPieces; ++i) {
                     const int key = i * (64 / kLanes) + lane / kLanes;
                     v4u x = vreg[i];
+                    if (edge && at + key > all_see && ((ok >> key) & 1)) endless |= drop_endless<kHalf>(x);
                     if (!((ok >> key) & 1)) x = v4u{0u, 0u, 0u, 0u};
                     *(v4u*)(lds + key * kRow + (((lane % kLanes) ^ turn<D>(key)) * 16)) = x;
                 }
@@ -285,42 +289,26 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 const v2u hi = read_transposed(lds + (vrow + 4) * kRow + ((col ^ turn<D>(vrow + 4)) * 16) + in);
                 vt[i] = join(lo, hi);
             }
-            bool odd = false;
-            if (some_hidden) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) odd |= not_finite<kHalf>(vt[i]);
-            }
-            if (__any(odd)) {
-                // a weight of zero times an infinity would be a NaN: where a key that some
-                // row must not see is not finite, the products are taken one by one
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t two = w[b][j >> 1];
-                    const float mine = E::wide((uint16_t)(j & 1 ? two >> 16 : two));
-                    for (int hh = 0; hh < 4; ++hh) {
-                        const float weight = __shfl(mine, hh * 16 + n);
-                        const int key = 8 * hh + j;
-                        if (weight == 0.f) continue;
-#pragma unroll
-                        for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int d = 16 * i + 4 * h4 + e;
-                                const uint16_t x = *(const uint16_t*)(
-                                    lds + key * kRow + (((d >> 3) ^ turn<D>(key)) * 16) + (d & 7) * 2);
-                                o[i][e] = __builtin_fmaf(weight, E::wide(x), o[i][e]);
-                            }
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    o[i] = E::mma16(__builtin_bit_cast(typename E::v8, vt[i]),
-                                    __builtin_bit_cast(typename E::v8, w[b]), o[i]);
-            }
+            for (int i = 0; i < D / 16; ++i)
+                o[i] = E::mma16(__builtin_bit_cast(typename E::v8, vt[i]),
+                                __builtin_bit_cast(typename E::v8, w[b]), o[i]);
             __builtin_amdgcn_wave_barrier();
         }
         at = next;
+    }
+    if (__any(endless)) {
+        for (int32_t first = k0 + wave * kKeys; first < k1; first += stride)
+            for (int32_t key = first; key < k1 && key < first + kKeys; ++key) {
+                const uint32_t pl = place_of(p, page_entry(p, table, key, k1), key, there);
+                if (!there || key <= all_see || key > pos) continue;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[i][e] = add_endless(
+                            o[i][e], v_value<D, kHalf, kFour>(p.kv, pl, head_row, 16 * i + 4 * h4 + e));
+            }
     }
 
     // join the four waves; then this part's rows go out, or to the workspace

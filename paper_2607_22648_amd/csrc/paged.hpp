@@ -1,6 +1,6 @@
 // Operators of the caller's paged cache: block tables, appends and attention
-// (paged_api.hip checks the calls; tables.hip, append.hip and decode.hip hold
-// the kernels). What the kernels share is here.
+// (paged_api.hip checks the calls; tables.hip, append.hip, decode.hip and
+// prompt.hip hold the kernels). What the kernels share is here.
 //
 // One layer of a paged cache is a K plane and a V plane, each
 // [cache block][slab]. A 16-bit slab is [head][slot][dim]. A 4-bit slab is
@@ -83,8 +83,10 @@ struct AttendPlan {
     int32_t splits, part_keys;              // most parts of a request, keys of a part
 };
 
-// Query rows of a tile: the columns of one matrix instruction.
+// Query rows of a decode tile (one matrix instruction's columns) and of a
+// prompt tile.
 constexpr int kDecodeRows = 16;
+constexpr int kPromptRows = 128;
 
 // A request's rows are its (token, head of the group) pairs, token first; its
 // tiles are numbered from offsets * group / rows + r, which leaves room for
@@ -100,5 +102,6 @@ hipError_t launch_append(const Planes& kv, const Rows& k, const Rows& v, const i
 hipError_t launch_read(const Planes& kv, const Rows& k, const Rows& v, const int64_t* slots, int64_t n,
                        hipStream_t s);
 hipError_t launch_decode(const AttendPlan& p, hipStream_t s);
+hipError_t launch_prompt(const AttendPlan& p, hipStream_t s);
 
 }  // namespace ptsd

@@ -70,6 +70,10 @@ int compute_units(int* cus) {
     return PTSTORE_OK;
 }
 
+// Whether a call's rows go 128 or 16 to a tile. The host knows the average
+// request alone.
+bool many_rows(const AttendPlan& p) { return p.n_tokens * p.group > (int64_t)32 * p.R; }
+
 // How a call's keys are split: a part's keys, and the most parts of a request.
 // The host knows the block table's width, not the lengths. Parts are sized so
 // that a batch whose requests all fill their rows has about 16 workgroups a
@@ -183,6 +187,8 @@ int ptstore_attention_workspace(const ptstore_kv_t* kv, int32_t q_heads, int64_t
     if (!bytes) return refuse("ptstore_attention_workspace: null argument");
     if (const char* bad = sized(kv, q_heads, n_tokens, R, max_blocks, &p, &units))
         return refuse_as("ptstore_attention_workspace", bad);
+    *bytes = 0;
+    if (many_rows(p)) return PTSTORE_OK;
     int cus = 0;
     if (const int rc = compute_units(&cus)) return rc;
     split_keys(p.kv, units, max_blocks, cus, &p);
@@ -204,9 +210,13 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
         !rows_ok(a->out, a->out_token_stride, a->out_head_stride))
         return refuse("ptstore_attention: rows of q or out null or not 16-byte aligned");
     if (p.kv.blocks < 1) return refuse("ptstore_attention: the cache has no blocks");
+    const bool prompts = many_rows(p);
     int cus = 0;
-    if (const int rc = compute_units(&cus)) return rc;
-    split_keys(p.kv, units, a->max_blocks, cus, &p);
+    p.splits = 1;
+    if (!prompts) {
+        if (const int rc = compute_units(&cus)) return rc;
+        split_keys(p.kv, units, a->max_blocks, cus, &p);
+    }
     const int64_t need = parts_bytes(p, units);
     if (need > 0 && (a->workspace_bytes < need || !a->workspace || !aligned16(a->workspace)))
         return refuse("ptstore_attention: workspace too small or not 16-byte aligned "
@@ -220,7 +230,7 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
     p.table = a->block_table;
     p.scale2 = a->scale * 1.4426950408889634f;
     p.parts = static_cast<float*>(a->workspace);
-    const hipError_t e = launch_decode(p, (hipStream_t)stream);
+    const hipError_t e = prompts ? launch_prompt(p, (hipStream_t)stream) : launch_decode(p, (hipStream_t)stream);
     return e == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, "ptstore_attention: launch");
 }
 
