@@ -154,14 +154,16 @@ __device__ inline Tile find_tile(const AttendPlan& p, int64_t t, int rows) {
     return f;
 }
 
-// The place of key `key` of a request's pages: cache block << 6 | slot, or -1 if
-// it is at or past `end` or its page does not exist.
+// The block-table entry of key `key` of a request that has keys up to `end` > 0. Past
+// them it is the last one's: loads need no branch, and place_of tells them apart.
 __device__ inline int32_t page_entry(const AttendPlan& p, const int32_t* table, int32_t key, int32_t end) {
-    return key < end ? table[div_page((uint32_t)key, p.kv.div)] : -1;
+    return table[div_page((uint32_t)(key < end ? key : end - 1), p.kv.div)];
 }
 
-__device__ inline uint32_t place_of(const AttendPlan& p, int32_t entry, int32_t key, bool& there) {
-    there = entry >= 0 && entry < (int32_t)p.kv.blocks;
+// The place of that key: cache block << 6 | slot. Block 0's first slot, and not
+// `there`, if it is at or past `end` or its page does not exist.
+__device__ inline uint32_t place_of(const AttendPlan& p, int32_t entry, int32_t key, int32_t end, bool& there) {
+    there = key < end && entry >= 0 && entry < (int32_t)p.kv.blocks;
     const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
     return there ? ((uint32_t)entry << kSlotBits) | slot : 0u;
 }

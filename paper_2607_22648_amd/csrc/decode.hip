@@ -28,12 +28,23 @@ constexpr int kThreads = kWaves * 64;
 // Floats of one (tile, KV head, part) in the workspace: rows, maxima, sums.
 constexpr int part_floats(int dim) { return kDecodeRows * (dim + 2); }
 
-// Swizzle of V's rows in LDS: 16-byte column c of row r is at c ^ turn(r). Two
-// groups of 16 lanes read rows {0-3} and {8-11} (or {16-19} and {24-27}), 32
+// K and V are read once: past the caches' usual order, so that they leave the
+// parts' results there.
+__device__ inline v4u once16(const uint8_t* p) { return __builtin_nontemporal_load((const v4u*)p); }
+__device__ inline v2u once8(const uint8_t* p) { return __builtin_nontemporal_load((const v2u*)p); }
+
+// Swizzle of K's rows in LDS: 16-byte column c of row r is at c ^ turn(r). 16 lanes
+// read one column of rows {0-3, 8-11, 16-19, 24-27} (or those 4 further on).
+template <int D>
+__device__ inline int turn_k(int row) {
+    return D == 128 ? (row & 3) | ((row >> 3) & 3) << 2 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+}
+
+// And of V's: two groups of 16 lanes read rows {0-3} and {8-11} (or {16-19} and {24-27}), 32
 // bytes each, in one pass of the banks: eight rows have to differ in the upper
 // bits. Rows of 128 bytes (dim 64) already differ by parity.
 template <int D>
-__device__ inline int turn(int row) {
+__device__ inline int turn_v(int row) {
     if constexpr (D == 128)
         return 2 * ((row & 3) + 4 * ((row >> 3) & 1));
     else
@@ -110,29 +121,31 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     const int step_key = lane & (kKeys - 1);
     const int32_t stride = kKeys * kWaves;
 
-    v4u kreg[kGroups][kFour ? 1 : kSteps], vreg[kFour ? kKeys / kVKeys : kPieces];
+    v4u kreg[kFour ? kGroups : kPieces], vreg[kFour ? kKeys / kVKeys : kPieces];
     uint8_t kpow[kGroups], vpow[kKeys / kVKeys];
 
     auto load_k = [&](uint32_t place) {
+        if constexpr (kFour) {
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            const int key = 32 * (g >> 1) + 4 * (g & 1) + key_of_row;
-            const uint32_t pl = (uint32_t)__shfl((int)place, key);
-            const uint64_t line = head_row + (pl & 63u);
-            const uint8_t* page = p.kv.k + (uint64_t)(pl >> kSlotBits) * p.kv.slab;
-            if constexpr (kFour) {
+            for (int g = 0; g < kGroups; ++g) {
+                const uint32_t pl = (uint32_t)__shfl((int)place, 32 * (g >> 1) + 4 * (g & 1) + key_of_row);
+                const uint64_t line = head_row + (pl & 63u);
+                const uint8_t* page = p.kv.k + (uint64_t)(pl >> kSlotBits) * p.kv.slab;
                 const uint8_t* at = page + line * (D / 2) + h4 * (D / 8);
                 if constexpr (D == 128) {
-                    kreg[g][0] = *(const v4u*)at;
+                    kreg[g] = once16(at);
                 } else {
-                    const v2u x = *(const v2u*)at;
-                    kreg[g][0] = v4u{x[0], x[1], 0u, 0u};
+                    const v2u x = once8(at);
+                    kreg[g] = v4u{x[0], x[1], 0u, 0u};
                 }
                 kpow[g] = page[p.kv.exponents + line * (D / kGroup) + h4 * (D / 4) / kGroup];
-            } else {
-                const uint8_t* at = page + line * kRow + h4 * 16;
+            }
+        } else {
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) kreg[g][s] = *(const v4u*)(at + s * 64);
+            for (int i = 0; i < kPieces; ++i) {
+                const uint32_t pl = (uint32_t)__shfl((int)place, i * (64 / kLanes) + lane / kLanes);
+                kreg[i] = once16(p.kv.k + (uint64_t)(pl >> kSlotBits) * p.kv.slab +
+                                 (head_row + (pl & 63u)) * kRow + (lane % kLanes) * 16);
             }
         }
     };
@@ -145,9 +158,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 const uint8_t* page = p.kv.v + (uint64_t)(pl >> kSlotBits) * p.kv.slab;
                 const uint8_t* at = page + line * (D / 2) + (lane & 3) * (D / 8);
                 if constexpr (D == 128) {
-                    vreg[i] = *(const v4u*)at;
+                    vreg[i] = once16(at);
                 } else {
-                    const v2u x = *(const v2u*)at;
+                    const v2u x = once8(at);
                     vreg[i] = v4u{x[0], x[1], 0u, 0u};
                 }
                 vpow[i] = page[p.kv.exponents + line * (D / kGroup) + (lane & 3) * (D / 4) / kGroup];
@@ -156,12 +169,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const uint32_t pl = (uint32_t)__shfl((int)place, i * (64 / kLanes) + lane / kLanes);
-                vreg[i] = *(const v4u*)(p.kv.v + (uint64_t)(pl >> kSlotBits) * p.kv.slab +
-                                        (head_row + (pl & 63u)) * kRow + (lane % kLanes) * 16);
+                vreg[i] = once16(p.kv.v + (uint64_t)(pl >> kSlotBits) * p.kv.slab +
+                                 (head_row + (pl & 63u)) * kRow + (lane % kLanes) * 16);
             }
         }
     };
 
+    // The order of loads is fixed (a wait for one waits for all before it): the page
+    // entries of the step after next, the next step's K, the next step's V. Past the
+    // part's end they read block 0, which costs less than a branch.
     int32_t at = k0 + wave * kKeys;
     bool there = false;
     uint32_t place = 0;
@@ -169,11 +185,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     int32_t entry = -1;
     if (at < k1) {
         entry = page_entry(p, table, at + step_key, k1);
-        place = place_of(p, entry, at + step_key, there);
+        place = place_of(p, entry, at + step_key, k1, there);
         valid = __ballot(there);
-        load_k(place);
-        load_v(place);
         entry = page_entry(p, table, at + stride + step_key, k1);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(place);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(place);
+        __builtin_amdgcn_sched_barrier(0);
     }
     uint8_t* const lds = s_mem.v[wave];
     bool endless = false;  // a V value that is not finite lies behind the first row's last key
@@ -181,28 +200,38 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     while (at < k1) {
         // scores of column n: keys 32 b + 8 h4 + 4 (g & 1) + i in s[g][i], b = g >> 1
         v4f s[kGroups];
+        if constexpr (!kFour) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int key = i * (64 / kLanes) + lane / kLanes;
+                *(v4u*)(lds + key * kRow + (((lane % kLanes) ^ turn_k<D>(key)) * 16)) = kreg[i];
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             s[g] = v4f{0, 0, 0, 0};
+            const int key = 4 * (g & 1) + key_of_row;
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
                 v4u a;
                 if constexpr (kFour)
-                    a = widen8(kreg[g][0][t], __uint_as_float((uint32_t)kpow[g] << 23));
+                    a = widen8(kreg[g][t], __uint_as_float((uint32_t)kpow[g] << 23));
                 else
-                    a = kreg[g][t];
+                    a = *(const v4u*)(lds + key * kRow + (((4 * t + h4) ^ turn_k<D>(key)) * 16));
                 s[g] = E::mma16(__builtin_bit_cast(typename E::v8, a), __builtin_bit_cast(typename E::v8, q[t]),
                                 s[g]);
             }
         }
+        __builtin_amdgcn_wave_barrier();
         const int32_t next = at + stride;
         const uint64_t ok = valid;
-        uint32_t next_place = 0;
-        if (next < k1) {
-            next_place = place_of(p, entry, next + step_key, there);
-            valid = __ballot(there);
-            load_k(next_place);
-        }
+        place = place_of(p, entry, next + step_key, k1, there);
+        valid = __ballot(there);
+        entry = page_entry(p, table, next + stride + step_key, k1);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(place);
+        __builtin_amdgcn_sched_barrier(0);
 
         constexpr uint64_t kAll = kKeys == 64 ? ~0ull : 0xFFFFFFFFull;
         const bool edge = k1 - 1 > all_see && at + kKeys - 1 > all_see;
@@ -214,6 +243,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (!((ok >> (key + i)) & 1) || at + key + i > pos) s[g][i] = -INFINITY;
+            }
+            // V's rows that are not there become zeros
+#pragma unroll
+            for (int i = 0; i < (kFour ? kKeys / kVKeys : kPieces); ++i) {
+                const int key = kFour ? i * kVKeys + (lane >> 2) : i * (64 / kLanes) + lane / kLanes;
+                if (!((ok >> key) & 1)) {
+                    vreg[i] = v4u{0u, 0u, 0u, 0u};
+                    if constexpr (kFour) vpow[i] = 0;
+                } else if (!kFour && at + key > all_see) {
+                    endless |= drop_endless<kHalf>(vreg[i]);
+                }
             }
         }
         float most = -INFINITY;
@@ -247,37 +287,32 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 
 #pragma unroll
         for (int b = 0; b < kKeys / 32; ++b) {
-            // V's rows of 32 keys into LDS; rows that are not there as zeros
+            // V's rows of 32 keys into LDS
             if constexpr (kFour) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int key = i * kVKeys + (lane >> 2);
-                    const int j = 2 * b + i;
-                    const bool in = (ok >> (32 * b + key)) & 1;
+                    const int key = i * kVKeys + (lane >> 2), j = 2 * b + i;
                     const float step = __uint_as_float((uint32_t)vpow[j] << 23);
 #pragma unroll
                     for (int c = 0; c < kWords; ++c) {
                         v4u x = widen8(vreg[j][c], step);
-                        if (edge && at + 32 * b + key > all_see && in) endless |= drop_endless<kHalf>(x);
-                        if (!in) x = v4u{0u, 0u, 0u, 0u};
+                        if (edge) endless |= at + 32 * b + key > all_see && drop_endless<kHalf>(x);
                         const int col = (lane & 3) * kWords + c;
-                        *(v4u*)(lds + key * kRow + ((col ^ turn<D>(key)) * 16)) = x;
+                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D>(key)) * 16)) = x;
                     }
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                     const int key = i * (64 / kLanes) + lane / kLanes;
-                    v4u x = vreg[i];
-                    if (edge && at + key > all_see && ((ok >> key) & 1)) endless |= drop_endless<kHalf>(x);
-                    if (!((ok >> key) & 1)) x = v4u{0u, 0u, 0u, 0u};
-                    *(v4u*)(lds + key * kRow + (((lane % kLanes) ^ turn<D>(key)) * 16)) = x;
+                    *(v4u*)(lds + key * kRow + (((lane % kLanes) ^ turn_v<D>(key)) * 16)) = vreg[i];
                 }
             }
             __builtin_amdgcn_wave_barrier();
-            if (b == kKeys / 32 - 1 && next < k1) {
-                load_v(next_place);
-                entry = page_entry(p, table, next + stride + step_key, k1);
+            if (b == kKeys / 32 - 1) {
+                __builtin_amdgcn_sched_barrier(0);
+                load_v(place);
+                __builtin_amdgcn_sched_barrier(0);
             }
             // column d of 32 keys, 8 of them a lane: two transposed reads
             const int vrow = 8 * h4 + (n >> 2);
@@ -285,8 +320,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 const int col = 2 * i + ((n & 3) >> 1), in = (n & 1) * 8;
-                const v2u lo = read_transposed(lds + vrow * kRow + ((col ^ turn<D>(vrow)) * 16) + in);
-                const v2u hi = read_transposed(lds + (vrow + 4) * kRow + ((col ^ turn<D>(vrow + 4)) * 16) + in);
+                const v2u lo = read_transposed(lds + vrow * kRow + ((col ^ turn_v<D>(vrow)) * 16) + in);
+                const v2u hi = read_transposed(lds + (vrow + 4) * kRow + ((col ^ turn_v<D>(vrow + 4)) * 16) + in);
                 vt[i] = join(lo, hi);
             }
 #pragma unroll
@@ -300,7 +335,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     if (__any(endless)) {
         for (int32_t first = k0 + wave * kKeys; first < k1; first += stride)
             for (int32_t key = first; key < k1 && key < first + kKeys; ++key) {
-                const uint32_t pl = place_of(p, page_entry(p, table, key, k1), key, there);
+                const uint32_t pl = place_of(p, page_entry(p, table, key, k1), key, k1, there);
                 if (!there || key <= all_see || key > pos) continue;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)

@@ -161,17 +161,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 
     if (threadIdx.x == 0) s_endless = 0;
     __syncthreads();
-    int32_t entry = page_entry(p, table, lane, end);
+    int32_t entry = steps > 0 ? page_entry(p, table, lane, end) : -1;
     uint64_t ok = 0, ok_next = 0;  // which keys of the step, and of the loaded one, are there
     bool there;
     if (steps > 0) {
-        uint32_t place = place_of(p, entry, lane, there);
+        uint32_t place = place_of(p, entry, lane, end, there);
         ok = __ballot(there);
         load(place);
         entry = page_entry(p, table, kKeys + lane, end);
         store(0, ok, 0);
         if (steps > 1) {
-            place = place_of(p, entry, kKeys + lane, there);
+            place = place_of(p, entry, kKeys + lane, end, there);
             ok_next = __ballot(there);
             load(place);
             entry = page_entry(p, table, 2 * kKeys + lane, end);
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         ok = ok_next;
         if (t + 2 < steps) {
             const int32_t key = (t + 2) * kKeys + lane;
-            const uint32_t place = place_of(p, entry, key, there);
+            const uint32_t place = place_of(p, entry, key, end, there);
             ok_next = __ballot(there);
             load(place);
             entry = page_entry(p, table, key + kKeys, end);
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 
     if (s_endless) {
         for (int32_t key = tile_sees + 1; key < end; ++key) {
-            const uint32_t place = place_of(p, page_entry(p, table, key, end), key, there);
+            const uint32_t place = place_of(p, page_entry(p, table, key, end), key, end, there);
             if (!there || key > pos) continue;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
