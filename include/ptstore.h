@@ -463,7 +463,7 @@ int ptstore_lookup_gather_noalloc(ptstore_t *store, const int32_t *tokens, const
  * exponents, padded to a multiple of 16 bytes. 32 elements along dim share an
  * exponent byte b; element 2i is in the low half of byte i; a code is a sign and
  * one of the levels 0, 0.5, 1, 1.5, 2, 3, 4, 6, and stands for level * 2^(b-127);
- * b = 255 is NaN. A store holds such blocks when it is made with
+ * b = 255 is NaN, and so are 253 and 254, whose values bf16 could not hold. A store holds such blocks when it is made with
  * layer_chunk_bytes of ptstore_kv_slab_bytes: gather and scatter copy slabs
  * whatever they hold. The calls below take and give bf16 for BF16 and MXFP4
  * caches and fp16 for FP16. */
@@ -476,7 +476,7 @@ enum { PTSTORE_KV_BF16 = 0, PTSTORE_KV_FP16 = 1, PTSTORE_KV_MXFP4 = 2 };
 typedef struct {
     void *k;
     void *v;
-    int64_t cache_blocks;  /* 0 .. 2^26 */
+    int64_t cache_blocks;  /* 0 .. 2^30, and at most 64 GiB a plane */
     int32_t kv_heads;
     int32_t head_dim;      /* 64 or 128 */
     int32_t block_tokens;  /* 1 .. 64 */

@@ -85,7 +85,7 @@ __device__ inline uint32_t encode(v4u x, uint32_t& byte) {
 }
 
 __device__ inline v4u decode(uint32_t code, uint32_t byte) {
-    const float step = __uint_as_float(byte << 23);
+    const float step = __uint_as_float((byte >= kEndless ? 255u : byte) << 23);
     v4u x;
     x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 0));
     x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 1));

@@ -96,6 +96,12 @@ __device__ inline v4u widen8(uint32_t code, float step) {
     return x;
 }
 
+// 2^(b - 127) of an exponent byte. From 253 on a code could leave bf16's range: all
+// of them read as NaN, as 255 does.
+__device__ inline float step_of(uint32_t byte) {
+    return __uint_as_float((byte >= kEndless ? 255u : byte) << 23);
+}
+
 // Lowest score kept: what a row starts from instead of minus infinity, so that
 // the differences of two such rows stay numbers.
 constexpr float kLowest = -3.0e38f;
@@ -155,33 +161,83 @@ __device__ inline Tile find_tile(const AttendPlan& p, int64_t t, int rows) {
 }
 
 // The block-table entry of key `key` of a request that has keys up to `end` > 0. Past
-// them it is the last one's: loads need no branch, and place_of tells them apart.
+// them it is the last one's: loads need no branch, and key_row tells them apart.
 __device__ inline int32_t page_entry(const AttendPlan& p, const int32_t* table, int32_t key, int32_t end) {
     return table[div_page((uint32_t)(key < end ? key : end - 1), p.kv.div)];
 }
 
-// The place of that key: cache block << 6 | slot. Block 0's first slot, and not
-// `there`, if it is at or past `end` or its page does not exist.
-__device__ inline uint32_t place_of(const AttendPlan& p, int32_t entry, int32_t key, int32_t end, bool& there) {
-    there = key < end && entry >= 0 && entry < (int32_t)p.kv.blocks;
-    const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
-    return there ? ((uint32_t)entry << kSlotBits) | slot : 0u;
+// A key's row of a head in a plane, in units of 16 bytes (a plane has at most 64 GiB),
+// and the byte of its exponents in a 4-bit one. Block 0's first slot, and not `there`,
+// if the key is at or past `end` or its page does not exist.
+struct KeyRow {
+    uint32_t at;
+    uint64_t power;
+};
+
+template <int D, bool kFour>
+__device__ inline KeyRow key_row(const Planes& kv, int32_t entry, int32_t key, int32_t end, uint32_t head_row,
+                                 bool& there) {
+    there = key < end && entry >= 0 && entry < (int32_t)kv.blocks;
+    const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, kv.div) * kv.div.page;
+    const uint32_t block = there ? (uint32_t)entry : 0u, line = head_row + (there ? slot : 0u);
+    KeyRow r;
+    r.at = block * (kv.slab / 16) + line * (kFour ? D / 32 : D / 8);
+    r.power = kFour ? (uint64_t)block * kv.slab + kv.exponents + line * (D / kGroup) : 0;
+    return r;
 }
 
-// The value at dimension d of the V row at `place` of a head.
+// The exponents of a key's row: a byte each 32 dimensions.
+template <int D>
+__device__ inline uint32_t load_powers(const uint8_t* plane, uint64_t power) {
+    if constexpr (D == 128)
+        return *(const uint32_t*)(plane + power);
+    else
+        return *(const uint16_t*)(plane + power);
+}
+
+// Exponents with those of a key that is not there, or not finite behind `sees`, made
+// smallest: its values are then finite, and a weight of zero keeps them out.
+template <int D>
+__device__ inline uint32_t keep_finite(uint32_t powers, bool there, bool behind, bool& endless) {
+    if (!there) return 0;
+    if (behind) {
+#pragma unroll
+        for (int i = 0; i < D; i += kGroup) {
+            const uint32_t byte = (powers >> (i / kGroup * 8)) & 255u;
+            if (byte >= kEndless) {
+                powers &= ~(255u << (i / kGroup * 8));
+                endless = true;
+            }
+        }
+    }
+    return powers;
+}
+
+// The value at dimension d of the V row `r`.
 template <int D, bool kHalf, bool kFour>
-__device__ inline float v_value(const Planes& kv, uint32_t place, uint64_t head_row, int d) {
-    const uint8_t* page = kv.v + (uint64_t)(place >> kSlotBits) * kv.slab;
-    const uint64_t line = head_row + (place & 63u);
+__device__ inline float v_value(const Planes& kv, const KeyRow& r, int d) {
+    const uint8_t* row = kv.v + ((uint64_t)r.at << 4);
     if constexpr (kFour) {
-        const float step = __uint_as_float((uint32_t)page[kv.exponents + line * (D / kGroup) + d / kGroup] << 23);
-        const uint32_t code = page[line * (D / 2) + d / 2] >> (4 * (d & 1));
-        const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step, 0));
+        const uint32_t code = row[d / 2] >> (4 * (d & 1));
+        const uint32_t two = __builtin_bit_cast(
+            uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, step_of(kv.v[r.power + d / kGroup]), 0));
         return __uint_as_float(two << 16);
     } else {
-        const uint16_t x = *(const uint16_t*)(page + (line * D + d) * 2);
+        const uint16_t x = *(const uint16_t*)(row + d * 2);
         return kHalf ? (float)__builtin_bit_cast(_Float16, x) : __uint_as_float((uint32_t)x << 16);
     }
+}
+
+// The largest of a column's values over the wave: of lanes 16 apart, or 32.
+__device__ inline float larger_16_32(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float larger_32(float x) {
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // Adds to a sum what drop_endless took from it.

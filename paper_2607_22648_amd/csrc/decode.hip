@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     const int32_t all_see = first64 < limit ? (int32_t)first64 : (int32_t)limit;
 
     const int32_t* table = p.table + (int64_t)f.r * p.max_blocks;
-    const uint64_t head_row = (uint64_t)head * p.kv.div.page;
+    const uint32_t head_row = (uint32_t)head * p.kv.div.page;
 
     // queries: column n, 8 consecutive dimensions a lane (4-bit: those of its quarter of a row)
     v4u q[kSteps];
@@ -117,62 +117,49 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 
     // K row of this lane within a row group: key_of_row
     const int key_of_row = 8 * (n >> 2) + (n & 3);
-    // the 64 keys' places, one a lane (32 keys: the upper half repeats them)
+    // the step's keys, one a lane (32 keys: the upper half repeats them)
     const int step_key = lane & (kKeys - 1);
     const int32_t stride = kKeys * kWaves;
 
     v4u kreg[kFour ? kGroups : kPieces], vreg[kFour ? kKeys / kVKeys : kPieces];
-    uint8_t kpow[kGroups], vpow[kKeys / kVKeys];
+    uint32_t kpow = 0, vpow = 0;  // 4-bit: exponents of the lane's key
 
-    auto load_k = [&](uint32_t place) {
+    // A lane's bytes of the rows that the lanes hold: the places in a plane go round
+    // the wave in 32 bits.
+    const uint8_t* const kbase = p.kv.k + (kFour ? h4 * (D / 8) : (lane % kLanes) * 16);
+    const uint8_t* const vbase = p.kv.v + (kFour ? (lane & 3) * (D / 8) : (lane % kLanes) * 16);
+    auto row_at = [&](const uint8_t* base, const KeyRow& r, int key) {
+        return base + ((uint64_t)(uint32_t)__shfl((int)r.at, key) << 4);
+    };
+    auto four = [&](const uint8_t* at) {
+        if constexpr (D == 128) return once16(at);
+        const v2u x = once8(at);
+        return v4u{x[0], x[1], 0u, 0u};
+    };
+    auto load_k = [&](const KeyRow& r) {
         if constexpr (kFour) {
+            kpow = load_powers<D>(p.kv.k, r.power);
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const uint32_t pl = (uint32_t)__shfl((int)place, 32 * (g >> 1) + 4 * (g & 1) + key_of_row);
-                const uint64_t line = head_row + (pl & 63u);
-                const uint8_t* page = p.kv.k + (uint64_t)(pl >> kSlotBits) * p.kv.slab;
-                const uint8_t* at = page + line * (D / 2) + h4 * (D / 8);
-                if constexpr (D == 128) {
-                    kreg[g] = once16(at);
-                } else {
-                    const v2u x = once8(at);
-                    kreg[g] = v4u{x[0], x[1], 0u, 0u};
-                }
-                kpow[g] = page[p.kv.exponents + line * (D / kGroup) + h4 * (D / 4) / kGroup];
-            }
+            for (int g = 0; g < kGroups; ++g)
+                kreg[g] = four(row_at(kbase, r, 32 * (g >> 1) + 4 * (g & 1) + key_of_row));
         } else {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const uint32_t pl = (uint32_t)__shfl((int)place, i * (64 / kLanes) + lane / kLanes);
-                kreg[i] = once16(p.kv.k + (uint64_t)(pl >> kSlotBits) * p.kv.slab +
-                                 (head_row + (pl & 63u)) * kRow + (lane % kLanes) * 16);
-            }
+            for (int i = 0; i < kPieces; ++i) kreg[i] = once16(row_at(kbase, r, i * (64 / kLanes) + lane / kLanes));
         }
     };
-    auto load_v = [&](uint32_t place) {
+    auto load_v = [&](const KeyRow& r) {
         if constexpr (kFour) {
+            vpow = load_powers<D>(p.kv.v, r.power);
 #pragma unroll
-            for (int i = 0; i < kKeys / kVKeys; ++i) {
-                const uint32_t pl = (uint32_t)__shfl((int)place, i * kVKeys + (lane >> 2));
-                const uint64_t line = head_row + (pl & 63u);
-                const uint8_t* page = p.kv.v + (uint64_t)(pl >> kSlotBits) * p.kv.slab;
-                const uint8_t* at = page + line * (D / 2) + (lane & 3) * (D / 8);
-                if constexpr (D == 128) {
-                    vreg[i] = once16(at);
-                } else {
-                    const v2u x = once8(at);
-                    vreg[i] = v4u{x[0], x[1], 0u, 0u};
-                }
-                vpow[i] = page[p.kv.exponents + line * (D / kGroup) + (lane & 3) * (D / 4) / kGroup];
-            }
+            for (int i = 0; i < kKeys / kVKeys; ++i) vreg[i] = four(row_at(vbase, r, i * kVKeys + (lane >> 2)));
         } else {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const uint32_t pl = (uint32_t)__shfl((int)place, i * (64 / kLanes) + lane / kLanes);
-                vreg[i] = once16(p.kv.v + (uint64_t)(pl >> kSlotBits) * p.kv.slab +
-                                 (head_row + (pl & 63u)) * kRow + (lane % kLanes) * 16);
-            }
+            for (int i = 0; i < kPieces; ++i) vreg[i] = once16(row_at(vbase, r, i * (64 / kLanes) + lane / kLanes));
         }
+    };
+    // the exponent of the lane's quarter q of row `key`
+    auto power = [&](uint32_t pow, int key, int quarter) {
+        return ((uint32_t)__shfl((int)pow, key) >> (quarter * (D / 4) / kGroup * 8)) & 255u;
     };
 
     // The order of loads is fixed (a wait for one waits for all before it): the page
@@ -180,12 +167,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     // part's end they read block 0, which costs less than a branch.
     int32_t at = k0 + wave * kKeys;
     bool there = false;
-    uint32_t place = 0;
+    KeyRow place;
     uint64_t valid = 0;
     int32_t entry = -1;
     if (at < k1) {
         entry = page_entry(p, table, at + step_key, k1);
-        place = place_of(p, entry, at + step_key, k1, there);
+        place = key_row<D, kFour>(p.kv, entry, at + step_key, k1, head_row, there);
         valid = __ballot(there);
         entry = page_entry(p, table, at + stride + step_key, k1);
         __builtin_amdgcn_sched_barrier(0);
@@ -212,11 +199,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         for (int g = 0; g < kGroups; ++g) {
             s[g] = v4f{0, 0, 0, 0};
             const int key = 4 * (g & 1) + key_of_row;
+            const float step = kFour ? step_of(power(kpow, 32 * (g >> 1) + key, h4)) : 0.f;
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
                 v4u a;
                 if constexpr (kFour)
-                    a = widen8(kreg[g][t], __uint_as_float((uint32_t)kpow[g] << 23));
+                    a = widen8(kreg[g][t], step);
                 else
                     a = *(const v4u*)(lds + key * kRow + (((4 * t + h4) ^ turn_k<D>(key)) * 16));
                 s[g] = E::mma16(__builtin_bit_cast(typename E::v8, a), __builtin_bit_cast(typename E::v8, q[t]),
@@ -226,7 +214,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         __builtin_amdgcn_wave_barrier();
         const int32_t next = at + stride;
         const uint64_t ok = valid;
-        place = place_of(p, entry, next + step_key, k1, there);
+        place = key_row<D, kFour>(p.kv, entry, next + step_key, k1, head_row, there);
         valid = __ballot(there);
         entry = page_entry(p, table, next + stride + step_key, k1);
         __builtin_amdgcn_sched_barrier(0);
@@ -244,15 +232,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 for (int i = 0; i < 4; ++i)
                     if (!((ok >> (key + i)) & 1) || at + key + i > pos) s[g][i] = -INFINITY;
             }
-            // V's rows that are not there become zeros
+            // V's rows that are not there become zeros (4-bit: finite)
+            if constexpr (kFour) {
+                vpow = keep_finite<D>(vpow, (ok >> lane) & 1, at + lane > all_see, endless);
+            } else {
 #pragma unroll
-            for (int i = 0; i < (kFour ? kKeys / kVKeys : kPieces); ++i) {
-                const int key = kFour ? i * kVKeys + (lane >> 2) : i * (64 / kLanes) + lane / kLanes;
-                if (!((ok >> key) & 1)) {
-                    vreg[i] = v4u{0u, 0u, 0u, 0u};
-                    if constexpr (kFour) vpow[i] = 0;
-                } else if (!kFour && at + key > all_see) {
-                    endless |= drop_endless<kHalf>(vreg[i]);
+                for (int i = 0; i < kPieces; ++i) {
+                    const int key = i * (64 / kLanes) + lane / kLanes;
+                    const bool in = (ok >> key) & 1;
+                    if (!in) vreg[i] = v4u{0u, 0u, 0u, 0u};
+                    if (in && at + key > all_see) endless |= drop_endless<kHalf>(vreg[i]);
                 }
             }
         }
@@ -261,8 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, s[g][i]);
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
+        most = larger_16_32(most);
         const float top2 = fmaxf(top, most * p.scale2);
         if (__any(top2 > top)) {
             const float less = exp2_of(top - top2);
@@ -292,13 +280,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int key = i * kVKeys + (lane >> 2), j = 2 * b + i;
-                    const float step = __uint_as_float((uint32_t)vpow[j] << 23);
+                    const float step = step_of(power(vpow, 32 * b + key, lane & 3));
 #pragma unroll
                     for (int c = 0; c < kWords; ++c) {
-                        v4u x = widen8(vreg[j][c], step);
-                        if (edge) endless |= at + 32 * b + key > all_see && drop_endless<kHalf>(x);
                         const int col = (lane & 3) * kWords + c;
-                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D>(key)) * 16)) = x;
+                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D>(key)) * 16)) = widen8(vreg[j][c], step);
                     }
                 }
             } else {
@@ -335,14 +321,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     if (__any(endless)) {
         for (int32_t first = k0 + wave * kKeys; first < k1; first += stride)
             for (int32_t key = first; key < k1 && key < first + kKeys; ++key) {
-                const uint32_t pl = place_of(p, page_entry(p, table, key, k1), key, k1, there);
+                const KeyRow row = key_row<D, kFour>(p.kv, page_entry(p, table, key, k1), key, k1, head_row, there);
                 if (!there || key <= all_see || key > pos) continue;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        o[i][e] = add_endless(
-                            o[i][e], v_value<D, kHalf, kFour>(p.kv, pl, head_row, 16 * i + 4 * h4 + e));
+                        o[i][e] = add_endless(o[i][e], v_value<D, kHalf, kFour>(p.kv, row, 16 * i + 4 * h4 + e));
             }
     }
 

@@ -15,8 +15,9 @@
 namespace ptsd {
 
 constexpr int kGroup = 32;          // elements that share one exponent
-constexpr int kSlotBits = 6;        // block_tokens <= 64
-constexpr int64_t kMaxCacheBlocks = 1ll << 26;  // a block and a slot share 32 bits
+constexpr uint32_t kEndless = 253;  // exponent bytes from here on read as NaN
+constexpr int64_t kMaxCacheBlocks = 1ll << 30;
+constexpr int64_t kMaxPlane = 1ll << 36;  // bytes: rows are numbered in 16 bytes, 32 bits
 
 // Division of a key's position (below 2^31) by the page size: with 2^s >=
 // 2^31 d and M = ceil(2^s / d), the error M d - 2^s is below d, so n M / 2^s

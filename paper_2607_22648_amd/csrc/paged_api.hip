@@ -42,7 +42,8 @@ const char* planes_of(const ptstore_kv_t* kv, Planes* out) {
     if (!kv) return "null cache";
     const int64_t slab = slab_bytes(kv->kind, kv->kv_heads, kv->head_dim, kv->block_tokens);
     if (slab < 0) return "the cache's kind, heads, head_dim (64, 128) or block_tokens (1..64) is not supported";
-    if (kv->cache_blocks < 0 || kv->cache_blocks > kMaxCacheBlocks) return "cache_blocks out of range (0..2^26)";
+    if (kv->cache_blocks < 0 || kv->cache_blocks > kMaxCacheBlocks) return "cache_blocks out of range (0..2^30)";
+    if (kv->cache_blocks * slab > kMaxPlane) return "a plane of the cache exceeds 64 GiB";
     if (kv->cache_blocks > 0 && (!kv->k || !kv->v || !aligned16(kv->k) || !aligned16(kv->v)))
         return "the cache's planes must be 16-byte aligned";
     out->k = static_cast<uint8_t*>(kv->k);

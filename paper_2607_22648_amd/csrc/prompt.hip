@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     const int steps = (end + kKeys - 1) / kKeys;
 
     const int32_t* table = p.table + (int64_t)f.r * p.max_blocks;
-    const uint64_t head_row = (uint64_t)head * p.kv.div.page;
+    const uint32_t head_row = (uint32_t)head * p.kv.div.page;
 
     V8 q[kSteps];
     {
@@ -100,63 +100,66 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 
     // a step's keys, one a lane; rows 16 wave .. + 15 are this wave's to load
     v4u kreg[kLoads], vreg[kLoads];
-    uint8_t kpow[kLoads], vpow[kLoads];
-    auto load = [&](uint32_t place) {
+    uint32_t kpow = 0, vpow = 0;  // 4-bit: exponents of the lane's key
+    const int lane_at = kFour ? (lane & 3) * (D / 8) : (lane % kLanes) * 16;
+    auto load = [&](const KeyRow& r) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const uint32_t pl = (uint32_t)__shfl((int)place, 16 * wave + i * (64 / kLanes) + lane / kLanes);
-            const uint64_t page = (uint64_t)(pl >> kSlotBits) * p.kv.slab, line = head_row + (pl & 63u);
-            if constexpr (kFour) {
-                const uint64_t at = page + line * (D / 2) + (lane & 3) * (D / 8);
-                const uint64_t pw = page + p.kv.exponents + line * (D / kGroup) + (lane & 3) * (D / 4) / kGroup;
-                if constexpr (D == 128) {
-                    kreg[i] = *(const v4u*)(p.kv.k + at);
-                    vreg[i] = *(const v4u*)(p.kv.v + at);
-                } else {
-                    const v2u a = *(const v2u*)(p.kv.k + at), b = *(const v2u*)(p.kv.v + at);
-                    kreg[i] = v4u{a[0], a[1], 0u, 0u};
-                    vreg[i] = v4u{b[0], b[1], 0u, 0u};
-                }
-                kpow[i] = p.kv.k[pw];
-                vpow[i] = p.kv.v[pw];
+            const uint64_t at =
+                ((uint64_t)(uint32_t)__shfl((int)r.at, 16 * wave + i * (64 / kLanes) + lane / kLanes) << 4) + lane_at;
+            if constexpr (kFour && D == 64) {
+                const v2u a = *(const v2u*)(p.kv.k + at), b = *(const v2u*)(p.kv.v + at);
+                kreg[i] = v4u{a[0], a[1], 0u, 0u};
+                vreg[i] = v4u{b[0], b[1], 0u, 0u};
             } else {
-                const uint64_t at = page + line * kRow + (lane % kLanes) * 16;
                 kreg[i] = *(const v4u*)(p.kv.k + at);
                 vreg[i] = *(const v4u*)(p.kv.v + at);
             }
         }
+        if constexpr (kFour) {
+            kpow = load_powers<D>(p.kv.k, r.power);
+            vpow = load_powers<D>(p.kv.v, r.power);
+        }
     };
-    // step t to LDS; rows that are not there as zeros
+    // step t to LDS; V's rows that are not there as zeros (4-bit: as finite values)
     auto store = [&](int buf, uint64_t ok, int t) {
         const bool edge = t * kKeys + kKeys - 1 > tile_sees;
-        bool endless = false;
-        const v4u zero = {0u, 0u, 0u, 0u};
+        if (ok != ~0ull || edge) {
+            bool endless = false;
+            if constexpr (kFour) {
+                vpow = keep_finite<D>(vpow, (ok >> lane) & 1, t * kKeys + lane > tile_sees, endless);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int row = 16 * wave + i * (64 / kLanes) + lane / kLanes;
+                    const bool in = (ok >> row) & 1;
+                    if (!in) vreg[i] = v4u{0u, 0u, 0u, 0u};
+                    if (in && t * kKeys + row > tile_sees) endless |= drop_endless<kHalf>(vreg[i]);
+                }
+            }
+            if (endless) s_endless = 1;
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int row = 16 * wave + i * (64 / kLanes) + lane / kLanes;
-            const bool in = (ok >> row) & 1;
             uint8_t* const kr = s_k[buf] + row * kRow;
             uint8_t* const vr = s_v[buf] + row * kRow;
             if constexpr (kFour) {
-                const float ks = __uint_as_float((uint32_t)kpow[i] << 23);
-                const float vs = __uint_as_float((uint32_t)vpow[i] << 23);
+                const int shift = (lane & 3) * (D / 4) / kGroup * 8;
+                const float ks = step_of(((uint32_t)__shfl((int)kpow, row) >> shift) & 255u);
+                const float vs = step_of(((uint32_t)__shfl((int)vpow, row) >> shift) & 255u);
 #pragma unroll
                 for (int c = 0; c < kPieces; ++c) {
                     const int col = (lane & 3) * kPieces + c;
-                    const v4u a = widen8(kreg[i][c], ks);
-                    v4u b = widen8(vreg[i][c], vs);
-                    if (edge && t * kKeys + row > tile_sees && in) endless |= drop_endless<kHalf>(b);
-                    *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = in ? a : zero;
-                    *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = in ? b : zero;
+                    *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = widen8(kreg[i][c], ks);
+                    *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = widen8(vreg[i][c], vs);
                 }
             } else {
                 const int col = lane % kLanes;
-                if (edge && t * kKeys + row > tile_sees && in) endless |= drop_endless<kHalf>(vreg[i]);
-                *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = in ? kreg[i] : zero;
-                *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = in ? vreg[i] : zero;
+                *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = kreg[i];
+                *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = vreg[i];
             }
         }
-        if (endless) s_endless = 1;
     };
 
     if (threadIdx.x == 0) s_endless = 0;
@@ -165,13 +168,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     uint64_t ok = 0, ok_next = 0;  // which keys of the step, and of the loaded one, are there
     bool there;
     if (steps > 0) {
-        uint32_t place = place_of(p, entry, lane, end, there);
+        KeyRow place = key_row<D, kFour>(p.kv, entry, lane, end, head_row, there);
         ok = __ballot(there);
         load(place);
         entry = page_entry(p, table, kKeys + lane, end);
         store(0, ok, 0);
         if (steps > 1) {
-            place = place_of(p, entry, kKeys + lane, end, there);
+            place = key_row<D, kFour>(p.kv, entry, kKeys + lane, end, head_row, there);
             ok_next = __ballot(there);
             load(place);
             entry = page_entry(p, table, 2 * kKeys + lane, end);
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         ok = ok_next;
         if (t + 2 < steps) {
             const int32_t key = (t + 2) * kKeys + lane;
-            const uint32_t place = place_of(p, entry, key, end, there);
+            const KeyRow place = key_row<D, kFour>(p.kv, entry, key, end, head_row, there);
             ok_next = __ballot(there);
             load(place);
             entry = page_entry(p, table, key + kKeys, end);
@@ -229,7 +232,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
-            most = fmaxf(most, __shfl_xor(most, 32));
+            most = larger_32(most);
             const float top2 = fmaxf(top, most * p.scale2);
             if (__any(top2 > top + kBehind)) {
                 const float less = exp2_of(top - top2);
@@ -280,14 +283,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 
     if (s_endless) {
         for (int32_t key = tile_sees + 1; key < end; ++key) {
-            const uint32_t place = place_of(p, page_entry(p, table, key, end), key, end, there);
+            const KeyRow row =
+                key_row<D, kFour>(p.kv, page_entry(p, table, key, end), key, end, head_row, there);
             if (!there || key > pos) continue;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    o[i][e] = add_endless(o[i][e], v_value<D, kHalf, kFour>(p.kv, place, head_row,
-                                                                            32 * i + 8 * (e >> 2) + 4 * half + (e & 3)));
+                    o[i][e] = add_endless(
+                        o[i][e], v_value<D, kHalf, kFour>(p.kv, row, 32 * i + 8 * (e >> 2) + 4 * half + (e & 3)));
         }
     }
     if (row0 + n >= all_rows) return;  // both halves of a row leave together

@@ -59,8 +59,11 @@ def test_attention_refuses_on_the_host(P):
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "16-byte" in text()
     a.kv.k = 0x1004
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "planes" in text()
-    kv = P.ptstore_kv_t(0x1000, 0x2000, (1 << 26) + 1, 2, 64, 16, 0)
-    with pytest.raises(P.PTStoreError, match="2\\^26"):
+    kv = P.ptstore_kv_t(0x1000, 0x2000, (1 << 30) + 1, 2, 64, 16, 0)
+    with pytest.raises(P.PTStoreError, match="2\\^30"):
+        P.ptstore_attention_workspace(kv, 4, 1, 1, 4)
+    kv.cache_blocks = (1 << 36) // 4096 + 1
+    with pytest.raises(P.PTStoreError, match="64 GiB"):
         P.ptstore_attention_workspace(kv, 4, 1, 1, 4)
     assert lib.ptstore_kv_append(C.byref(kv), 1, 1, 1, 1, 1, 1, 1, 1, None) == P.PTSTORE_ERR_INVALID
     assert lib.ptstore_kv_append(None, 1, 1, 1, 1, 1, 1, 1, 1, None) == P.PTSTORE_ERR_INVALID
