@@ -566,13 +566,15 @@ typedef struct {
     int32_t max_blocks;
     int32_t q_heads;            /* a multiple of kv.kv_heads */
     float scale;                /* positive, usually 1 / sqrt(head_dim) */
-    void *workspace;            /* the call's own until it is done; need not be cleared */
+    void *workspace;            /* need not be cleared; calls that overlap in time need one
+                                   each */
     int64_t workspace_bytes;
 } ptstore_attention_t;
 
 /* Bytes of workspace an attention of these sizes needs (0: none), 16-byte
- * aligned; it follows from the arguments and the device alone. Host only.
- * Errors: INVALID, HIP. */
+ * aligned. It follows from the cache's heads and head_dim, the device, and whether
+ * the call needs any at all: one workspace serves every call on a layer. Host
+ * only. Errors: INVALID, HIP. */
 int ptstore_attention_workspace(const ptstore_kv_t *kv, int32_t q_heads, int64_t n_tokens, int32_t R,
                                 int32_t max_blocks, int64_t *bytes);
 

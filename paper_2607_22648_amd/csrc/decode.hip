@@ -2,17 +2,24 @@
 // that is checked.
 //
 // Bound by memory: a request's K and V are read once and every other byte is
-// small beside them. So a request's keys are split into parts, one workgroup
-// each (flash-decoding in form: each part keeps its own maximum and sum, and a
-// second kernel joins them), and what matters is bytes in flight.
+// small beside them. What matters is that all compute units read all the time,
+// whatever the lengths. So the batch's work, in steps of keys, is laid out end to end
+// (request, tile of query rows, KV head, step) and cut into equal shares, one
+// for each workgroup that the device holds at once. A share that ends inside a
+// (tile, KV head) leaves its maximum, sum and output in the workspace, two such
+// parts a workgroup at most, and a second kernel joins them. 64 requests of 120 to 8,190
+// keys take the time of as many bytes in equal requests; workgroups for fixed
+// parts of a request were up to 1.3 times slower by how their number fell on the
+// device, and paid their start per part.
 //
-// A workgroup is four waves that share nothing until the end: wave w takes
-// every fourth step of keys of the part. A step's K goes from memory straight into
-// the matrix instruction's operand registers (16 keys a row group, 64
-// consecutive bytes of a row by four lanes), its V through 8 KiB of LDS that only
-// this wave uses, written as rows and read transposed. The next step's loads
-// are issued as soon as a register is free, so that each wave keeps a step's
-// bytes in flight while it computes.
+// A workgroup is four waves that share nothing until a (tile, KV head) is done: wave
+// w takes every fourth piece of a share's keys. K and V rows are loaded whole (four
+// rows of 256 bytes an instruction; rows in 64-byte pieces, as the matrix
+// instruction takes K, reached 5.8 TB/s instead of 6.4), pass through 8 KiB of LDS that
+// only this wave uses, and are read as the matrix instructions want them, V
+// transposed. 4-bit K is loaded in that order from the start: its rows are 64
+// bytes. The next piece's loads are issued as soon as a register is free, so that each wave
+// keeps a piece's bytes in flight while it computes.
 //
 // Query rows are the (token, head of the group) pairs of one KV head, 16 to a
 // tile: with 4 heads to a KV head a single token fills 4 of the 16 columns, and
@@ -25,8 +32,98 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 
-// Floats of one (tile, KV head, part) in the workspace: rows, maxima, sums.
+// Keys of a step: a piece for each wave.
+constexpr int step_keys(bool four) { return kWaves * (four ? 64 : 32); }
+
+// Floats of a part in the workspace: rows, then each one's maximum and sum.
 constexpr int part_floats(int dim) { return kDecodeRows * (dim + 2); }
+
+// A request's work for a KV head: its steps of keys for each of its tiles. A
+// request that sees no key has one step, which writes its zeros.
+struct Work {
+    int64_t begin;  // first token
+    int32_t n;
+    int64_t past;
+    int32_t steps, tiles;
+    __device__ int64_t all() const { return (int64_t)steps * tiles; }
+};
+
+__device__ inline Work work_of(const AttendPlan& p, int r, int step_keys) {
+    Work w;
+    const int64_t a = p.offsets[r], b = p.offsets[r + 1];
+    const bool ok = a >= 0 && b > a && b <= p.n_tokens;
+    w.begin = ok ? a : 0;
+    w.n = ok ? (int32_t)(b - a) : 0;
+    w.past = p.context[r];
+    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
+    int64_t end = w.past + w.n;
+    end = end < 1 ? 1 : (end > limit ? limit : end);
+    w.steps = (int32_t)((end + step_keys - 1) / step_keys);
+    w.tiles = (w.n * p.group + kDecodeRows - 1) / kDecodeRows;
+    return w;
+}
+
+// The shares: share w of `count` has steps [w all / count, (w + 1) all / count).
+struct Shares {
+    int64_t all, count;
+    __device__ int64_t begin(int64_t w) const { return w * all / count; }
+    // the share that has step x: the last that begins at or before it
+    __device__ int64_t of(int64_t x) const { return ((x + 1) * count + all - 1) / all - 1; }
+};
+
+// Sums the batch's work and finds the request `r` that the first (or last) step of
+// share `share` is in, its work and its first step. Every workgroup does so for
+// itself: thread t takes the requests from t ceil(R / threads) on.
+template <int kWavesOf>
+__device__ inline Shares find_step(const AttendPlan& p, int step_keys, int64_t share, bool last, int& r, Work& f,
+                                   int64_t& first) {
+    __shared__ int64_t s_sum[kWavesOf], s_first;
+    __shared__ int s_r;
+    __shared__ Work s_work;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per = (p.R + kWavesOf * 64 - 1) / (kWavesOf * 64);
+    const int r0 = threadIdx.x * per;
+    Work w;
+    int64_t mine = 0;
+    for (int i = 0; i < per && r0 + i < p.R; ++i) {
+        w = work_of(p, r0 + i, step_keys);
+        mine += w.all();
+    }
+    int64_t scan = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t o = __shfl_up(scan, d);
+        if (lane >= d) scan += o;
+    }
+    if (lane == 63) s_sum[wave] = scan;
+    __syncthreads();
+    Shares s{0, p.shares};
+    int64_t before = 0;
+#pragma unroll
+    for (int i = 0; i < kWavesOf; ++i) {
+        if (i < wave) before += s_sum[i];
+        s.all += s_sum[i];
+    }
+    if (s.all < s.count) s.count = s.all;
+    const int64_t at = share < s.count ? (last ? s.begin(share + 1) - 1 : s.begin(share)) : -1, lo = before + scan - mine;
+    if (at >= lo && at < lo + mine) {
+        s_r = r0;
+        s_first = lo;
+        s_work = w;  // of the only request, if `per` is 1
+    }
+    __syncthreads();
+    if (at < 0) return s;
+    r = __builtin_amdgcn_readfirstlane(s_r);
+    first = s_first;
+    if (per == 1) {
+        f = s_work;
+        return s;
+    }
+    while (f = work_of(p, r, step_keys), first + f.all() <= at) {
+        first += f.all();
+        ++r;
+    }
+    return s;
+}
 
 // K and V are read once: past the caches' usual order, so that they leave the
 // parts' results there.
@@ -54,7 +151,8 @@ __device__ inline int turn_v(int row) {
 template <int D, bool kHalf, bool kFour>
 __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     using E = Elem<kHalf>;
-    constexpr int kKeys = kFour ? 64 : 32;        // keys of a step
+    constexpr int kKeys = kFour ? 64 : 32;        // keys of a wave's piece
+    constexpr int kStepKeys = step_keys(kFour);
     constexpr int kGroups = kKeys / 16;           // row groups of 16 keys
     constexpr int kSteps = D / 32;                // matrix steps over the dimension
     constexpr int kRow = D * 2;                   // bytes of a row of V in LDS
@@ -73,31 +171,41 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int n = lane & 15, h4 = lane >> 4;  // query column, quarter
-    const int part = blockIdx.x % p.splits;
-    const int64_t unit = blockIdx.x / p.splits;  // tile, KV head
-    const int head = (int)(unit % p.kv.heads);
-    const Tile f = find_tile(p, unit / p.kv.heads, kDecodeRows);
-    if (f.tile < 0) return;
-
-    // the tile's rows see keys up to `last`; those of this part are [k0, k1)
-    const int rows_left = f.n * p.group - f.tile * kDecodeRows;
-    const int rows = rows_left < kDecodeRows ? rows_left : kDecodeRows;
-    const int row = f.tile * kDecodeRows + (n < rows ? n : rows - 1);
-    const int token = row / p.group, sub = row - token * p.group;
     const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
-    const int64_t last = f.past + (f.tile * kDecodeRows + rows - 1) / p.group;
-    int64_t seen = last + 1;
+    const int head = blockIdx.x % p.kv.heads, share = blockIdx.x / p.kv.heads;
+    int r;
+    int64_t first;  // the request's first step
+    Work f;
+    const Shares shares = find_step<kWaves>(p, kStepKeys, share, false, r, f, first);
+    if (share >= shares.count) return;
+    const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
+    for (int64_t done = share0; done < share1;) {
+    while (done >= first + f.all()) {  // on to the next request with work
+        first += f.all();
+        f = work_of(p, ++r, kStepKeys);
+    }
+    const int tile = (int)((done - first) / f.steps);
+    const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
+    const int step0 = (int)(done - tile0);
+    const int step1 = share1 - tile0 < f.steps ? (int)(share1 - tile0) : f.steps;
+    done = tile0 + step1;
+
+    // the tile's rows see keys up to `end`; those of this share are [k0, k1)
+    const int rows_left = f.n * p.group - tile * kDecodeRows;
+    const int rows = rows_left < kDecodeRows ? rows_left : kDecodeRows;
+    const int row = tile * kDecodeRows + (n < rows ? n : rows - 1);
+    const int token = row / p.group, sub = row - token * p.group;
+    int64_t seen = f.past + (tile * kDecodeRows + rows - 1) / p.group + 1;
     seen = seen < 0 ? 0 : (seen > limit ? limit : seen);
     const int32_t end = (int32_t)seen;
-    const int32_t k0 = part * p.part_keys;
-    if (k0 >= end && part > 0) return;
-    const int32_t k1 = end - k0 < p.part_keys ? end : k0 + p.part_keys;
+    const int32_t k0 = step0 * kStepKeys;
+    const int32_t k1 = end - k0 < (step1 - step0) * kStepKeys ? end : step1 * kStepKeys;
     const int64_t pos64 = f.past + token;  // the last key this lane's query sees
     const int32_t pos = pos64 < limit ? (int32_t)pos64 : (int32_t)limit;
-    const int64_t first64 = f.past + f.tile * kDecodeRows / p.group;
+    const int64_t first64 = f.past + tile * kDecodeRows / p.group;
     const int32_t all_see = first64 < limit ? (int32_t)first64 : (int32_t)limit;
 
-    const int32_t* table = p.table + (int64_t)f.r * p.max_blocks;
+    const int32_t* table = p.table + (int64_t)r * p.max_blocks;
     const uint32_t head_row = (uint32_t)head * p.kv.div.page;
 
     // queries: column n, 8 consecutive dimensions a lane (4-bit: those of its quarter of a row)
@@ -185,20 +293,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     bool endless = false;  // a V value that is not finite lies behind the first row's last key
 
     while (at < k1) {
+        // LDS addresses are formed anew each time: kept, they take two dozen registers
+        int here = lane;
+        asm volatile("" : "+v"(here));
         // scores of column n: keys 32 b + 8 h4 + 4 (g & 1) + i in s[g][i], b = g >> 1
         v4f s[kGroups];
         if constexpr (!kFour) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
-                const int key = i * (64 / kLanes) + lane / kLanes;
-                *(v4u*)(lds + key * kRow + (((lane % kLanes) ^ turn_k<D>(key)) * 16)) = kreg[i];
+                const int key = i * (64 / kLanes) + here / kLanes;
+                *(v4u*)(lds + key * kRow + (((here % kLanes) ^ turn_k<D>(key)) * 16)) = kreg[i];
             }
             __builtin_amdgcn_wave_barrier();
         }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             s[g] = v4f{0, 0, 0, 0};
-            const int key = 4 * (g & 1) + key_of_row;
+            const int key = 4 * (g & 1) + 8 * ((here & 15) >> 2) + (here & 3);
             const float step = kFour ? step_of(power(kpow, 32 * (g >> 1) + key, h4)) : 0.f;
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
@@ -206,7 +317,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 if constexpr (kFour)
                     a = widen8(kreg[g][t], step);
                 else
-                    a = *(const v4u*)(lds + key * kRow + (((4 * t + h4) ^ turn_k<D>(key)) * 16));
+                    a = *(const v4u*)(lds + key * kRow + (((4 * t + (here >> 4)) ^ turn_k<D>(key)) * 16));
                 s[g] = E::mma16(__builtin_bit_cast(typename E::v8, a), __builtin_bit_cast(typename E::v8, q[t]),
                                 s[g]);
             }
@@ -279,19 +390,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
             if constexpr (kFour) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int key = i * kVKeys + (lane >> 2), j = 2 * b + i;
+                    const int key = i * kVKeys + (here >> 2), j = 2 * b + i;
                     const float step = step_of(power(vpow, 32 * b + key, lane & 3));
+                    // every other pair of rows takes a lane's words in the order 1 0 3 2: turn_v
+                    // leaves the lowest bit of the columns that 16 lanes write alike
+                    const int swap = (key >> 1) & 1;
 #pragma unroll
                     for (int c = 0; c < kWords; ++c) {
-                        const int col = (lane & 3) * kWords + c;
-                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D>(key)) * 16)) = widen8(vreg[j][c], step);
+                        const int col = (here & 3) * kWords + (c ^ swap);
+                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D>(key)) * 16)) =
+                            widen8(swap ? vreg[j][c ^ 1] : vreg[j][c], step);
                     }
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
-                    const int key = i * (64 / kLanes) + lane / kLanes;
-                    *(v4u*)(lds + key * kRow + (((lane % kLanes) ^ turn_v<D>(key)) * 16)) = vreg[i];
+                    const int key = i * (64 / kLanes) + here / kLanes;
+                    *(v4u*)(lds + key * kRow + (((here % kLanes) ^ turn_v<D>(key)) * 16)) = vreg[i];
                 }
             }
             __builtin_amdgcn_wave_barrier();
@@ -301,11 +416,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 __builtin_amdgcn_sched_barrier(0);
             }
             // column d of 32 keys, 8 of them a lane: two transposed reads
-            const int vrow = 8 * h4 + (n >> 2);
+            const int m = here & 15, vrow = 8 * (here >> 4) + (m >> 2);
             v4u vt[D / 16];
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-                const int col = 2 * i + ((n & 3) >> 1), in = (n & 1) * 8;
+                const int col = 2 * i + ((m & 3) >> 1), in = (m & 1) * 8;
                 const v2u lo = read_transposed(lds + vrow * kRow + ((col ^ turn_v<D>(vrow)) * 16) + in);
                 const v2u hi = read_transposed(lds + (vrow + 4) * kRow + ((col ^ turn_v<D>(vrow + 4)) * 16) + in);
                 vt[i] = join(lo, hi);
@@ -344,98 +459,123 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     __syncthreads();
     constexpr int kRowLanes = D / 8;
     const int orow = threadIdx.x / kRowLanes, oc = threadIdx.x % kRowLanes;
-    if (orow >= rows) return;
-    float all = kLowest;
+    if (orow < rows) {
+        float all = kLowest;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) all = fmaxf(all, s_max[w][orow]);
-    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
+        for (int w = 0; w < kWaves; ++w) all = fmaxf(all, s_max[w][orow]);
+        float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float part_of = exp2_of(s_max[w][orow] - all);
-        total += part_of * s_sum[w][orow];
+        for (int w = 0; w < kWaves; ++w) {
+            const float part_of = exp2_of(s_max[w][orow] - all);
+            total += part_of * s_sum[w][orow];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += part_of * s_mem.o[w][orow * kOut + oc * 8 + e];
-    }
-    if (end > p.part_keys) {
-        float* to = p.parts + ((uint64_t)unit * p.splits + part) * part_floats(D);
-        *(v4f*)(to + orow * D + oc * 8) = v4f{acc[0], acc[1], acc[2], acc[3]};
-        *(v4f*)(to + orow * D + oc * 8 + 4) = v4f{acc[4], acc[5], acc[6], acc[7]};
-        if (oc == 0) {
-            to[kDecodeRows * D + orow] = all;
-            to[kDecodeRows * (D + 1) + orow] = total;
+            for (int e = 0; e < 8; ++e) acc[e] += part_of * s_mem.o[w][orow * kOut + oc * 8 + e];
         }
-        return;
-    }
-    const int out_row = f.tile * kDecodeRows + orow;
-    const int ot = out_row / p.group, os = out_row - ot * p.group;
-    const int64_t oh = (int64_t)head * p.group + os;
-    // no key, or none with a weight: zeros, and the logarithm of nothing
-    const float inv = total != 0.f ? 1.f / total : 0.f;
-    v4u x;
+        if (step0 > 0 || step1 < f.steps) {
+            // a part: of a tile that began in an earlier share, or one that goes on
+            float* to = p.parts + (2 * (int64_t)blockIdx.x + (step0 > 0 ? 0 : 1)) * part_floats(D);
+            *(v4f*)(to + orow * D + oc * 8) = v4f{acc[0], acc[1], acc[2], acc[3]};
+            *(v4f*)(to + orow * D + oc * 8 + 4) = v4f{acc[4], acc[5], acc[6], acc[7]};
+            if (oc == 0) *(v2f*)(to + kDecodeRows * D + 2 * orow) = v2f{all, total};
+        } else {
+            const int out_row = tile * kDecodeRows + orow;
+            const int ot = out_row / p.group, os = out_row - ot * p.group;
+            const int64_t oh = (int64_t)head * p.group + os;
+            // no key, or none with a weight: zeros, and the logarithm of nothing
+            const float inv = total != 0.f ? 1.f / total : 0.f;
+            v4u x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = pack2<kHalf>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    *(v4u*)((uint8_t*)p.out.p + ((f.begin + ot) * p.out.token + oh * p.out.head + oc * 8) * 2) = x;
-    if (p.lse && oc == 0)
-        p.lse[(f.begin + ot) * p.q_heads + oh] =
-            total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+            for (int e = 0; e < 4; ++e) x[e] = pack2<kHalf>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+            *(v4u*)((uint8_t*)p.out.p + ((f.begin + ot) * p.out.token + oh * p.out.head + oc * 8) * 2) = x;
+            if (p.lse && oc == 0)
+                p.lse[(f.begin + ot) * p.q_heads + oh] =
+                    total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+        }
+    }
+    __syncthreads();  // the next tile writes there
+    }
 }
 
-// Joins the parts of tiles that have more than one: a workgroup a (tile, KV head).
-template <int D, bool kHalf>
-__global__ __launch_bounds__(kThreads) void k_join(AttendPlan p) {
-    const int64_t unit = blockIdx.x;
-    const int head = (int)(unit % p.kv.heads);
-    const Tile f = find_tile(p, unit / p.kv.heads, kDecodeRows);
-    if (f.tile < 0) return;
-    const int rows_left = f.n * p.group - f.tile * kDecodeRows;
+// Joins the parts of a tile that several shares have: the workgroup of the share
+// that it begins in and the KV head, a wave a row. The wave's halves (dim 64: quarters)
+// take every other part, 4 dimensions a lane, several parts in flight. (A kernel of
+// its own: joined by the workgroup that writes the last part, which has to pass the parts
+// through memory that all dies see, one request of 32,768 keys takes 45 us, not 34.)
+constexpr int kJoinWaves = 8;
+
+template <int D, bool kHalf, bool kFour>
+__global__ __launch_bounds__(kJoinWaves * 64) void k_join(AttendPlan p) {
+    constexpr int kRowLanes = D / 4, kPhases = 64 / kRowLanes, kFlight = 8;
+    const int lane = threadIdx.x & 63, phase = lane / kRowLanes, c = lane % kRowLanes;
+    const int head = blockIdx.x % p.kv.heads, share = blockIdx.x / p.kv.heads;
+    int r;
+    int64_t first;
+    Work f;
+    const Shares shares = find_step<kJoinWaves>(p, step_keys(kFour), share, true, r, f, first);
+    if (share >= shares.count) return;
+    const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
+    const int tile = (int)((share1 - 1 - first) / f.steps);
+    const int64_t tile0 = first + (int64_t)tile * f.steps, tile1 = tile0 + f.steps;
+    if (tile0 < share0 || tile1 <= share1) return;
+    const int parts = (int)(shares.of(tile1 - 1) - share + 1);
+    const int rows_left = f.n * p.group - tile * kDecodeRows;
     const int rows = rows_left < kDecodeRows ? rows_left : kDecodeRows;
-    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
-    int64_t seen = f.past + (f.tile * kDecodeRows + rows - 1) / p.group + 1;
-    if (seen > limit) seen = limit;
-    if (seen <= p.part_keys) return;
-    const int parts = (int)((seen + p.part_keys - 1) / p.part_keys);
-    constexpr int kRowLanes = D / 8;
-    const int orow = threadIdx.x / kRowLanes, oc = threadIdx.x % kRowLanes;
-    if (orow >= rows) return;
-    const float* from = p.parts + (uint64_t)unit * p.splits * part_floats(D);
-    float all = kLowest;
-    for (int i = 0; i < parts; ++i)
-        all = fmaxf(all, from[(int64_t)i * part_floats(D) + kDecodeRows * D + orow]);
-    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
-    for (int i = 0; i < parts; ++i) {
-        const float* part = from + (int64_t)i * part_floats(D);
-        const float part_of = exp2_of(part[kDecodeRows * D + orow] - all);
-        total += part_of * part[kDecodeRows * (D + 1) + orow];
-        const v4f a = *(const v4f*)(part + orow * D + oc * 8), b = *(const v4f*)(part + orow * D + oc * 8 + 4);
+    // this share's second part, then the first of each following
+    const float* from = p.parts + (2 * (int64_t)blockIdx.x + 1) * part_floats(D);
+    const int64_t next = 2ll * p.kv.heads * part_floats(D);
+    auto part_at = [&](int i) { return from + i * next - (i > 0 ? part_floats(D) : 0); };
+    for (int row = threadIdx.x >> 6; row < rows; row += kJoinWaves) {
+        float all = kLowest;
+        for (int i = lane; i < parts; i += 64) all = fmaxf(all, part_at(i)[kDecodeRows * D + 2 * row]);
+        for (int d = 32; d; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
+        v4f acc = {0, 0, 0, 0};
+        float total = 0.f;
+        for (int i0 = phase; i0 < parts; i0 += kPhases * kFlight) {
+            v4f o[kFlight];
+            v2f ms[kFlight];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            acc[e] += part_of * a[e];
-            acc[4 + e] += part_of * b[e];
+            for (int u = 0; u < kFlight; ++u) {
+                const int i = i0 + u * kPhases;
+                const float* part = part_at(i < parts ? i : i0);
+                o[u] = *(const v4f*)(part + row * D + c * 4);
+                ms[u] = *(const v2f*)(part + kDecodeRows * D + 2 * row);
+                if (i >= parts) ms[u][0] = -INFINITY;
+            }
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) {
+                const float part_of = exp2_of(ms[u][0] - all);
+                if (part_of == 0.f) continue;  // nothing of it counts, and 0 * infinity would
+                total += part_of * ms[u][1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += part_of * o[u][e];
+            }
         }
-    }
-    const int out_row = f.tile * kDecodeRows + orow;
-    const int ot = out_row / p.group, os = out_row - ot * p.group;
-    const int64_t oh = (int64_t)head * p.group + os;
-    const float inv = total != 0.f ? 1.f / total : 0.f;
-    v4u x;
+        for (int d = kRowLanes; d < 64; d <<= 1) {
+            total += __shfl_xor(total, d);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = pack2<kHalf>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    *(v4u*)((uint8_t*)p.out.p + ((f.begin + ot) * p.out.token + oh * p.out.head + oc * 8) * 2) = x;
-    if (p.lse && oc == 0)
-        p.lse[(f.begin + ot) * p.q_heads + oh] =
-            total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
+        }
+        if (phase) continue;
+        const int out_row = tile * kDecodeRows + row;
+        const int ot = out_row / p.group, os = out_row - ot * p.group;
+        const int64_t oh = (int64_t)head * p.group + os;
+        const float inv = total != 0.f ? 1.f / total : 0.f;
+        const v2u x = {pack2<kHalf>(acc[0] * inv, acc[1] * inv), pack2<kHalf>(acc[2] * inv, acc[3] * inv)};
+        *(v2u*)((uint8_t*)p.out.p + ((f.begin + ot) * p.out.token + oh * p.out.head + c * 4) * 2) = x;
+        if (p.lse && c == 0)
+            p.lse[(f.begin + ot) * p.q_heads + oh] =
+                total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 template <int D, bool kHalf, bool kFour>
 hipError_t run(const AttendPlan& p, hipStream_t s) {
-    const int64_t units = tile_bound(p.n_tokens, p.group, p.R, kDecodeRows) * p.kv.heads;
-    hipLaunchKernelGGL((k_decode<D, kHalf, kFour>), dim3((unsigned)(units * p.splits)), dim3(kThreads), 0, s, p);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.splits > 1) {
-        hipLaunchKernelGGL((k_join<D, kHalf>), dim3((unsigned)units), dim3(kThreads), 0, s, p);
-        e = hipGetLastError();
-    }
-    return e;
+    const dim3 grid((unsigned)(p.shares * p.kv.heads));
+    hipLaunchKernelGGL((k_decode<D, kHalf, kFour>), grid, dim3(kThreads), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_join<D, kHalf, kFour>), grid, dim3(kJoinWaves * 64), 0, s, p);
+    return hipGetLastError();
 }
 
 template <int D>
@@ -445,6 +585,18 @@ hipError_t run_kind(const AttendPlan& p, hipStream_t s) {
 }
 
 }  // namespace
+
+// As many as fill the device: two workgroups a compute unit. More, smaller ones even
+// out no better and pay their start: 64 requests of 8,191 keys 345 us, with four a
+// compute unit 358, with eight 369.
+int decode_shares(const Planes& kv, int cus) {
+    const int shares = 2 * cus / kv.heads;
+    return shares > 0 ? shares : 1;
+}
+
+int64_t decode_workspace(const Planes& kv, int shares) {
+    return 2ll * shares * kv.heads * part_floats(kv.dim) * (int64_t)sizeof(float);
+}
 
 hipError_t launch_decode(const AttendPlan& p, hipStream_t s) {
     return p.kv.dim == 128 ? run_kind<128>(p, s) : run_kind<64>(p, s);

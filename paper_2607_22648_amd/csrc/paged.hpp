@@ -80,8 +80,8 @@ struct AttendPlan {
     int64_t n_tokens;
     int32_t R, max_blocks, q_heads, group;  // group: query heads of a KV head
     float scale2;                           // scale * log2(e): scores in base 2
-    float* parts;                           // workspace of the split over keys
-    int32_t splits, part_keys;              // most parts of a request, keys of a part
+    float* parts;                           // workspace: two parts of a tile a share and head
+    int32_t shares;                         // of the batch's work (decode.hip)
 };
 
 // Query rows of a decode tile (one matrix instruction's columns) and of a
@@ -102,6 +102,8 @@ hipError_t launch_append(const Planes& kv, const Rows& k, const Rows& v, const i
                          hipStream_t s);
 hipError_t launch_read(const Planes& kv, const Rows& k, const Rows& v, const int64_t* slots, int64_t n,
                        hipStream_t s);
+int decode_shares(const Planes& kv, int cus);
+int64_t decode_workspace(const Planes& kv, int shares);  // bytes
 hipError_t launch_decode(const AttendPlan& p, hipStream_t s);
 hipError_t launch_prompt(const AttendPlan& p, hipStream_t s);
 

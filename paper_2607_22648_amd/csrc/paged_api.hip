@@ -2,6 +2,7 @@
 // host, launch rules, no allocation and no state.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 
@@ -63,11 +64,16 @@ bool rows_ok(const void* p, int64_t token, int64_t head) {
     return p && aligned16(p) && token % 8 == 0 && head % 8 == 0;
 }
 
+// Compute units of the current device, asked for once a device.
 int compute_units(int* cus) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
     int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess ||
-        hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
+    if (hipGetDevice(&dev) != hipSuccess) return set_last_error(PTSTORE_ERR_HIP, "ptstore_attention: device query");
+    if (dev >= 0 && dev < kDevices && (*cus = known[dev].load(std::memory_order_relaxed)) > 0) return PTSTORE_OK;
+    if (hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
         return set_last_error(PTSTORE_ERR_HIP, "ptstore_attention: device query");
+    if (dev >= 0 && dev < kDevices) known[dev].store(*cus, std::memory_order_relaxed);
     return PTSTORE_OK;
 }
 
@@ -75,27 +81,9 @@ int compute_units(int* cus) {
 // request alone.
 bool many_rows(const AttendPlan& p) { return p.n_tokens * p.group > (int64_t)32 * p.R; }
 
-// How a call's keys are split: a part's keys, and the most parts of a request.
-// The host knows the block table's width, not the lengths. Parts are sized so
-// that a batch whose requests all fill their rows has about 16 workgroups a
-// compute unit (ragged batches even out over them; a part's start and its
-// partial result cost about 2 % of 1,024 keys), and no part is below 256 keys
-// (64 a wave).
-void split_keys(const Planes& kv, int64_t units, int32_t max_blocks, int cus, AttendPlan* p) {
-    const int64_t keys = (int64_t)max_blocks * kv.div.page;
-    int64_t part = (units * keys + 16 * cus - 1) / (16 * cus);
-    part = (part + 255) / 256 * 256;
-    p->part_keys = (int32_t)(part < 256 ? 256 : (part > kMaxKeys ? kMaxKeys : part));
-    p->splits = (int32_t)((keys + p->part_keys - 1) / p->part_keys);
-}
-
-int64_t parts_bytes(const AttendPlan& p, int64_t units) {
-    return p.splits > 1 ? units * p.splits * kDecodeRows * (p.kv.dim + 2) * 4 : 0;
-}
-
 // Checks the sizes and fills what the workspace and the launch follow from.
 const char* sized(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int32_t R, int32_t max_blocks,
-                  AttendPlan* p, int64_t* units) {
+                  AttendPlan* p) {
     if (const char* bad = planes_of(kv, &p->kv)) return bad;
     if (q_heads < 1 || q_heads % kv->kv_heads) return "q_heads must be a multiple of the cache's heads";
     if (R < 0 || max_blocks < 1 || (int64_t)R * max_blocks > kMaxEntries || n_tokens < 0 ||
@@ -108,8 +96,8 @@ const char* sized(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int
     p->max_blocks = max_blocks;
     p->q_heads = q_heads;
     p->group = q_heads / kv->kv_heads;
-    *units = tile_bound(n_tokens, p->group, R, kDecodeRows) * kv->kv_heads;
-    if (*units >= kMaxGrid) return "too many tiles for one call";
+    if (tile_bound(n_tokens, p->group, R, kDecodeRows) * kv->kv_heads >= kMaxGrid)
+        return "too many tiles for one call";
     return nullptr;
 }
 
@@ -184,24 +172,21 @@ int ptstore_kv_read(const ptstore_kv_t* kv, void* k, int64_t k_token_stride, int
 int ptstore_attention_workspace(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int32_t R,
                                 int32_t max_blocks, int64_t* bytes) {
     AttendPlan p;
-    int64_t units;
     if (!bytes) return refuse("ptstore_attention_workspace: null argument");
-    if (const char* bad = sized(kv, q_heads, n_tokens, R, max_blocks, &p, &units))
+    if (const char* bad = sized(kv, q_heads, n_tokens, R, max_blocks, &p))
         return refuse_as("ptstore_attention_workspace", bad);
     *bytes = 0;
     if (many_rows(p)) return PTSTORE_OK;
     int cus = 0;
     if (const int rc = compute_units(&cus)) return rc;
-    split_keys(p.kv, units, max_blocks, cus, &p);
-    *bytes = parts_bytes(p, units);
+    *bytes = decode_workspace(p.kv, decode_shares(p.kv, cus));
     return PTSTORE_OK;
 }
 
 int ptstore_attention(const ptstore_attention_t* a, void* stream) {
     if (!a) return refuse("ptstore_attention: null argument");
     AttendPlan p;
-    int64_t units;
-    if (const char* bad = sized(&a->kv, a->q_heads, a->n_tokens, a->R, a->max_blocks, &p, &units))
+    if (const char* bad = sized(&a->kv, a->q_heads, a->n_tokens, a->R, a->max_blocks, &p))
         return refuse_as("ptstore_attention", bad);
     if (!(a->scale > 0.f) || !std::isfinite(a->scale * 1.4426950408889634f))
         return refuse("ptstore_attention: scale must be positive and finite");
@@ -212,17 +197,14 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
         return refuse("ptstore_attention: rows of q or out null or not 16-byte aligned");
     if (p.kv.blocks < 1) return refuse("ptstore_attention: the cache has no blocks");
     const bool prompts = many_rows(p);
-    int cus = 0;
-    p.splits = 1;
     if (!prompts) {
+        int cus = 0;
         if (const int rc = compute_units(&cus)) return rc;
-        split_keys(p.kv, units, a->max_blocks, cus, &p);
+        p.shares = decode_shares(p.kv, cus);
+        if (a->workspace_bytes < decode_workspace(p.kv, p.shares) || !a->workspace || !aligned16(a->workspace))
+            return refuse("ptstore_attention: workspace too small or not 16-byte aligned "
+                          "(ptstore_attention_workspace)");
     }
-    const int64_t need = parts_bytes(p, units);
-    if (need > 0 && (a->workspace_bytes < need || !a->workspace || !aligned16(a->workspace)))
-        return refuse("ptstore_attention: workspace too small or not 16-byte aligned "
-                      "(ptstore_attention_workspace)");
-    if (units * p.splits >= kMaxGrid) return refuse("ptstore_attention: too many tiles for one call");
     p.q = Rows{a->q, a->q_token_stride, a->q_head_stride};
     p.out = Rows{a->out, a->out_token_stride, a->out_head_stride};
     p.lse = a->lse;

@@ -148,11 +148,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                 const int shift = (lane & 3) * (D / 4) / kGroup * 8;
                 const float ks = step_of(((uint32_t)__shfl((int)kpow, row) >> shift) & 255u);
                 const float vs = step_of(((uint32_t)__shfl((int)vpow, row) >> shift) & 255u);
+                // turn_v leaves the low bits of the columns that 16 lanes write alike: rows
+                // take a lane's words in orders of their own
+                const bool one = D == 128 ? row & 1 : (row >> 1) & 1, two = D == 128 && (row & 2);
+                const v4u a = one ? v4u{vreg[i][1], vreg[i][0], vreg[i][3], vreg[i][2]} : vreg[i];
+                const v4u w = two ? v4u{a[2], a[3], a[0], a[1]} : a;
+                const int turned = (one ? 1 : 0) | (two ? 2 : 0);
 #pragma unroll
                 for (int c = 0; c < kPieces; ++c) {
-                    const int col = (lane & 3) * kPieces + c;
+                    const int col = (lane & 3) * kPieces + c, vcol = (lane & 3) * kPieces + (c ^ turned);
                     *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = widen8(kreg[i][c], ks);
-                    *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = widen8(vreg[i][c], vs);
+                    *(v4u*)(vr + ((vcol ^ turn_v<D>(row)) * 16)) = widen8(w[c], vs);
                 }
             } else {
                 const int col = lane % kLanes;

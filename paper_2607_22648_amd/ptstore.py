@@ -7,6 +7,7 @@ import time: there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -721,6 +722,7 @@ class PrefixStore:
                 _wrap_device(b.prio, b.capacity, torch.int64))
 
 
+_CURRENT = contextlib.nullcontext()  # tensors for the current stream
 _KV_KINDS = {"bf16": PTSTORE_KV_BF16, "fp16": PTSTORE_KV_FP16, "mxfp4": PTSTORE_KV_MXFP4}
 
 
@@ -752,6 +754,7 @@ class PagedCache:
             raise ValueError(f"data must be a contiguous device tensor of {nbytes} bytes")
         self.data = data
         self.dtype = _KV_DTYPES[_KV_KINDS[kind]]
+        self._workspaces = {}
         self._planes = []
         at = data.data_ptr()
         for h, slab in zip(heads, slabs):
@@ -766,20 +769,33 @@ class PagedCache:
     @staticmethod
     def _on(stream):
         """A context in which tensors are allocated for `stream` (a torch stream or a raw handle)."""
-        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        if stream is None:
+            return _CURRENT
+        if not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(int(stream))
-        return torch.cuda.stream(stream)  # no change where it is None
+        return torch.cuda.stream(stream)
+
+    def _workspace(self, stream) -> torch.Tensor:
+        """The workspace of a stream: one serves every layer, and the calls on it in turn."""
+        handle = _stream(stream)
+        ws = self._workspaces.get(handle)
+        if ws is None:
+            need = max(ptstore_attention_workspace(kv, kv.kv_heads, 1, 1, 1) for kv in self._planes)
+            with self._on(stream):
+                ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
+                if not torch.cuda.is_current_stream_capturing():  # a graph keeps its own
+                    self._workspaces[handle] = ws
+        return ws
 
     def tables(self, offsets, context, block_table, free_blocks, n_tokens: int, held=None, first=None,
                stream=None):
         """Give the batch's requests their blocks: fills the new entries of `block_table` and
         returns (slots, positions, held after, next free entry)."""
-        dev = offsets.device
         with self._on(stream):
-            slots = torch.empty(n_tokens, dtype=torch.int64, device=dev)
-            positions = torch.empty(n_tokens, dtype=torch.int32, device=dev)
-            held_out = torch.empty(block_table.shape[0], dtype=torch.int32, device=dev)
-            next_free = torch.empty(1, dtype=torch.int64, device=dev)
+            slots = offsets.new_empty(n_tokens)
+            positions = context.new_empty(n_tokens)
+            held_out = context.new_empty(block_table.shape[0])
+            next_free = offsets.new_empty(1)
         ptstore_block_tables(offsets, context, held, self.block_tokens, free_blocks, first, block_table,
                              slots, positions, held_out, next_free, stream)
         return slots, positions, held_out, next_free
@@ -800,16 +816,15 @@ class PagedCache:
     def attend(self, layer: int, q, offsets, context, block_table, scale: Optional[float] = None, out=None,
                lse: bool = False, workspace=None, stream=None):
         """Causal attention of q [tokens, q_heads, head_dim] over a layer: out, or (out, lse).
-        scale: 1 / sqrt(head_dim) unless given. A `workspace` (uint8) is used if it is large enough."""
+        scale: 1 / sqrt(head_dim) unless given. workspace: one of the caller's,
+        instead of the one that the cache keeps for the stream."""
         kv = self._planes[layer]
-        n, heads = q.shape[0], q.shape[1]
-        need = ptstore_attention_workspace(kv, heads, n, *_table(offsets, block_table))
         with self._on(stream):
             if out is None:
-                out = torch.empty((n, heads, kv.head_dim), dtype=q.dtype, device=q.device)
-            sums = torch.empty((n, heads), dtype=torch.float32, device=q.device) if lse else None
-            if need and (workspace is None or workspace.numel() < need):
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+                out = q.new_empty(q.shape)
+            sums = q.new_empty(q.shape[:2], dtype=torch.float32) if lse else None
+        if workspace is None:
+            workspace = self._workspace(stream)
         ptstore_attention(kv, q, out, sums, offsets, context, block_table,
                           kv.head_dim ** -0.5 if scale is None else scale, workspace, stream)
         return (out, sums) if lse else out

@@ -401,6 +401,22 @@ def test_attention_in_a_graph(P, reqs):
         assert torch.equal(out, c.cache.attend(0, q, off, ctx, table))
 
 
+def test_attention_first_call_in_a_graph(P):
+    """A cache whose first attention is captured: replays and later eager calls agree."""
+    c = Case(P, "bf16", 2, 4, 128, 16, [(1, 3000), (1, 40)], seed=13)
+    q, off, ctx, table = c.q.cuda(), c.off.cuda(), c.ctx.cuda(), c.table.cuda()
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.attend(0, q, off, ctx, table, out=out)
+    for i in range(4):
+        q.copy_(torch.randn_like(q))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, c.cache.attend(0, q, off, ctx, table))
+
+
 def test_attention_on_other_streams(P):
     """Two streams at once, by stream and by raw handle, each with its own workspace."""
     c = Case(P, "bf16", 2, 4, 128, 16, [(1, 4000), (1, 3500)], seed=14)
@@ -456,6 +472,9 @@ def test_refusals(P):
     refused("slots 3", lambda: c.cache.append(0, k, k, s[:3]), ValueError)
     refused("int64", lambda: c.cache.append(0, k, k, s.int()), ValueError)
     empty = P.PagedCache(1, 2, 64, 0)
+    one_row = (kv, q[:1], out[:1], None, torch.tensor([0, 1], device="cuda"), ctx, table, 1.0)
+    refused("workspace", lambda: P.ptstore_attention(*one_row))
+    refused("workspace", lambda: P.ptstore_attention(*one_row, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda")))
     refused("no blocks", lambda: empty.attend(0, q, off, ctx, table))
     # nothing to do is no error
     assert c.cache.attend(0, q[:0], torch.zeros(2, dtype=torch.int64, device="cuda"), ctx, table).shape[0] == 0
