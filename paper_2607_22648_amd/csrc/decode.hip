@@ -80,7 +80,7 @@ __device__ inline Shares find_step(const AttendPlan& p, int step_keys, int64_t s
     __shared__ int64_t s_sum[kWavesOf], s_first;
     __shared__ int s_r;
     __shared__ Work s_work;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per = (p.R + kWavesOf * 64 - 1) / (kWavesOf * 64);
     const int r0 = threadIdx.x * per;
     Work w;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     } s_mem;
     __shared__ float s_max[kWaves][kDecodeRows], s_sum[kWaves][kDecodeRows];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, h4 = lane >> 4;  // query column, quarter
     const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
     const int head = blockIdx.x % p.kv.heads, share = blockIdx.x / p.kv.heads;
@@ -217,6 +217,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         for (int s = 0; s < kSteps; ++s)
             q[s] = *(const v4u*)(at + (kFour ? h4 * (D / 4) + s * 8 : s * 32 + h4 * 8) * 2);
     }
+    // The queries are loaded before K and V and waited for on every path here: where
+    // one path left that to the loop, each step's wait would be for its V as well.
+    __builtin_amdgcn_sched_barrier(0);
+    auto have_queries = [&] {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) asm volatile("" ::"v"(q[s]));
+    };
 
     v4f o[D / 16];
 #pragma unroll
@@ -282,12 +289,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         entry = page_entry(p, table, at + step_key, k1);
         place = key_row<D, kFour>(p.kv, entry, at + step_key, k1, head_row, there);
         valid = __ballot(there);
+        have_queries();
         entry = page_entry(p, table, at + stride + step_key, k1);
         __builtin_amdgcn_sched_barrier(0);
         load_k(place);
         __builtin_amdgcn_sched_barrier(0);
         load_v(place);
         __builtin_amdgcn_sched_barrier(0);
+    } else {
+        have_queries();
     }
     uint8_t* const lds = s_mem.v[wave];
     bool endless = false;  // a V value that is not finite lies behind the first row's last key

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     __shared__ uint8_t s_k[2][kKeys * kRow], s_v[2][kKeys * kRow];
     __shared__ int s_endless;  // a V value that is not finite lies behind the first row's last key
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int head = blockIdx.x % p.kv.heads;
     // the last tiles of a request see the most keys: they go first
