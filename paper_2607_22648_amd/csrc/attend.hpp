@@ -160,10 +160,12 @@ __device__ inline Tile find_tile(const AttendPlan& p, int64_t t, int rows) {
     return f;
 }
 
-// The block-table entry of key `key` of a request that has keys up to `end` > 0. Past
-// them it is the last one's: loads need no branch, and key_row tells them apart.
+// The block-table entry of key `key` of a request that has keys up to `end`. Past
+// them it is the last one's (the first, if there is no key): loads need no branch, and
+// key_row tells them apart.
 __device__ inline int32_t page_entry(const AttendPlan& p, const int32_t* table, int32_t key, int32_t end) {
-    return table[div_page((uint32_t)(key < end ? key : end - 1), p.kv.div)];
+    const int32_t last = end > 0 ? end - 1 : 0;
+    return table[div_page((uint32_t)(key < last ? key : last), p.kv.div)];
 }
 
 // A key's row of a head in a plane, in units of 16 bytes (a plane has at most 64 GiB),

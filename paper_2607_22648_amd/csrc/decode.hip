@@ -217,13 +217,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         for (int s = 0; s < kSteps; ++s)
             q[s] = *(const v4u*)(at + (kFour ? h4 * (D / 4) + s * 8 : s * 32 + h4 * 8) * 2);
     }
-    // The queries are loaded before K and V and waited for on every path here: where
-    // one path left that to the loop, each step's wait would be for its V as well.
     __builtin_amdgcn_sched_barrier(0);
-    auto have_queries = [&] {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) asm volatile("" ::"v"(q[s]));
-    };
 
     v4f o[D / 16];
 #pragma unroll
@@ -277,28 +271,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
         return ((uint32_t)__shfl((int)pow, key) >> (quarter * (D / 4) / kGroup * 8)) & 255u;
     };
 
-    // The order of loads is fixed (a wait for one waits for all before it): the page
-    // entries of the step after next, the next step's K, the next step's V. Past the
-    // part's end they read block 0, which costs less than a branch.
+    // The order of loads is fixed, since a wait for one waits for all before it: the
+    // queries; then, for each piece, the page entries of the piece after it, its K, its V.
+    // None depends on a branch, past which a wait would have to allow for either
+    // way: what lies past the share's end reads block 0.
     int32_t at = k0 + wave * kKeys;
-    bool there = false;
-    KeyRow place;
-    uint64_t valid = 0;
-    int32_t entry = -1;
-    if (at < k1) {
-        entry = page_entry(p, table, at + step_key, k1);
-        place = key_row<D, kFour>(p.kv, entry, at + step_key, k1, head_row, there);
-        valid = __ballot(there);
-        have_queries();
-        entry = page_entry(p, table, at + stride + step_key, k1);
-        __builtin_amdgcn_sched_barrier(0);
-        load_k(place);
-        __builtin_amdgcn_sched_barrier(0);
-        load_v(place);
-        __builtin_amdgcn_sched_barrier(0);
-    } else {
-        have_queries();
-    }
+    bool there;
+    int32_t entry = page_entry(p, table, at + step_key, k1);
+    KeyRow place = key_row<D, kFour>(p.kv, entry, at + step_key, k1, head_row, there);
+    uint64_t valid = __ballot(there);
+    entry = page_entry(p, table, at + stride + step_key, k1);
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(place);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(place);
+    __builtin_amdgcn_sched_barrier(0);
     uint8_t* const lds = s_mem.v[wave];
     bool endless = false;  // a V value that is not finite lies behind the first row's last key
 
