@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         }
     };
     // step t to LDS; V's rows that are not there as zeros (4-bit: as finite values)
-    auto store = [&](int buf, uint64_t ok, int t) {
+    auto store = [&](int buf, uint64_t ok, int t, int here) {
         const bool edge = t * kKeys + kKeys - 1 > tile_sees;
         if (ok != ~0ull || edge) {
             bool endless = false;
@@ -141,11 +141,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = 16 * wave + i * (64 / kLanes) + lane / kLanes;
+            const int row = 16 * wave + i * (64 / kLanes) + here / kLanes;
             uint8_t* const kr = s_k[buf] + row * kRow;
             uint8_t* const vr = s_v[buf] + row * kRow;
             if constexpr (kFour) {
-                const int shift = (lane & 3) * (D / 4) / kGroup * 8;
+                const int shift = (here & 3) * (D / 4) / kGroup * 8;
                 const float ks = step_of(((uint32_t)__shfl((int)kpow, row) >> shift) & 255u);
                 const float vs = step_of(((uint32_t)__shfl((int)vpow, row) >> shift) & 255u);
                 // turn_v leaves the low bits of the columns that 16 lanes write alike: rows
@@ -156,12 +156,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                 const int turned = (one ? 1 : 0) | (two ? 2 : 0);
 #pragma unroll
                 for (int c = 0; c < kPieces; ++c) {
-                    const int col = (lane & 3) * kPieces + c, vcol = (lane & 3) * kPieces + (c ^ turned);
+                    const int col = (here & 3) * kPieces + c, vcol = (here & 3) * kPieces + (c ^ turned);
                     *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = widen8(kreg[i][c], ks);
                     *(v4u*)(vr + ((vcol ^ turn_v<D>(row)) * 16)) = widen8(w[c], vs);
                 }
             } else {
-                const int col = lane % kLanes;
+                const int col = here % kLanes;
                 *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = kreg[i];
                 *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = vreg[i];
             }
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         ok = __ballot(there);
         load(place);
         entry = page_entry(p, table, kKeys + lane, end);
-        store(0, ok, 0);
+        store(0, ok, 0, lane);
         if (steps > 1) {
             place = key_row<D, kFour>(p.kv, entry, kKeys + lane, end, head_row, there);
             ok_next = __ballot(there);
@@ -188,16 +188,20 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     }
     __syncthreads();
 
-    // row of K that accumulator row m of a 32-key piece stands for: lanes then hold
-    // 8 consecutive keys of each 16
-    const int a8 = n >> 3, key_of_row = 16 * (a8 >> 1) + 8 * ((n >> 2) & 1) + 4 * (a8 & 1) + (n & 3);
-
     for (int t = 0; t < steps; ++t) {
         const int buf = t & 1;
         const int32_t at = t * kKeys;
         const bool active = at <= some_see;
+        // LDS addresses are formed anew each time: kept, they take registers of which
+        // there are none to spare
+        int here = lane;
+        asm volatile("" : "+v"(here));
         v16f s[2];
         if (active) {
+            // row of K that accumulator row m of a 32-key piece stands for: lanes then hold
+            // 8 consecutive keys of each 16
+            const int m = here & 31, m8 = m >> 3;
+            const int key_of_row = 16 * (m8 >> 1) + 8 * ((m >> 2) & 1) + 4 * (m8 & 1) + (m & 3);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int row = 32 * c + key_of_row;
@@ -206,12 +210,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                 for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    const v4u a = *(const v4u*)(kr + (((2 * i + half) ^ turn_k<D>(row)) * 16));
+                    const v4u a = *(const v4u*)(kr + (((2 * i + (here >> 5)) ^ turn_k<D>(key_of_row)) * 16));
                     s[c] = E::mma32(__builtin_bit_cast(V8, a), q[i], s[c]);
                 }
             }
         }
-        if (t + 1 < steps) store(buf ^ 1, ok_next, t + 1);
+        if (t + 1 < steps) store(buf ^ 1, ok_next, t + 1, here);
         const uint64_t ok_now = ok;
         ok = ok_next;
         if (t + 2 < steps) {
@@ -225,13 +229,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             // keys 32 c + 16 (e >> 3) + 8 half + (e & 7) in s[c][e]
             const bool some_hidden = ok_now != ~0ull || at + kKeys - 1 > all_see;
             if (some_hidden) {
+                // the keys that are there and that the row sees, from bit 0 those of s[0][0] on
+                const int32_t ahead = pos - at;
+                uint64_t seen = ahead < 0 ? 0 : (ahead > 62 ? ~0ull : (2ull << ahead) - 1);
+                seen = (seen & ok_now) >> (8 * (here >> 5));
+                const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int key = 32 * c + 16 * (e >> 3) + 8 * half + (e & 7);
-                        if (!((ok_now >> key) & 1) || at + key > pos) s[c][e] = -INFINITY;
-                    }
+                    for (int e = 0; e < 16; ++e)
+                        if (!(bits[c] & (1u << (16 * (e >> 3) + (e & 7))))) s[c][e] = -INFINITY;
             }
             float most = -INFINITY;
 #pragma unroll
@@ -264,7 +271,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                     w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
             }
             // column d of 16 keys, 8 of them a lane: two transposed reads
-            const int g = lane >> 4, l16 = lane & 15;  // 16 lanes: dims 16 (g & 1), keys 8 (g >> 1)
+            const int g = here >> 4, l16 = here & 15;  // 16 lanes: dims 16 (g & 1), keys 8 (g >> 1)
             const int vrow0 = 8 * (g >> 1) + (l16 >> 2);
             const int vcol = 2 * (g & 1) + ((l16 & 3) >> 1), vin = (l16 & 1) * 8;
 #pragma unroll
@@ -274,9 +281,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
                     const int col = 4 * i + vcol;
-                    const v2u lo = read_transposed(s_v[buf] + r0 * kRow + ((col ^ turn_v<D>(r0)) * 16) + vin);
+                    const v2u lo = read_transposed(s_v[buf] + r0 * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
                     const v2u hi =
-                        read_transposed(s_v[buf] + (r0 + 4) * kRow + ((col ^ turn_v<D>(r0 + 4)) * 16) + vin);
+                        read_transposed(s_v[buf] + (r0 + 4) * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
                     vt[i] = join(lo, hi);
                 }
 #pragma unroll
