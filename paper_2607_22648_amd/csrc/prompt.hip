@@ -68,15 +68,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     const int row_at = row0 + n < all_rows ? row0 + n : all_rows - 1;
     const int token = row_at / p.group, sub = row_at - token * p.group;
     auto clip = [&](int64_t x) { return (int32_t)(x < -1 ? -1 : (x < limit ? x : limit - 1)); };
-    // the last key that the tile's last and first row, the wave's first and last and this row see
+    // the last key that the tile's last and first row, the wave's first and this row see
     const int last_row = f.tile * kPromptRows + kPromptRows - 1 < all_rows ? f.tile * kPromptRows + kPromptRows - 1
                                                                             : all_rows - 1;
     const int32_t end = clip(f.past + last_row / p.group) + 1;
     const int first_row = row0 < all_rows ? row0 : all_rows - 1;
-    const int wave_last = row0 + 31 < all_rows ? row0 + 31 : all_rows - 1;
     const int32_t tile_sees = clip(f.past + f.tile * kPromptRows / p.group);
     const int32_t all_see = clip(f.past + first_row / p.group);
-    const int32_t some_see = row0 < all_rows ? clip(f.past + wave_last / p.group) : -1;
     const int32_t pos = clip(f.past + token);
     const int steps = (end + kKeys - 1) / kKeys;
 
@@ -191,28 +189,25 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     for (int t = 0; t < steps; ++t) {
         const int buf = t & 1;
         const int32_t at = t * kKeys;
-        const bool active = at <= some_see;
         // LDS addresses are formed anew each time: kept, they take registers of which
         // there are none to spare
         int here = lane;
         asm volatile("" : "+v"(here));
         v16f s[2];
-        if (active) {
-            // row of K that accumulator row m of a 32-key piece stands for: lanes then hold
-            // 8 consecutive keys of each 16
-            const int m = here & 31, m8 = m >> 3;
-            const int key_of_row = 16 * (m8 >> 1) + 8 * ((m >> 2) & 1) + 4 * (m8 & 1) + (m & 3);
+        // row of K that accumulator row m of a 32-key piece stands for: lanes then hold
+        // 8 consecutive keys of each 16
+        const int m = here & 31, m8 = m >> 3;
+        const int key_of_row = 16 * (m8 >> 1) + 8 * ((m >> 2) & 1) + 4 * (m8 & 1) + (m & 3);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int row = 32 * c + key_of_row;
-                const uint8_t* kr = s_k[buf] + row * kRow;
+        for (int c = 0; c < 2; ++c) {
+            const int row = 32 * c + key_of_row;
+            const uint8_t* kr = s_k[buf] + row * kRow;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
+            for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    const v4u a = *(const v4u*)(kr + (((2 * i + (here >> 5)) ^ turn_k<D>(key_of_row)) * 16));
-                    s[c] = E::mma32(__builtin_bit_cast(V8, a), q[i], s[c]);
-                }
+            for (int i = 0; i < kSteps; ++i) {
+                const v4u a = *(const v4u*)(kr + (((2 * i + (here >> 5)) ^ turn_k<D>(key_of_row)) * 16));
+                s[c] = E::mma32(__builtin_bit_cast(V8, a), q[i], s[c]);
             }
         }
         if (t + 1 < steps) store(buf ^ 1, ok_next, t + 1, here);
@@ -225,71 +220,69 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             load(place);
             entry = page_entry(p, table, key + kKeys, end);
         }
-        if (active) {
-            // keys 32 c + 16 (e >> 3) + 8 half + (e & 7) in s[c][e]
-            const bool some_hidden = ok_now != ~0ull || at + kKeys - 1 > all_see;
-            if (some_hidden) {
-                // the keys that are there and that the row sees, from bit 0 those of s[0][0] on
-                const int32_t ahead = pos - at;
-                uint64_t seen = ahead < 0 ? 0 : (ahead > 62 ? ~0ull : (2ull << ahead) - 1);
-                seen = (seen & ok_now) >> (8 * (here >> 5));
-                const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (!(bits[c] & (1u << (16 * (e >> 3) + (e & 7))))) s[c][e] = -INFINITY;
-            }
-            float most = -INFINITY;
+        // keys 32 c + 16 (e >> 3) + 8 half + (e & 7) in s[c][e]
+        const bool some_hidden = ok_now != ~0ull || at + kKeys - 1 > all_see;
+        if (some_hidden) {
+            // the keys that are there and that the row sees, from bit 0 those of s[0][0] on
+            const int32_t ahead = pos - at;
+            uint64_t seen = ahead < 0 ? 0 : (ahead > 62 ? ~0ull : (2ull << ahead) - 1);
+            seen = (seen & ok_now) >> (8 * (here >> 5));
+            const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
-            most = larger_32(most);
-            const float top2 = fmaxf(top, most * p.scale2);
-            if (__any(top2 > top + kBehind)) {
-                const float less = exp2_of(top - top2);
-                sum *= less;
+                for (int e = 0; e < 16; ++e)
+                    if (!(bits[c] & (1u << (16 * (e >> 3) + (e & 7))))) s[c][e] = -INFINITY;
+        }
+        float most = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[i][e] *= less;
-                top = top2;
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
+        most = larger_32(most);
+        const float top2 = fmaxf(top, most * p.scale2);
+        if (__any(top2 > top + kBehind)) {
+            const float less = exp2_of(top - top2);
+            sum *= less;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] *= less;
+            top = top2;
+        }
+        v4u w[4];  // weights of 16 keys each
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[c][e] = exp2_of(__builtin_fmaf(s[c][e], p.scale2, -top));
+                sum += s[c][e];
             }
-            v4u w[4];  // weights of 16 keys each
+            // weights enter the second product as 16-bit values, as V does: the error
+            // of a weight is below the output's own rounding and averages over the keys
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int e = 0; e < 8; ++e)
+                w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
+        }
+        // column d of 16 keys, 8 of them a lane: two transposed reads
+        const int g = here >> 4, l16 = here & 15;  // 16 lanes: dims 16 (g & 1), keys 8 (g >> 1)
+        const int vrow0 = 8 * (g >> 1) + (l16 >> 2);
+        const int vcol = 2 * (g & 1) + ((l16 & 3) >> 1), vin = (l16 & 1) * 8;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[c][e] = exp2_of(__builtin_fmaf(s[c][e], p.scale2, -top));
-                    sum += s[c][e];
-                }
-                // weights enter the second product as 16-bit values, as V does: the error
-                // of a weight is below the output's own rounding and averages over the keys
+        for (int b = 0; b < 4; ++b) {
+            v4u vt[D / 32];
+            const int r0 = 16 * b + vrow0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
+            for (int i = 0; i < D / 32; ++i) {
+                const int col = 4 * i + vcol;
+                const v2u lo = read_transposed(s_v[buf] + r0 * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
+                const v2u hi =
+                    read_transposed(s_v[buf] + (r0 + 4) * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
+                vt[i] = join(lo, hi);
             }
-            // column d of 16 keys, 8 of them a lane: two transposed reads
-            const int g = here >> 4, l16 = here & 15;  // 16 lanes: dims 16 (g & 1), keys 8 (g >> 1)
-            const int vrow0 = 8 * (g >> 1) + (l16 >> 2);
-            const int vcol = 2 * (g & 1) + ((l16 & 3) >> 1), vin = (l16 & 1) * 8;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                v4u vt[D / 32];
-                const int r0 = 16 * b + vrow0;
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const int col = 4 * i + vcol;
-                    const v2u lo = read_transposed(s_v[buf] + r0 * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
-                    const v2u hi =
-                        read_transposed(s_v[buf] + (r0 + 4) * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
-                    vt[i] = join(lo, hi);
-                }
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i)
-                    o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b]), o[i]);
-            }
+            for (int i = 0; i < D / 32; ++i)
+                o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b]), o[i]);
         }
         __syncthreads();
     }
