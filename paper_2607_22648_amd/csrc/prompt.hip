@@ -14,6 +14,8 @@
 // of one row, and the row's maximum and sum need one exchange between the wave's
 // halves; the weights are then already where the second product O^T = V^T P^T
 // wants them (see attend.hpp), and V is read from LDS transposed.
+#include <type_traits>
+
 #include "attend.hpp"
 
 namespace ptsd {
@@ -51,7 +53,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     constexpr int kLoads = 16 * kLanes / 64;     // loads of a wave's 16 rows
     constexpr int kPieces = kFour ? D / 32 : 1;  // 16-byte pieces in LDS of a lane's load
 
-    __shared__ uint8_t s_k[2][kKeys * kRow], s_v[2][kKeys * kRow];
+    // two buffers of K, two of V
+    constexpr int kTile = kKeys * kRow;
+    __shared__ uint8_t s_mem[4 * kTile];
     __shared__ int s_endless;  // a V value that is not finite lies behind the first row's last key
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -119,8 +123,48 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             vpow = load_powers<D>(p.kv.v, r.power);
         }
     };
+    // LDS addresses of a lane, the rest of which are constants: the swizzles of a row do
+    // not change with the parts of its number that are left out here. Writes: row
+    // 16 wave + i rows of a load + .. (K: turned by i, too).
+    const int at_row = 16 * wave + lane / kLanes;
+    uint32_t k_write[kFour ? kPieces : kLoads], v_write[kFour ? kPieces : 1];
+    const int turned = kFour ? (D == 128 ? at_row & 3 : (at_row >> 1) & 1) : 0;
+    if constexpr (kFour) {
+        // V: turn_v leaves the low bits of the columns that 16 lanes write alike, so rows
+        // take a lane's words in orders of their own
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) {
+            k_write[c] = at_row * kRow + ((((lane & 3) * kPieces + c) ^ turn_k<D>(at_row)) * 16);
+            v_write[c] = at_row * kRow + ((((lane & 3) * kPieces + (c ^ turned)) ^ turn_v<D>(at_row)) * 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            k_write[i] = at_row * kRow + (((lane % kLanes) ^ turn_k<D>(at_row + i * (64 / kLanes))) * 16);
+        v_write[0] = at_row * kRow + (((lane % kLanes) ^ turn_v<D>(at_row)) * 16);
+    }
+    // K reads: row of K that accumulator row m of a 32-key piece stands for, so that lanes
+    // then hold 8 consecutive keys of each 16; column 2 i + half.
+    uint32_t k_read[kSteps];
+    {
+        const int m8 = n >> 3, row = 16 * (m8 >> 1) + 8 * ((n >> 2) & 1) + 4 * (m8 & 1) + (n & 3);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) k_read[i] = row * kRow + (((2 * i + half) ^ turn_k<D>(row)) * 16);
+    }
+    // V reads: 16 lanes take dimensions 16 (g & 1) .., keys 8 (g >> 1) .. of each 16.
+    uint32_t v_read[D / 32];
+    {
+        const int g = lane >> 4, l16 = lane & 15, row = 8 * (g >> 1) + (l16 >> 2);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+            v_read[i] = row * kRow + (((4 * i + 2 * (g & 1) + ((l16 & 3) >> 1)) ^ turn_v<D>(row)) * 16) + (l16 & 1) * 8;
+    }
+
     // step t to LDS; V's rows that are not there as zeros (4-bit: as finite values)
-    auto store = [&](int buf, uint64_t ok, int t, int here) {
+    auto store = [&](auto buffer, uint64_t ok, int t) {
+        constexpr int buf = decltype(buffer)::value;
+        uint8_t* const km = s_mem + buf * kTile;
+        uint8_t* const vm = s_mem + (2 + buf) * kTile;
         const bool edge = t * kKeys + kKeys - 1 > tile_sees;
         if (ok != ~0ull || edge) {
             bool endless = false;
@@ -129,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             } else {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
-                    const int row = 16 * wave + i * (64 / kLanes) + lane / kLanes;
+                    const int row = at_row + i * (64 / kLanes);
                     const bool in = (ok >> row) & 1;
                     if (!in) vreg[i] = v4u{0u, 0u, 0u, 0u};
                     if (in && t * kKeys + row > tile_sees) endless |= drop_endless<kHalf>(vreg[i]);
@@ -137,31 +181,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             }
             if (endless) s_endless = 1;
         }
+        if constexpr (kFour) {
+            const int shift = (lane & 3) * (D / 4) / kGroup * 8;
+            const float ks = step_of(((uint32_t)__shfl((int)kpow, at_row) >> shift) & 255u);
+            const float vs = step_of(((uint32_t)__shfl((int)vpow, at_row) >> shift) & 255u);
+            const v4u a = turned & 1 ? v4u{vreg[0][1], vreg[0][0], vreg[0][3], vreg[0][2]} : vreg[0];
+            const v4u w = turned & 2 ? v4u{a[2], a[3], a[0], a[1]} : a;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int row = 16 * wave + i * (64 / kLanes) + here / kLanes;
-            uint8_t* const kr = s_k[buf] + row * kRow;
-            uint8_t* const vr = s_v[buf] + row * kRow;
-            if constexpr (kFour) {
-                const int shift = (here & 3) * (D / 4) / kGroup * 8;
-                const float ks = step_of(((uint32_t)__shfl((int)kpow, row) >> shift) & 255u);
-                const float vs = step_of(((uint32_t)__shfl((int)vpow, row) >> shift) & 255u);
-                // turn_v leaves the low bits of the columns that 16 lanes write alike: rows
-                // take a lane's words in orders of their own
-                const bool one = D == 128 ? row & 1 : (row >> 1) & 1, two = D == 128 && (row & 2);
-                const v4u a = one ? v4u{vreg[i][1], vreg[i][0], vreg[i][3], vreg[i][2]} : vreg[i];
-                const v4u w = two ? v4u{a[2], a[3], a[0], a[1]} : a;
-                const int turned = (one ? 1 : 0) | (two ? 2 : 0);
+            for (int c = 0; c < kPieces; ++c) {
+                *(v4u*)(km + k_write[c]) = widen8(kreg[0][c], ks);
+                *(v4u*)(vm + v_write[c]) = widen8(w[c], vs);
+            }
+        } else {
 #pragma unroll
-                for (int c = 0; c < kPieces; ++c) {
-                    const int col = (here & 3) * kPieces + c, vcol = (here & 3) * kPieces + (c ^ turned);
-                    *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = widen8(kreg[i][c], ks);
-                    *(v4u*)(vr + ((vcol ^ turn_v<D>(row)) * 16)) = widen8(w[c], vs);
-                }
-            } else {
-                const int col = here % kLanes;
-                *(v4u*)(kr + ((col ^ turn_k<D>(row)) * 16)) = kreg[i];
-                *(v4u*)(vr + ((col ^ turn_v<D>(row)) * 16)) = vreg[i];
+            for (int i = 0; i < kLoads; ++i) {
+                *(v4u*)(km + k_write[i] + i * (64 / kLanes) * kRow) = kreg[i];
+                *(v4u*)(vm + v_write[0] + i * (64 / kLanes) * kRow) = vreg[i];
             }
         }
     };
@@ -176,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         ok = __ballot(there);
         load(place);
         entry = page_entry(p, table, kKeys + lane, end);
-        store(0, ok, 0, lane);
+        store(std::integral_constant<int, 0>{}, ok, 0);
         if (steps > 1) {
             place = key_row<D, kFour>(p.kv, entry, kKeys + lane, end, head_row, there);
             ok_next = __ballot(there);
@@ -186,31 +221,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     }
     __syncthreads();
 
-    for (int t = 0; t < steps; ++t) {
-        const int buf = t & 1;
+    auto turn = [&](auto buffer, int t) {
+        constexpr int buf = decltype(buffer)::value;
+        const uint8_t* const km = s_mem + buf * kTile;
+        const uint8_t* const vm = s_mem + (2 + buf) * kTile;
         const int32_t at = t * kKeys;
-        // LDS addresses are formed anew each time: kept, they take registers of which
-        // there are none to spare
-        int here = lane;
-        asm volatile("" : "+v"(here));
         v16f s[2];
-        // row of K that accumulator row m of a 32-key piece stands for: lanes then hold
-        // 8 consecutive keys of each 16
-        const int m = here & 31, m8 = m >> 3;
-        const int key_of_row = 16 * (m8 >> 1) + 8 * ((m >> 2) & 1) + 4 * (m8 & 1) + (m & 3);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const int row = 32 * c + key_of_row;
-            const uint8_t* kr = s_k[buf] + row * kRow;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const v4u a = *(const v4u*)(kr + (((2 * i + (here >> 5)) ^ turn_k<D>(key_of_row)) * 16));
-                s[c] = E::mma32(__builtin_bit_cast(V8, a), q[i], s[c]);
-            }
+            for (int i = 0; i < kSteps; ++i)
+                s[c] = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(km + k_read[i] + c * 32 * kRow)), q[i], s[c]);
         }
-        if (t + 1 < steps) store(buf ^ 1, ok_next, t + 1, here);
+        if (t + 1 < steps) store(std::integral_constant<int, buf ^ 1>{}, ok_next, t + 1);
         const uint64_t ok_now = ok;
         ok = ok_next;
         if (t + 2 < steps) {
@@ -226,7 +251,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             // the keys that are there and that the row sees, from bit 0 those of s[0][0] on
             const int32_t ahead = pos - at;
             uint64_t seen = ahead < 0 ? 0 : (ahead > 62 ? ~0ull : (2ull << ahead) - 1);
-            seen = (seen & ok_now) >> (8 * (here >> 5));
+            seen = (seen & ok_now) >> (8 * half);
             const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
             for (int c = 0; c < 2; ++c)
@@ -265,26 +290,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                 w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
         }
         // column d of 16 keys, 8 of them a lane: two transposed reads
-        const int g = here >> 4, l16 = here & 15;  // 16 lanes: dims 16 (g & 1), keys 8 (g >> 1)
-        const int vrow0 = 8 * (g >> 1) + (l16 >> 2);
-        const int vcol = 2 * (g & 1) + ((l16 & 3) >> 1), vin = (l16 & 1) * 8;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             v4u vt[D / 32];
-            const int r0 = 16 * b + vrow0;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                const int col = 4 * i + vcol;
-                const v2u lo = read_transposed(s_v[buf] + r0 * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
-                const v2u hi =
-                    read_transposed(s_v[buf] + (r0 + 4) * kRow + ((col ^ turn_v<D>(vrow0)) * 16) + vin);
-                vt[i] = join(lo, hi);
-            }
+            for (int i = 0; i < D / 32; ++i)
+                vt[i] = join(read_transposed(vm + v_read[i] + 16 * b * kRow),
+                             read_transposed(vm + v_read[i] + (16 * b + 4) * kRow));
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
                 o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b]), o[i]);
         }
         __syncthreads();
+    };
+    for (int t = 0; t < steps; t += 2) {
+        turn(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < steps) turn(std::integral_constant<int, 1>{}, t + 1);
     }
 
     if (s_endless) {
