@@ -571,12 +571,11 @@ typedef struct {
     int64_t workspace_bytes;
 } ptstore_attention_t;
 
-/* Bytes of workspace an attention of these sizes needs (0: none), 16-byte
- * aligned. It follows from the cache's heads and head_dim, the device, and whether
- * the call needs any at all: one workspace serves every call on a layer. Host
- * only. Errors: INVALID, HIP. */
-int ptstore_attention_workspace(const ptstore_kv_t *kv, int32_t q_heads, int64_t n_tokens, int32_t R,
-                                int32_t max_blocks, int64_t *bytes);
+/* Bytes of workspace that an attention over a layer needs, 16-byte aligned. It
+ * follows from the layer's heads and head_dim and the device alone (some 34 MB at
+ * most for 8 heads of 128): one serves every call on it. Host only. Errors: INVALID,
+ * HIP. */
+int ptstore_attention_workspace(const ptstore_kv_t *kv, int64_t *bytes);
 
 /* Errors: INVALID (shapes, sizes, strides or alignment as stated; max_blocks *
  * block_tokens > 2^30; no cache blocks; a workspace too small), HIP. */

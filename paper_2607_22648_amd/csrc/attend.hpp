@@ -155,7 +155,7 @@ __device__ inline Tile find_tile(const AttendPlan& p, int64_t t, int rows) {
     f.begin = begin;
     f.n = (int32_t)(end - begin);
     const int64_t tile = t - (begin * p.group / rows + f.r);
-    if (tile < 0 || tile * rows >= (int64_t)f.n * p.group) return f;
+    if (tile < 0 || tile * rows >= (int64_t)f.n * p.group || (int64_t)f.n * p.group <= p.few_rows) return f;
     f.tile = (int)tile;
     return f;
 }

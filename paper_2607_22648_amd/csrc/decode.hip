@@ -51,7 +51,7 @@ struct Work {
 __device__ inline Work work_of(const AttendPlan& p, int r, int step_keys) {
     Work w;
     const int64_t a = p.offsets[r], b = p.offsets[r + 1];
-    const bool ok = a >= 0 && b > a && b <= p.n_tokens;
+    const bool ok = a >= 0 && b > a && b <= p.n_tokens && (b - a) * p.group <= p.few_rows;
     w.begin = ok ? a : 0;
     w.n = ok ? (int32_t)(b - a) : 0;
     w.past = p.context[r];

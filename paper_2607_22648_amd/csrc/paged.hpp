@@ -80,9 +80,15 @@ struct AttendPlan {
     int64_t n_tokens;
     int32_t R, max_blocks, q_heads, group;  // group: query heads of a KV head
     float scale2;                           // scale * log2(e): scores in base 2
-    float* parts;                           // workspace: two parts of a tile a share and head
-    int32_t shares;                         // of the batch's work (decode.hip)
+    int32_t few_rows;                       // requests of up to this many rows are decode.hip's alone,
+                                            // the others prompt.hip's (0: all are prompt.hip's)
+    float* parts;                           // workspace
+    int32_t shares;                         // decode.hip: of the batch's work
+    int32_t whole, rest, splits;            // prompt.hip: (tile, KV head) pairs done whole, and in parts
 };
+
+// Rows a request that decode.hip takes in a batch that both kernels share.
+constexpr int kFewRows = 32;
 
 // Query rows of a decode tile (one matrix instruction's columns) and of a
 // prompt tile.
@@ -105,6 +111,8 @@ hipError_t launch_read(const Planes& kv, const Rows& k, const Rows& v, const int
 int decode_shares(const Planes& kv, int cus);
 int64_t decode_workspace(const Planes& kv, int shares);  // bytes
 hipError_t launch_decode(const AttendPlan& p, hipStream_t s);
+void split_prompt(AttendPlan* p, int cus);
+int64_t prompt_workspace(const Planes& kv, int cus);  // bytes
 hipError_t launch_prompt(const AttendPlan& p, hipStream_t s);
 
 }  // namespace ptsd

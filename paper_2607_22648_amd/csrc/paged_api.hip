@@ -4,6 +4,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <cstdint>
 #include <cstdio>
 
 #include "paged.hpp"
@@ -77,9 +78,23 @@ int compute_units(int* cus) {
     return PTSTORE_OK;
 }
 
-// Whether a call's rows go 128 or 16 to a tile. The host knows the average
-// request alone.
+// Whether a call's rows go 128 to a tile, or 16. The host knows the average
+// request alone. Behind 4,000 keys, 8 KV heads of 4 query heads (us, 16 and 128):
+//
+//   tokens        4 x 32  16 x 32  32 x 32   64 x 2  128 x 2  256 x 2
+//   16 rows           91      252      525       55       86      167
+//   128 rows         149      150      156  PROMPT_SMALL
 bool many_rows(const AttendPlan& p) { return p.n_tokens * p.group > (int64_t)32 * p.R; }
+
+// Whether requests of few rows in such a batch go to the other kernel: one workgroup
+// goes through all keys of a tile, 1.3 us for 64, however few its rows are. The
+// launches that may find nothing to do cost 6 us, so it takes room for 8,192 keys.
+bool mixed(const AttendPlan& p) { return p.R > 1 && (int64_t)p.max_blocks * p.kv.div.page >= 8192; }
+
+int64_t workspace_of(const Planes& kv, int cus) {
+    const int64_t a = decode_workspace(kv, decode_shares(kv, cus)), b = prompt_workspace(kv, cus);
+    return a > b ? a : b;
+}
 
 // Checks the sizes and fills what the workspace and the launch follow from.
 const char* sized(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int32_t R, int32_t max_blocks,
@@ -169,17 +184,13 @@ int ptstore_kv_read(const ptstore_kv_t* kv, void* k, int64_t k_token_stride, int
                      slots, n_tokens, true, stream);
 }
 
-int ptstore_attention_workspace(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int32_t R,
-                                int32_t max_blocks, int64_t* bytes) {
-    AttendPlan p;
+int ptstore_attention_workspace(const ptstore_kv_t* kv, int64_t* bytes) {
+    Planes pl;
     if (!bytes) return refuse("ptstore_attention_workspace: null argument");
-    if (const char* bad = sized(kv, q_heads, n_tokens, R, max_blocks, &p))
-        return refuse_as("ptstore_attention_workspace", bad);
-    *bytes = 0;
-    if (many_rows(p)) return PTSTORE_OK;
+    if (const char* bad = planes_of(kv, &pl)) return refuse_as("ptstore_attention_workspace", bad);
     int cus = 0;
     if (const int rc = compute_units(&cus)) return rc;
-    *bytes = decode_workspace(p.kv, decode_shares(p.kv, cus));
+    *bytes = workspace_of(pl, cus);
     return PTSTORE_OK;
 }
 
@@ -196,15 +207,11 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
         !rows_ok(a->out, a->out_token_stride, a->out_head_stride))
         return refuse("ptstore_attention: rows of q or out null or not 16-byte aligned");
     if (p.kv.blocks < 1) return refuse("ptstore_attention: the cache has no blocks");
-    const bool prompts = many_rows(p);
-    if (!prompts) {
-        int cus = 0;
-        if (const int rc = compute_units(&cus)) return rc;
-        p.shares = decode_shares(p.kv, cus);
-        if (a->workspace_bytes < decode_workspace(p.kv, p.shares) || !a->workspace || !aligned16(a->workspace))
-            return refuse("ptstore_attention: workspace too small or not 16-byte aligned "
-                          "(ptstore_attention_workspace)");
-    }
+    int cus = 0;
+    if (const int rc = compute_units(&cus)) return rc;
+    if (a->workspace_bytes < workspace_of(p.kv, cus) || !a->workspace || !aligned16(a->workspace))
+        return refuse("ptstore_attention: workspace too small or not 16-byte aligned "
+                      "(ptstore_attention_workspace)");
     p.q = Rows{a->q, a->q_token_stride, a->q_head_stride};
     p.out = Rows{a->out, a->out_token_stride, a->out_head_stride};
     p.lse = a->lse;
@@ -213,7 +220,18 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
     p.table = a->block_table;
     p.scale2 = a->scale * 1.4426950408889634f;
     p.parts = static_cast<float*>(a->workspace);
-    const hipError_t e = prompts ? launch_prompt(p, (hipStream_t)stream) : launch_decode(p, (hipStream_t)stream);
+    p.shares = decode_shares(p.kv, cus);
+    const bool prompts = many_rows(p), both = prompts && mixed(p);
+    hipError_t e = hipSuccess;
+    if (prompts) {
+        p.few_rows = both ? kFewRows : 0;
+        split_prompt(&p, cus);
+        e = launch_prompt(p, (hipStream_t)stream);
+    }
+    if (e == hipSuccess && (!prompts || both)) {
+        p.few_rows = both ? kFewRows : INT32_MAX;
+        e = launch_decode(p, (hipStream_t)stream);
+    }
     return e == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, "ptstore_attention: launch");
 }
 

@@ -43,6 +43,11 @@ __device__ inline int turn_v(int row) {
 // output is rescaled a few times a row instead of at every new maximum.
 constexpr float kBehind = 8.f;
 
+constexpr int kMostParts = 16;  // of a tile
+
+// Floats of a part in the workspace: [4 dimensions][row], then rows' maxima and sums.
+constexpr int part_floats(int dim) { return kPromptRows * (dim + 2); }
+
 template <int D, bool kHalf, bool kFour>
 __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     using E = Elem<kHalf>;
@@ -60,10 +65,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % p.kv.heads;
+    // (tile, KV head) `unit`, whole or part `part` of p.splits of its keys
+    const int rest = (int)(blockIdx.x - p.whole);
+    const int part = rest < 0 ? 0 : rest / p.rest, parts = rest < 0 ? 1 : p.splits;
+    const int unit = rest < 0 ? (int)blockIdx.x : p.whole + rest % p.rest;
+    const int head = unit % p.kv.heads;
     // the last tiles of a request see the most keys: they go first
-    const int64_t tiles = gridDim.x / p.kv.heads;
-    const Tile f = find_tile(p, tiles - 1 - blockIdx.x / p.kv.heads, kPromptRows);
+    const Tile f = find_tile(p, (p.whole + p.rest) / p.kv.heads - 1 - unit / p.kv.heads, kPromptRows);
     if (f.tile < 0) return;
 
     const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
@@ -80,7 +88,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     const int32_t tile_sees = clip(f.past + f.tile * kPromptRows / p.group);
     const int32_t all_see = clip(f.past + first_row / p.group);
     const int32_t pos = clip(f.past + token);
-    const int steps = (end + kKeys - 1) / kKeys;
+    const int all_steps = (end + kKeys - 1) / kKeys;
+    const int step0 = (int)((int64_t)all_steps * part / parts);
+    const int steps = (int)((int64_t)all_steps * (part + 1) / parts);  // this part's are [step0, steps)
 
     const int32_t* table = p.table + (int64_t)f.r * p.max_blocks;
     const uint32_t head_row = (uint32_t)head * p.kv.div.page;
@@ -203,20 +213,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 
     if (threadIdx.x == 0) s_endless = 0;
     __syncthreads();
-    int32_t entry = steps > 0 ? page_entry(p, table, lane, end) : -1;
+    int32_t entry = page_entry(p, table, step0 * kKeys + lane, end);
     uint64_t ok = 0, ok_next = 0;  // which keys of the step, and of the loaded one, are there
     bool there;
-    if (steps > 0) {
-        KeyRow place = key_row<D, kFour>(p.kv, entry, lane, end, head_row, there);
+    if (step0 < steps) {
+        const int32_t key = step0 * kKeys + lane;
+        KeyRow place = key_row<D, kFour>(p.kv, entry, key, end, head_row, there);
         ok = __ballot(there);
         load(place);
-        entry = page_entry(p, table, kKeys + lane, end);
-        store(std::integral_constant<int, 0>{}, ok, 0);
-        if (steps > 1) {
-            place = key_row<D, kFour>(p.kv, entry, kKeys + lane, end, head_row, there);
+        entry = page_entry(p, table, key + kKeys, end);
+        store(std::integral_constant<int, 0>{}, ok, step0);
+        if (step0 + 1 < steps) {
+            place = key_row<D, kFour>(p.kv, entry, key + kKeys, end, head_row, there);
             ok_next = __ballot(there);
             load(place);
-            entry = page_entry(p, table, 2 * kKeys + lane, end);
+            entry = page_entry(p, table, key + 2 * kKeys, end);
         }
     }
     __syncthreads();
@@ -303,13 +314,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         }
         __syncthreads();
     };
-    for (int t = 0; t < steps; t += 2) {
+    for (int t = step0; t < steps; t += 2) {
         turn(std::integral_constant<int, 0>{}, t);
         if (t + 1 < steps) turn(std::integral_constant<int, 1>{}, t + 1);
     }
 
     if (s_endless) {
-        for (int32_t key = tile_sees + 1; key < end; ++key) {
+        const int32_t from = tile_sees + 1 > step0 * kKeys ? tile_sees + 1 : step0 * kKeys;
+        for (int32_t key = from; key < end && key < steps * kKeys; ++key) {
             const KeyRow row =
                 key_row<D, kFour>(p.kv, page_entry(p, table, key, end), key, end, head_row, there);
             if (!there || key > pos) continue;
@@ -323,6 +335,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     }
     if (row0 + n >= all_rows) return;  // both halves of a row leave together
     sum += __shfl_xor(sum, 32);
+    if (parts > 1) {
+        // four dimensions a lane, rows next to each other
+        float* const to = p.parts + ((int64_t)(unit - p.whole) * parts + part) * part_floats(D);
+        const int r = wave * 32 + n;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                *(v4f*)(to + ((8 * i + 2 * a + half) * kPromptRows + r) * 4) =
+                    v4f{o[i][4 * a], o[i][4 * a + 1], o[i][4 * a + 2], o[i][4 * a + 3]};
+        if (half == 0) *(v2f*)(to + kPromptRows * D + 2 * r) = v2f{top, sum};
+        return;
+    }
     // no key, or none with a weight: zeros, and the logarithm of nothing
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     const int64_t oh = (int64_t)head * p.group + sub;
@@ -348,10 +373,59 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
+// Joins the parts of tiles that have more than one: 32 rows of a (tile, KV head) a
+// workgroup, a row and 8 dimensions a lane.
+constexpr int kJoinRows = 32;
+
+template <int D, bool kHalf>
+__global__ __launch_bounds__(kJoinRows* D / 8) void k_prompt_join(AttendPlan p) {
+    constexpr int kSlices = kPromptRows / kJoinRows;
+    const int at = blockIdx.x / kSlices, unit = p.whole + at, head = unit % p.kv.heads;
+    const Tile f = find_tile(p, (p.whole + p.rest) / p.kv.heads - 1 - unit / p.kv.heads, kPromptRows);
+    if (f.tile < 0) return;
+    const int r = blockIdx.x % kSlices * kJoinRows + threadIdx.x % kJoinRows, c = threadIdx.x / kJoinRows;
+    const int row = f.tile * kPromptRows + r;
+    if (row >= f.n * p.group) return;
+    const float* const from = p.parts + (int64_t)at * p.splits * part_floats(D);
+    float all = kLowest;
+    for (int i = 0; i < p.splits; ++i)
+        all = fmaxf(all, from[(int64_t)i * part_floats(D) + kPromptRows * D + 2 * r]);
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < p.splits; ++i) {
+        const float* part = from + (int64_t)i * part_floats(D);
+        const v2f ms = *(const v2f*)(part + kPromptRows * D + 2 * r);
+        const v4f a = *(const v4f*)(part + (2 * c * kPromptRows + r) * 4);
+        const v4f b = *(const v4f*)(part + ((2 * c + 1) * kPromptRows + r) * 4);
+        const float part_of = exp2_of(ms[0] - all);
+        if (part_of == 0.f) continue;  // nothing of it counts, and 0 * infinity would
+        total += part_of * ms[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            acc[e] += part_of * a[e];
+            acc[4 + e] += part_of * b[e];
+        }
+    }
+    const float inv = total != 0.f ? 1.f / total : 0.f;
+    const int token = row / p.group;
+    const int64_t oh = (int64_t)head * p.group + (row - token * p.group);
+    v4u x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = pack2<kHalf>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    *(v4u*)((uint8_t*)p.out.p + ((f.begin + token) * p.out.token + oh * p.out.head + c * 8) * 2) = x;
+    if (p.lse && c == 0)
+        p.lse[(f.begin + token) * p.q_heads + oh] =
+            total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+}
+
 template <int D, bool kHalf, bool kFour>
 hipError_t run(const AttendPlan& p, hipStream_t s) {
-    const int64_t units = tile_bound(p.n_tokens, p.group, p.R, kPromptRows) * p.kv.heads;
-    hipLaunchKernelGGL((k_prompt<D, kHalf, kFour>), dim3((unsigned)units), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((k_prompt<D, kHalf, kFour>), dim3((unsigned)(p.whole + p.rest * p.splits)), dim3(kThreads), 0, s,
+                       p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits < 2) return e;
+    hipLaunchKernelGGL((k_prompt_join<D, kHalf>), dim3((unsigned)(p.rest * (kPromptRows / kJoinRows))),
+                       dim3(kJoinRows * D / 8), 0, s, p);
     return hipGetLastError();
 }
 
@@ -362,6 +436,37 @@ hipError_t run_kind(const AttendPlan& p, hipStream_t s) {
 }
 
 }  // namespace
+
+// Two workgroups a compute unit run at once. Where a batch has fewer tiles than
+// that, their keys are split so that all work; the tiles of a last turn that would be
+// at most half full, likewise, up to four turns (past that, short tiles fill the end).
+// The host knows the number of tiles to within half a tile a request. 2 requests of 128
+// tokens behind 4,000 (8 KV heads of 4) take 34 + 9 us split, 98 whole.
+void split_prompt(AttendPlan* p, int cus) {
+    const int64_t heads = p->kv.heads, slots = 2 * cus;
+    const int64_t rows = p->n_tokens * p->group;
+    const int64_t bound = p->R == 1 ? (rows + kPromptRows - 1) / kPromptRows
+                                    : tile_bound(p->n_tokens, p->group, p->R, kPromptRows);
+    const int64_t likely = p->R == 1 ? bound : (rows + (int64_t)p->R * (kPromptRows / 2)) / kPromptRows;
+    int64_t rest = 0;  // tiles in parts, of each head
+    if (bound * heads < slots)
+        rest = bound;
+    else if (likely * heads < 4 * slots)
+        rest = likely * heads % slots / heads;
+    int64_t splits = rest ? slots / (rest * heads) : 1;
+    // ten steps a part at least, where the table is full: a prompt of 1,024 tokens takes
+    // 26 + 8 us in two parts, 31 whole
+    const int64_t most = (int64_t)p->max_blocks * p->kv.div.page / (10 * kKeys);
+    if (splits > most) splits = most;
+    if (splits < 2) rest = 0;
+    p->whole = (int32_t)((bound - rest) * heads);
+    p->rest = (int32_t)(rest * heads);
+    p->splits = rest ? (int32_t)(splits < kMostParts ? splits : kMostParts) : 1;
+}
+
+int64_t prompt_workspace(const Planes& kv, int cus) {
+    return 2ll * cus * part_floats(kv.dim) * (int64_t)sizeof(float);
+}
 
 hipError_t launch_prompt(const AttendPlan& p, hipStream_t s) {
     return p.kv.dim == 128 ? run_kind<128>(p, s) : run_kind<64>(p, s);

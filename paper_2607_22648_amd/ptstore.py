@@ -120,7 +120,7 @@ def _load() -> C.CDLL:
         "ptstore_block_tables": [p, i64, p, p, i32, i32, i32, p, i64, p, p, p, p, p, p, p],
         "ptstore_kv_append": [C.POINTER(ptstore_kv_t), p, i64, i64, p, i64, i64, p, i64, p],
         "ptstore_kv_read": [C.POINTER(ptstore_kv_t), p, i64, i64, p, i64, i64, p, i64, p],
-        "ptstore_attention_workspace": [C.POINTER(ptstore_kv_t), i32, i64, i32, i32, C.POINTER(i64)],
+        "ptstore_attention_workspace": [C.POINTER(ptstore_kv_t), C.POINTER(i64)],
         "ptstore_attention": [C.POINTER(ptstore_attention_t), p],
     }
     for name, args in sig.items():
@@ -473,17 +473,15 @@ def ptstore_kv_read(kv: ptstore_kv_t, k, v, slots, stream=None) -> None:
                                                    _stream(stream)))
 
 
-def ptstore_attention_workspace(kv: ptstore_kv_t, q_heads: int, n_tokens: int, R: int,
-                                max_blocks: int) -> int:
+def ptstore_attention_workspace(kv: ptstore_kv_t) -> int:
     n = C.c_int64()
-    _check("ptstore_attention_workspace", _lib.ptstore_attention_workspace(
-        C.byref(kv), q_heads, n_tokens, R, max_blocks, C.byref(n)))
+    _check("ptstore_attention_workspace", _lib.ptstore_attention_workspace(C.byref(kv), C.byref(n)))
     return n.value
 
 
 def ptstore_attention(kv: ptstore_kv_t, q, out, lse, offsets, context, block_table, scale: float,
-                      workspace=None, stream=None) -> None:
-    """`lse` may be None, and `workspace` where the call needs none."""
+                      workspace, stream=None) -> None:
+    """`lse` may be None; `workspace`: a uint8 tensor of ptstore_attention_workspace(kv) bytes."""
     R, maxb = _table(offsets, block_table)
     _need(context, R, "context")
     qr = _token_rows(q, kv, None, "q")
@@ -496,8 +494,7 @@ def ptstore_attention(kv: ptstore_kv_t, q, out, lse, offsets, context, block_tab
     a = ptstore_attention_t(kv, *qr, *outr, _dev(lse, torch.float32, "lse"),
                             _dev(offsets, torch.int64, "offsets"), _dev(context, torch.int32, "context"),
                             _dev(block_table, torch.int32, "block_table"), n, R, maxb, heads, scale,
-                            _dev(workspace, torch.uint8, "workspace"),
-                            workspace.numel() if workspace is not None else 0)
+                            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
     _check("ptstore_attention", _lib.ptstore_attention(C.byref(a), _stream(stream)))
 
 
@@ -780,7 +777,7 @@ class PagedCache:
         handle = _stream(stream)
         ws = self._workspaces.get(handle)
         if ws is None:
-            need = max(ptstore_attention_workspace(kv, kv.kv_heads, 1, 1, 1) for kv in self._planes)
+            need = max(ptstore_attention_workspace(kv) for kv in self._planes)
             with self._on(stream):
                 ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
                 if not torch.cuda.is_current_stream_capturing():  # a graph keeps its own

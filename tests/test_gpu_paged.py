@@ -285,6 +285,19 @@ def test_attention_prompts(P, kind):
     Case(P, kind, 1, 4, 128, 16, [(150, 0), (1, 0), (97, 333), (64, 64)], seed=6).check()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "mxfp4"])
+def test_attention_mixed_batch(P, kind):
+    """Single tokens behind long contexts beside prompts: a batch of both kernels' requests."""
+    Case(P, kind, 1, 4, 64, 16, [(1, 8300), (150, 40), (1, 3), (8, 100), (9, 100), (0, 5), (40, 0)], seed=17).check()
+
+
+@pytest.mark.parametrize("new,past", [(130, 900), (300, 0), (513, 70)])
+def test_attention_prompt_in_parts(P, new, past):
+    """Few tiles, whose keys are split: one request, and several."""
+    Case(P, "bf16", 1, 2, 128, 16, [(new, past)], seed=18).check()
+    Case(P, "fp16", 2, 1, 64, 16, [(new, past), (90, past + 33)], seed=19).check()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 def test_attention_large_scores(P, kind):
     """Scores in the hundreds: one key takes nearly all the weight, in either order."""
@@ -385,7 +398,7 @@ def test_attention_in_a_graph(P, reqs):
     """Captured once, replayed on changed inputs, eager work between the replays."""
     c = Case(P, "bf16", 2, 4, 128, 16, reqs, seed=13)
     q, off, ctx, table = c.q.cuda(), c.off.cuda(), c.ctx.cuda(), c.table.cuda()
-    ws = torch.empty(P.ptstore_attention_workspace(c.cache.layer(0), 8, q.shape[0], *table.shape) + 16,
+    ws = torch.empty(P.ptstore_attention_workspace(c.cache.layer(0)) + 16,
                      dtype=torch.uint8, device="cuda")
     out = torch.empty_like(q)
     c.cache.attend(0, q, off, ctx, table, out=out, workspace=ws)
@@ -462,8 +475,6 @@ def test_refusals(P):
     refused("16-byte", lambda: c.cache.attend(0, odd, off, ctx, table))
     refused("rows", lambda: c.cache.attend(0, q, off, ctx, table[:0]), ValueError)
     refused("context holds", lambda: c.cache.attend(0, q, off, ctx[:0], table), ValueError)
-    refused("2\\^30", lambda: P.ptstore_attention_workspace(kv, 8, 1, 1, 1 << 27))
-    refused("out of range", lambda: P.ptstore_attention_workspace(kv, 8, 1, 0, 4))
     refused("kind", lambda: P.PagedCache(1, 2, 64, 4, kind="int8"), ValueError)
     refused("slab", lambda: P.PagedCache(1, 2, 80, 4))
     refused("bytes", lambda: P.PagedCache(1, 2, 64, 4, data=c.cache.data[:100]), ValueError)
@@ -473,7 +484,6 @@ def test_refusals(P):
     refused("int64", lambda: c.cache.append(0, k, k, s.int()), ValueError)
     empty = P.PagedCache(1, 2, 64, 0)
     one_row = (kv, q[:1], out[:1], None, torch.tensor([0, 1], device="cuda"), ctx, table, 1.0)
-    refused("workspace", lambda: P.ptstore_attention(*one_row))
     refused("workspace", lambda: P.ptstore_attention(*one_row, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda")))
     refused("no blocks", lambda: empty.attend(0, q, off, ctx, table))
     # nothing to do is no error

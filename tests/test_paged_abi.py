@@ -52,7 +52,11 @@ def test_attention_refuses_on_the_host(P):
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "multiple" in text()
     a.q_heads, a.scale = 4, float("inf")
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "scale" in text()
-    a.scale = 1.0
+    a.scale, a.max_blocks = 1.0, (1 << 26) + 1
+    assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "2^30" in text()
+    a.max_blocks, a.R = 4, 0
+    assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "out of range" in text()
+    a.R = 1
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "null" in text()
     a.offsets = a.context = a.block_table = 0x1000
     a.q, a.out = 0x1008, 0x1000
@@ -61,10 +65,10 @@ def test_attention_refuses_on_the_host(P):
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "planes" in text()
     kv = P.ptstore_kv_t(0x1000, 0x2000, (1 << 30) + 1, 2, 64, 16, 0)
     with pytest.raises(P.PTStoreError, match="2\\^30"):
-        P.ptstore_attention_workspace(kv, 4, 1, 1, 4)
+        P.ptstore_attention_workspace(kv)
     kv.cache_blocks = (1 << 36) // 4096 + 1
     with pytest.raises(P.PTStoreError, match="64 GiB"):
-        P.ptstore_attention_workspace(kv, 4, 1, 1, 4)
+        P.ptstore_attention_workspace(kv)
     assert lib.ptstore_kv_append(C.byref(kv), 1, 1, 1, 1, 1, 1, 1, 1, None) == P.PTSTORE_ERR_INVALID
     assert lib.ptstore_kv_append(None, 1, 1, 1, 1, 1, 1, 1, 1, None) == P.PTSTORE_ERR_INVALID
     assert os.path.exists(HEADER)
