@@ -503,8 +503,8 @@ int ptstore_kv_slab_bytes(int32_t kind, int32_t kv_heads, int32_t head_dim, int3
  * beyond max_blocks or its entry is negative. A held block is reused first: the
  * entry of a position below held[r] * block_tokens is read from block_table.
  * held_out must not be held, nor next first (outputs may not overlap inputs).
- * Errors: INVALID (sizes out of range, R * max_blocks > 2^29, tokens without
- * requests, a NULL pointer), HIP.
+ * Errors: INVALID (sizes out of range, R * max_blocks > 2^29, max_blocks *
+ * block_tokens > 2^30, tokens without requests, a NULL pointer), HIP.
  */
 int ptstore_block_tables(const int64_t *offsets, int64_t n_tokens, const int32_t *context,
                          const int32_t *held, int32_t R, int32_t max_blocks, int32_t block_tokens,

@@ -141,7 +141,7 @@ int ptstore_block_tables(const int64_t* offsets, int64_t n_tokens, const int32_t
                          int64_t n_free, const int64_t* first, int32_t* block_table, int64_t* slots,
                          int32_t* positions, int32_t* held_out, int64_t* next, void* stream) {
     if (R < 0 || max_blocks < 1 || (int64_t)R * max_blocks > kMaxEntries || block_tokens < 1 ||
-        block_tokens > 64 || n_tokens < 0 || n_tokens >= (1ll << 40) || n_free < 0 || (R == 0 && n_tokens > 0))
+        block_tokens > 64 || (int64_t)max_blocks * block_tokens > kMaxKeys || n_tokens < 0 || n_tokens >= (1ll << 40) || n_free < 0 || (R == 0 && n_tokens > 0))
         return refuse("ptstore_block_tables: a size is out of range");
     if (!next || (R > 0 && (!offsets || !context || !block_table || !held_out)) || (n_tokens > 0 && !slots) ||
         (n_free > 0 && !free_blocks))

@@ -18,12 +18,15 @@ namespace ptsd {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kChunk = 2048;                 // requests a workgroup scans
-constexpr int kPer = kChunk / kThreads;      // consecutive ones a thread
-constexpr int kTokensPer = 4;                // consecutive tokens a thread's step
+constexpr int kChunk = 1024;             // requests a workgroup scans
+constexpr int kPer = kChunk / kThreads;  // consecutive ones a thread
+constexpr int kTokensPer = 4;            // consecutive tokens a thread's step
+
+typedef long long v2l __attribute__((ext_vector_type(2)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 
 struct Request {
-    int64_t begin, n;  // tokens of the batch
+    int64_t begin, end;  // tokens of the batch
     int64_t past;
     int32_t held, want;
 };
@@ -32,17 +35,16 @@ __device__ Request request(const TablesPlan& p, int r) {
     Request q;
     const int64_t a = p.offsets[r], b = p.offsets[r + 1];
     const bool ok = a >= 0 && b >= a && b <= p.n_tokens;
-    q.begin = ok ? a : 0;
-    q.n = ok ? b - a : 0;
+    q.begin = a;
+    q.end = ok ? b : a;  // a malformed request has no tokens
     q.past = p.context[r];
     int held = p.held ? p.held[r] : 0;
     held = held < 0 ? 0 : (held > p.max_blocks ? p.max_blocks : held);
     q.held = held;
-    int64_t tokens = q.past + q.n;
-    if (tokens < 0) tokens = 0;
-    const int64_t room = (int64_t)p.max_blocks * p.div.page;
-    if (tokens > room) tokens = room;
-    const int32_t need = (int32_t)((tokens + p.div.page - 1) / p.div.page);
+    const int64_t room = (int64_t)p.max_blocks * p.div.page;  // at most 2^30
+    int64_t tokens = q.past + (q.end - q.begin);
+    tokens = tokens < 0 ? 0 : (tokens > room ? room : tokens);
+    const int32_t need = (int32_t)div_page((uint32_t)tokens + p.div.page - 1, p.div);
     q.want = need > held ? need - held : 0;
     return q;
 }
@@ -59,9 +61,9 @@ __device__ int32_t sum_all(int32_t x, int32_t* part) {
 }
 
 __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
-    __shared__ int64_t s_begin[kChunk];   // the chunk's requests: first token
-    __shared__ int32_t s_want[kChunk + 1];  // blocks wanted before each, within the chunk
-    __shared__ int32_t s_held[kChunk];
+    // the chunk's requests: tokens, first token's position, blocks held, wanted before
+    __shared__ int64_t s_begin[kChunk], s_end[kChunk];
+    __shared__ int32_t s_past[kChunk], s_held[kChunk], s_want[kChunk + 1];
     __shared__ int32_t s_part[kThreads / 64];
     const int tid = threadIdx.x;
     const int chunk = blockIdx.x / parts, part = blockIdx.x % parts;
@@ -81,9 +83,10 @@ __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
         if (l < nr) {
             const Request q = request(p, r0 + l);
             want[i] = q.want;
+            s_begin[l] = q.begin;
+            s_end[l] = q.end;
+            s_past[l] = (int32_t)q.past;
             s_held[l] = q.held;
-            // a malformed request has no tokens: one past every token
-            s_begin[l] = q.n ? q.begin : p.offsets[r0 + l];
         }
         mine += want[i];
     }
@@ -145,7 +148,12 @@ __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
     int64_t t1 = r0 + nr < p.R ? p.offsets[r0 + nr] : p.n_tokens;
     if (t0 < 0) t0 = 0;
     if (t1 > p.n_tokens) t1 = p.n_tokens;
-    for (int64_t t = t0 + ((int64_t)part * kThreads + tid) * kTokensPer; t < t1; t += step * kTokensPer) {
+    const int64_t room = (int64_t)p.max_blocks * p.div.page;
+    // groups of four tokens by their number, so that they are written as one where the
+    // arrays are aligned
+    const bool whole = ((reinterpret_cast<uintptr_t>(p.slots) | reinterpret_cast<uintptr_t>(p.positions)) & 15) == 0;
+    for (int64_t t = t0 / kTokensPer * kTokensPer + ((int64_t)part * kThreads + tid) * kTokensPer; t < t1;
+         t += step * kTokensPer) {
         int lo = 0, hi = nr - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -154,31 +162,39 @@ __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
             else
                 hi = mid - 1;
         }
+        int64_t slot[kTokensPer];
+        int32_t pos[kTokensPer];
 #pragma unroll
         for (int i = 0; i < kTokensPer; ++i) {
             const int64_t ti = t + i;
-            if (ti >= t1) break;
+            slot[i] = -1;
+            pos[i] = 0;
             while (lo + 1 < nr && s_begin[lo + 1] <= ti) ++lo;
-            const Request q = request(p, r0 + lo);
-            int64_t slot = -1;
-            int32_t pos = 0;
-            if (ti >= q.begin && ti < q.begin + q.n) {
-                const int64_t at_pos = q.past + (ti - q.begin);
-                pos = (int32_t)at_pos;
-                if (at_pos >= 0 && at_pos < (int64_t)p.max_blocks * p.div.page) {
-                    const int32_t b = (int32_t)(at_pos / p.div.page);
-                    int64_t entry;
-                    if (b < q.held) {
-                        entry = p.table[(int64_t)(r0 + lo) * p.max_blocks + b];
-                    } else {
-                        const int64_t at_free = base + s_want[lo] + (b - q.held);
-                        entry = at_free < p.n_free ? p.free_blocks[at_free] : -1;
-                    }
-                    if (entry >= 0) slot = entry * p.div.page + (at_pos - (int64_t)b * p.div.page);
-                }
+            if (nr == 0 || ti < s_begin[lo] || ti >= s_end[lo]) continue;
+            const int64_t at_pos = s_past[lo] + (ti - s_begin[lo]);
+            pos[i] = (int32_t)at_pos;
+            if (at_pos < 0 || at_pos >= room) continue;
+            const uint32_t b = div_page((uint32_t)at_pos, p.div);
+            int64_t entry;
+            if ((int32_t)b < s_held[lo]) {
+                entry = p.table[(int64_t)(r0 + lo) * p.max_blocks + b];
+            } else {
+                const int64_t at_free = base + s_want[lo] + ((int32_t)b - s_held[lo]);
+                entry = at_free < p.n_free ? p.free_blocks[at_free] : -1;
             }
-            p.slots[ti] = slot;
-            if (p.positions) p.positions[ti] = pos;
+            if (entry >= 0) slot[i] = entry * p.div.page + ((uint32_t)at_pos - b * p.div.page);
+        }
+        if (whole && t >= t0 && t + kTokensPer <= t1) {
+            *(v2l*)(p.slots + t) = v2l{slot[0], slot[1]};
+            *(v2l*)(p.slots + t + 2) = v2l{slot[2], slot[3]};
+            if (p.positions) *(v4i*)(p.positions + t) = v4i{pos[0], pos[1], pos[2], pos[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTokensPer; ++i) {
+                if (t + i < t0 || t + i >= t1) continue;
+                p.slots[t + i] = slot[i];
+                if (p.positions) p.positions[t + i] = pos[i];
+            }
         }
     }
 }

@@ -156,6 +156,15 @@ def _dev(t: Optional[torch.Tensor], dtype, name: str) -> int:
     return t.data_ptr()
 
 
+def _arg(t: torch.Tensor, dtype, n: int, name: str) -> int:
+    """The address of a required array of at least n elements: _dev and _need in one, since a short
+    call's checks are a part of its time."""
+    if t is not None and t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.numel() >= n:
+        return t.data_ptr()
+    _need(t, n, name)
+    return _dev(t, dtype, name)
+
+
 def _need(t: Optional[torch.Tensor], n: int, name: str) -> None:
     """The device arrays a call reads or writes are sized by R and max_blocks;
     the library cannot see an allocation's size, so it is checked here."""
@@ -170,7 +179,8 @@ def _need(t: Optional[torch.Tensor], n: int, name: str) -> None:
 def _rows(ids: torch.Tensor, name: str = "ids") -> Tuple[int, int]:
     if ids.dim() != 2:
         raise ValueError(f"{name} must be [R, max_blocks], got shape {tuple(ids.shape)}")
-    return int(ids.shape[0]), int(ids.shape[1])
+    R, max_blocks = ids.shape
+    return R, max_blocks
 
 
 def _requests(offsets: torch.Tensor) -> int:
@@ -181,7 +191,7 @@ def _requests(offsets: torch.Tensor) -> int:
 
 def _table(offsets: torch.Tensor, block_table: torch.Tensor) -> Tuple[int, int]:
     R, maxb = _rows(block_table, "block_table")
-    if _requests(offsets) != R:
+    if offsets.numel() != R + 1 or offsets.dim() != 1:
         raise ValueError(f"block_table has {R} rows, the batch {_requests(offsets)} requests")
     return R, maxb
 
@@ -416,24 +426,17 @@ def ptstore_block_tables(offsets, context, held, block_tokens, free_blocks, firs
                          positions, held_out, next_free, stream=None) -> None:
     """n_tokens is the length of `slots`; `held`, `first` and `positions` may be None."""
     R, maxb = _table(offsets, block_table)
-    n = slots.numel()
-    _need(context, R, "context")
-    if held is not None:
-        _need(held, R, "held")
-    _need(held_out, R, "held_out")
-    _need(next_free, 1, "next_free")
-    if first is not None:
-        _need(first, 1, "first")
-    if positions is not None:
-        _need(positions, n, "positions")
-    _check("ptstore_block_tables", _lib.ptstore_block_tables(
-        _dev(offsets, torch.int64, "offsets"), n, _dev(context, torch.int32, "context"),
-        _dev(held, torch.int32, "held"), R, maxb, block_tokens,
-        _dev(free_blocks, torch.int32, "free_blocks"), free_blocks.numel(),
-        _dev(first, torch.int64, "first"), _dev(block_table, torch.int32, "block_table"),
-        _dev(slots, torch.int64, "slots"), _dev(positions, torch.int32, "positions"),
-        _dev(held_out, torch.int32, "held_out"), _dev(next_free, torch.int64, "next_free"),
-        _stream(stream)))
+    n, i32, i64 = slots.numel(), torch.int32, torch.int64
+    rc = _lib.ptstore_block_tables(
+        _arg(offsets, i64, R + 1, "offsets"), n, _arg(context, i32, R, "context"),
+        None if held is None else _arg(held, i32, R, "held"), R, maxb, block_tokens,
+        _arg(free_blocks, i32, 0, "free_blocks"), free_blocks.numel(),
+        None if first is None else _arg(first, i64, 1, "first"),
+        _arg(block_table, i32, 0, "block_table"), _arg(slots, i64, 0, "slots"),
+        None if positions is None else _arg(positions, i32, n, "positions"),
+        _arg(held_out, i32, R, "held_out"), _arg(next_free, i64, 1, "next_free"), _stream(stream))
+    if rc:
+        _check("ptstore_block_tables", rc)
 
 
 _KV_DTYPES = {PTSTORE_KV_BF16: torch.bfloat16, PTSTORE_KV_FP16: torch.float16,
@@ -443,16 +446,17 @@ _KV_DTYPES = {PTSTORE_KV_BF16: torch.bfloat16, PTSTORE_KV_FP16: torch.float16,
 def _token_rows(t: torch.Tensor, kv: ptstore_kv_t, heads: Optional[int], name: str) -> Tuple[int, int, int]:
     """Address and strides of a [tokens, heads, head_dim] tensor whose rows are contiguous."""
     want = _KV_DTYPES[kv.kind]
-    if not t.is_cuda or t.dtype != want or t.dim() != 3:
+    if not t.is_cuda or t.dtype is not want or t.dim() != 3:
         raise ValueError(f"{name} must be a [tokens, heads, head_dim] device tensor of {want}")
-    if t.shape[2] != kv.head_dim or (heads is not None and t.shape[1] != heads):
+    n, h, dim = t.shape
+    if dim != kv.head_dim or (heads is not None and h != heads):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the cache {kv.kv_heads} heads of "
                          f"{kv.head_dim}")
     token, head, one = t.stride()
     if one != 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
     # a dimension of one row may have any stride: none of its others is reached
-    return t.data_ptr(), token if t.shape[0] > 1 else 0, head if t.shape[1] > 1 else 0
+    return t.data_ptr(), token if n > 1 else 0, head if h > 1 else 0
 
 
 def _rows_of(kv, k, v, slots):
@@ -460,7 +464,7 @@ def _rows_of(kv, k, v, slots):
     kr, vr = _token_rows(k, kv, kv.kv_heads, "k"), _token_rows(v, kv, kv.kv_heads, "v")
     if k.shape[0] != n or v.shape[0] != n:
         raise ValueError(f"k and v hold {k.shape[0]} and {v.shape[0]} tokens, slots {n}")
-    return (*kr, *vr, _dev(slots, torch.int64, "slots"), n)
+    return (*kr, *vr, _arg(slots, torch.int64, n, "slots"), n)
 
 
 def ptstore_kv_append(kv: ptstore_kv_t, k, v, slots, stream=None) -> None:
@@ -479,23 +483,31 @@ def ptstore_attention_workspace(kv: ptstore_kv_t) -> int:
     return n.value
 
 
+def _attention(kv, q, out_rows, lse: Optional[int], offsets, context, block_table, scale, workspace,
+               stream) -> None:
+    """out_rows: address and strides of an output of q's shape; lse: an address, or None."""
+    R, maxb = _table(offsets, block_table)
+    n, heads, _ = q.shape
+    a = ptstore_attention_t(kv, *_token_rows(q, kv, None, "q"), *out_rows, lse,
+                            _arg(offsets, torch.int64, R + 1, "offsets"),
+                            _arg(context, torch.int32, R, "context"),
+                            _arg(block_table, torch.int32, 0, "block_table"), n, R, maxb, heads, scale,
+                            _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
+    rc = _lib.ptstore_attention(C.byref(a), stream)
+    if rc:
+        _check("ptstore_attention", rc)
+
+
 def ptstore_attention(kv: ptstore_kv_t, q, out, lse, offsets, context, block_table, scale: float,
                       workspace, stream=None) -> None:
     """`lse` may be None; `workspace`: a uint8 tensor of ptstore_attention_workspace(kv) bytes."""
-    R, maxb = _table(offsets, block_table)
-    _need(context, R, "context")
-    qr = _token_rows(q, kv, None, "q")
-    outr = _token_rows(out, kv, q.shape[1], "out")
-    n, heads = q.shape[0], q.shape[1]
+    _token_rows(q, kv, None, "q")
+    n, heads, _ = q.shape
+    rows = _token_rows(out, kv, heads, "out")
     if out.shape[0] != n:
         raise ValueError(f"out holds {out.shape[0]} tokens, q {n}")
-    if lse is not None:
-        _need(lse, n * heads, "lse")
-    a = ptstore_attention_t(kv, *qr, *outr, _dev(lse, torch.float32, "lse"),
-                            _dev(offsets, torch.int64, "offsets"), _dev(context, torch.int32, "context"),
-                            _dev(block_table, torch.int32, "block_table"), n, R, maxb, heads, scale,
-                            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
-    _check("ptstore_attention", _lib.ptstore_attention(C.byref(a), _stream(stream)))
+    _attention(kv, q, rows, None if lse is None else _arg(lse, torch.float32, n * heads, "lse"), offsets,
+               context, block_table, scale, workspace, _stream(stream))
 
 
 # ---------------------------------------------------------------------------
@@ -752,6 +764,7 @@ class PagedCache:
         self.data = data
         self.dtype = _KV_DTYPES[_KV_KINDS[kind]]
         self._workspaces = {}
+        self._scale = head_dim ** -0.5
         self._planes = []
         at = data.data_ptr()
         for h, slab in zip(heads, slabs):
@@ -772,16 +785,13 @@ class PagedCache:
             stream = torch.cuda.ExternalStream(int(stream))
         return torch.cuda.stream(stream)
 
-    def _workspace(self, stream) -> torch.Tensor:
-        """The workspace of a stream: one serves every layer, and the calls on it in turn."""
-        handle = _stream(stream)
-        ws = self._workspaces.get(handle)
-        if ws is None:
-            need = max(ptstore_attention_workspace(kv) for kv in self._planes)
-            with self._on(stream):
-                ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
-                if not torch.cuda.is_current_stream_capturing():  # a graph keeps its own
-                    self._workspaces[handle] = ws
+    def _workspace(self, stream, handle: int) -> torch.Tensor:
+        """Makes the workspace of a stream: one serves every layer, and the calls on it in turn."""
+        need = max(ptstore_attention_workspace(kv) for kv in self._planes)
+        with self._on(stream):
+            ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
+            if not torch.cuda.is_current_stream_capturing():  # a graph keeps its own
+                self._workspaces[handle] = ws
         return ws
 
     def tables(self, offsets, context, block_table, free_blocks, n_tokens: int, held=None, first=None,
@@ -789,10 +799,8 @@ class PagedCache:
         """Give the batch's requests their blocks: fills the new entries of `block_table` and
         returns (slots, positions, held after, next free entry)."""
         with self._on(stream):
-            slots = offsets.new_empty(n_tokens)
-            positions = context.new_empty(n_tokens)
-            held_out = context.new_empty(block_table.shape[0])
-            next_free = offsets.new_empty(1)
+            slots, next_free = offsets.new_empty(n_tokens), offsets.new_empty(1)
+            positions, held_out = context.new_empty(n_tokens), context.new_empty(block_table.shape[0])
         ptstore_block_tables(offsets, context, held, self.block_tokens, free_blocks, first, block_table,
                              slots, positions, held_out, next_free, stream)
         return slots, positions, held_out, next_free
@@ -816,14 +824,24 @@ class PagedCache:
         scale: 1 / sqrt(head_dim) unless given. workspace: one of the caller's,
         instead of the one that the cache keeps for the stream."""
         kv = self._planes[layer]
-        with self._on(stream):
-            if out is None:
-                out = q.new_empty(q.shape)
-            sums = q.new_empty(q.shape[:2], dtype=torch.float32) if lse else None
+        handle = _stream(stream)
         if workspace is None:
-            workspace = self._workspace(stream)
-        ptstore_attention(kv, q, out, sums, offsets, context, block_table,
-                          kv.head_dim ** -0.5 if scale is None else scale, workspace, stream)
+            workspace = self._workspaces.get(handle)
+            if workspace is None:
+                workspace = self._workspace(stream, handle)
+        if q.dim() != 3:
+            raise ValueError(f"q must be [tokens, heads, head_dim], got shape {tuple(q.shape)}")
+        n, heads, dim = q.shape
+        scale = self._scale if scale is None else scale
+        with self._on(stream):
+            sums = q.new_empty((n, heads), dtype=torch.float32) if lse else None
+            made = q.new_empty((n, heads, dim)) if out is None else None
+        if made is None:
+            ptstore_attention(kv, q, out, sums, offsets, context, block_table, scale, workspace, handle)
+        else:  # contiguous, and of the right shape and place
+            out = made
+            _attention(kv, q, (out.data_ptr(), heads * dim, dim), sums.data_ptr() if lse else None, offsets,
+                       context, block_table, scale, workspace, handle)
         return (out, sums) if lse else out
 
 
