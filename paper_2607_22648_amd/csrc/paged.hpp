@@ -19,7 +19,8 @@ constexpr uint32_t kEndless = 253;  // exponent bytes from here on read as NaN
 constexpr int64_t kMaxCacheBlocks = 1ll << 30;
 constexpr int64_t kMaxPlane = 1ll << 36;  // bytes: rows are numbered in 16 bytes, 32 bits
 
-// Division of a key's position (below 2^31) by the page size: with 2^s >=
+// Division of a key's position (below 2^31) by the page size (or of another such
+// number by a constant of the call): with 2^s >=
 // 2^31 d and M = ceil(2^s / d), the error M d - 2^s is below d, so n M / 2^s
 // rounds down to n / d for every n < 2^31.
 struct PageDiv {
@@ -28,7 +29,7 @@ struct PageDiv {
 
 inline PageDiv page_div(int page) {
     uint32_t s = 31;
-    while ((1u << (s - 31)) < (uint32_t)page) ++s;
+    while ((1ull << (s - 31)) < (uint64_t)page) ++s;
     return {(uint32_t)(((1ull << s) + page - 1) / page), s, (uint32_t)page};
 }
 
