@@ -102,6 +102,18 @@ __device__ inline float step_of(uint32_t byte) {
     return __uint_as_float((byte >= kEndless ? 255u : byte) << 23);
 }
 
+// Makes the wave wait for several exchanged values at once: one by one, as the
+// compiler likes to place them, each costs a trip through LDS.
+__device__ inline void together(uint32_t (&x)[1]) { asm volatile("" : "+v"(x[0])); }
+__device__ inline void together(uint32_t (&x)[2]) { asm volatile("" : "+v"(x[0]), "+v"(x[1])); }
+__device__ inline void together(uint32_t (&x)[4]) {
+    asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+}
+__device__ inline void together(uint32_t (&x)[8]) {
+    asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]),
+                 "+v"(x[7]));
+}
+
 // Lowest score kept: what a row starts from instead of minus infinity, so that
 // the differences of two such rows stay numbers.
 constexpr float kLowest = -3.0e38f;

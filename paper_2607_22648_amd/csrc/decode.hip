@@ -237,9 +237,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     // the wave in 32 bits.
     const uint8_t* const kbase = p.kv.k + (kFour ? h4 * (D / 8) : (lane % kLanes) * 16);
     const uint8_t* const vbase = p.kv.v + (kFour ? (lane & 3) * (D / 8) : (lane % kLanes) * 16);
-    auto row_at = [&](const uint8_t* base, const KeyRow& r, int key) {
-        return base + ((uint64_t)(uint32_t)__shfl((int)r.at, key) << 4);
-    };
     auto four = [&](const uint8_t* at) {
         if constexpr (D == 128) return once16(at);
         const v2u x = once8(at);
@@ -248,28 +245,40 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     auto load_k = [&](const KeyRow& r) {
         if constexpr (kFour) {
             kpow = load_powers<D>(p.kv.k, r.power);
+            uint32_t at[kGroups];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g)
-                kreg[g] = four(row_at(kbase, r, 32 * (g >> 1) + 4 * (g & 1) + key_of_row));
+            for (int g = 0; g < kGroups; ++g) at[g] = (uint32_t)__shfl((int)r.at, 32 * (g >> 1) + 4 * (g & 1) + key_of_row);
+            together(at);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) kreg[g] = four(kbase + ((uint64_t)at[g] << 4));
         } else {
+            uint32_t at[kPieces];
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) kreg[i] = once16(row_at(kbase, r, i * (64 / kLanes) + lane / kLanes));
+            for (int i = 0; i < kPieces; ++i) at[i] = (uint32_t)__shfl((int)r.at, i * (64 / kLanes) + lane / kLanes);
+            together(at);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) kreg[i] = once16(kbase + ((uint64_t)at[i] << 4));
         }
     };
     auto load_v = [&](const KeyRow& r) {
-        if constexpr (kFour) {
-            vpow = load_powers<D>(p.kv.v, r.power);
+        constexpr int kLoads = kFour ? kKeys / kVKeys : kPieces;
+        if constexpr (kFour) vpow = load_powers<D>(p.kv.v, r.power);
+        uint32_t at[kLoads];
 #pragma unroll
-            for (int i = 0; i < kKeys / kVKeys; ++i) vreg[i] = four(row_at(vbase, r, i * kVKeys + (lane >> 2)));
-        } else {
+        for (int i = 0; i < kLoads; ++i)
+            at[i] = (uint32_t)__shfl((int)r.at, kFour ? i * kVKeys + (lane >> 2) : i * (64 / kLanes) + lane / kLanes);
+        together(at);
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) vreg[i] = once16(row_at(vbase, r, i * (64 / kLanes) + lane / kLanes));
+        for (int i = 0; i < kLoads; ++i) {
+            const uint8_t* row = vbase + ((uint64_t)at[i] << 4);
+            if constexpr (kFour)
+                vreg[i] = four(row);
+            else
+                vreg[i] = once16(row);
         }
     };
-    // the exponent of the lane's quarter q of row `key`
-    auto power = [&](uint32_t pow, int key, int quarter) {
-        return ((uint32_t)__shfl((int)pow, key) >> (quarter * (D / 4) / kGroup * 8)) & 255u;
-    };
+    // the exponent of the lane's quarter q of a row, from the word of the row's
+    auto power = [&](uint32_t word, int quarter) { return (word >> (quarter * (D / 4) / kGroup * 8)) & 255u; };
 
     // The order of loads is fixed, since a wait for one waits for all before it: the
     // queries; then, for each piece, the page entries of the piece after it, its K, its V.
@@ -290,9 +299,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     bool endless = false;  // a V value that is not finite lies behind the first row's last key
 
     while (at < k1) {
-        // LDS addresses are formed anew each time: kept, they take two dozen registers
+        // 16-bit: LDS addresses are formed anew each time; kept, they take two dozen
+        // registers
         int here = lane;
-        asm volatile("" : "+v"(here));
+        if constexpr (!kFour) asm volatile("" : "+v"(here));
         // scores of column n: keys 32 b + 8 h4 + 4 (g & 1) + i in s[g][i], b = g >> 1
         v4f s[kGroups];
         if constexpr (!kFour) {
@@ -303,22 +313,31 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
             }
             __builtin_amdgcn_wave_barrier();
         }
+        float kstep[kFour ? kGroups : 1];
+        if constexpr (kFour) {
+            uint32_t word[kGroups];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            s[g] = v4f{0, 0, 0, 0};
-            const int key = 4 * (g & 1) + 8 * ((here & 15) >> 2) + (here & 3);
-            const float step = kFour ? step_of(power(kpow, 32 * (g >> 1) + key, h4)) : 0.f;
+            for (int g = 0; g < kGroups; ++g)
+                word[g] = (uint32_t)__shfl((int)kpow, 32 * (g >> 1) + 4 * (g & 1) + key_of_row);
+            together(word);
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) {
+            for (int g = 0; g < kGroups; ++g) kstep[g] = step_of(power(word[g], h4));
+        }
+        const int krow = 8 * ((here & 15) >> 2) + (here & 3);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) s[g] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int key = 4 * (g & 1) + krow;
                 v4u a;
                 if constexpr (kFour)
-                    a = widen8(kreg[g][t], step);
+                    a = widen8(kreg[g][t], kstep[g]);
                 else
                     a = *(const v4u*)(lds + key * kRow + (((4 * t + (here >> 4)) ^ turn_k<D>(key)) * 16));
-                s[g] = E::mma16(__builtin_bit_cast(typename E::v8, a), __builtin_bit_cast(typename E::v8, q[t]),
-                                s[g]);
+                s[g] = E::mma16(__builtin_bit_cast(typename E::v8, a), __builtin_bit_cast(typename E::v8, q[t]), s[g]);
             }
-        }
         __builtin_amdgcn_wave_barrier();
         const int32_t next = at + stride;
         const uint64_t ok = valid;
@@ -381,6 +400,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
             w[g >> 1][2 * (g & 1) + 1] = pack2<kHalf>(s[g][2], s[g][3]);
         }
 
+        uint32_t vword[kFour ? kKeys / kVKeys : 1];
+        if constexpr (kFour) {
+#pragma unroll
+            for (int j = 0; j < kKeys / kVKeys; ++j) vword[j] = (uint32_t)__shfl((int)vpow, j * kVKeys + (here >> 2));
+            together(vword);
+        }
 #pragma unroll
         for (int b = 0; b < kKeys / 32; ++b) {
             // V's rows of 32 keys into LDS
@@ -388,7 +413,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int key = i * kVKeys + (here >> 2), j = 2 * b + i;
-                    const float step = step_of(power(vpow, 32 * b + key, lane & 3));
+                    const float step = step_of(power(vword[j], here & 3));
                     // every other pair of rows takes a lane's words in the order 1 0 3 2: turn_v
                     // leaves the lowest bit of the columns that 16 lanes write alike
                     const int swap = (key >> 1) & 1;
