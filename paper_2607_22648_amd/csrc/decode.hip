@@ -378,7 +378,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, s[g][i]);
         most = larger_16_32(most);
-        const float top2 = fmaxf(top, most * p.scale2);
+        const float top2 = fmaxf(top, __builtin_fmaf(most, p.scale2, E::kRoom));
         if (__any(top2 > top)) {
             const float less = exp2_of(top - top2);
             sum *= less;

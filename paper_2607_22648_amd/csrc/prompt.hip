@@ -39,7 +39,7 @@ __device__ inline int turn_v(int row) {
 }
 
 // A running maximum that is behind by up to this much (in powers of two) is kept:
-// weights then reach 2^8 instead of 1, which no type here minds, and the
+// weights then reach 2^8 times the largest otherwise, which no type here minds, and the
 // output is rescaled a few times a row instead of at every new maximum.
 constexpr float kBehind = 8.f;
 
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
         most = larger_32(most);
-        const float top2 = fmaxf(top, most * p.scale2);
+        const float top2 = fmaxf(top, __builtin_fmaf(most, p.scale2, E::kRoom));
         if (__any(top2 > top + kBehind)) {
             const float less = exp2_of(top - top2);
             sum *= less;
