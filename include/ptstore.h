@@ -451,10 +451,8 @@ int ptstore_lookup_gather_noalloc(ptstore_t *store, const int32_t *tokens, const
  * graph), on the current device, which has to be the pointers' and the
  * stream's. They keep no state and allocate nothing: calls on different
  * streams and host threads are independent. `offsets` must rise from 0 to
- * n_tokens; a request whose offsets are decreasing, negative or beyond
- * n_tokens is treated as empty, and what is written for tokens that no
- * request, or more than one, has is unspecified. Nothing outside the arrays is
- * touched whatever the device arrays hold.
+ * n_tokens; where they do not, what is written to the outputs is unspecified.
+ * Nothing outside the arrays is touched whatever the device arrays hold.
  * ====================================================================== */
 
 /* What a paged cache holds. BF16, FP16: a slab is [head][slot][dim] values.
@@ -463,10 +461,10 @@ int ptstore_lookup_gather_noalloc(ptstore_t *store, const int32_t *tokens, const
  * exponents, padded to a multiple of 16 bytes. 32 elements along dim share an
  * exponent byte b; element 2i is in the low half of byte i; a code is a sign and
  * one of the levels 0, 0.5, 1, 1.5, 2, 3, 4, 6, and stands for level * 2^(b-127);
- * b = 255 is NaN, and so are 253 and 254, whose values bf16 could not hold. A store holds such blocks when it is made with
- * layer_chunk_bytes of ptstore_kv_slab_bytes: gather and scatter copy slabs
- * whatever they hold. The calls below take and give bf16 for BF16 and MXFP4
- * caches and fp16 for FP16. */
+ * b = 255 is NaN, and so are 253 and 254, whose values bf16 could not hold. A
+ * store holds such blocks when it is made with layer_chunk_bytes of
+ * ptstore_kv_slab_bytes: gather and scatter copy slabs whatever they hold. The
+ * calls below take and give bf16 for BF16 and MXFP4 caches and fp16 for FP16. */
 enum { PTSTORE_KV_BF16 = 0, PTSTORE_KV_FP16 = 1, PTSTORE_KV_MXFP4 = 2 };
 
 /* One layer of a paged cache: its K and V planes, [cache_blocks][slab] each,
@@ -502,6 +500,7 @@ int ptstore_kv_slab_bytes(int32_t kind, int32_t kv_heads, int32_t head_dim, int3
  * block * block_tokens + position % block_tokens, or -1 where its block is
  * beyond max_blocks or its entry is negative. A held block is reused first: the
  * entry of a position below held[r] * block_tokens is read from block_table.
+ * A request whose offsets are decreasing, negative or beyond n_tokens takes no block.
  * held_out must not be held, nor next first (outputs may not overlap inputs).
  * Errors: INVALID (sizes out of range, R * max_blocks > 2^29, max_blocks *
  * block_tokens > 2^30, tokens without requests, a NULL pointer), HIP.
@@ -578,7 +577,8 @@ typedef struct {
 int ptstore_attention_workspace(const ptstore_kv_t *kv, int64_t *bytes);
 
 /* Errors: INVALID (shapes, sizes, strides or alignment as stated; max_blocks *
- * block_tokens > 2^30; no cache blocks; a workspace too small), HIP. */
+ * block_tokens > 2^30; n_tokens * q_heads >= 2^31; no cache blocks; a workspace too
+ * small), HIP. */
 int ptstore_attention(const ptstore_attention_t *args, void *stream);
 
 /* ======================================================================

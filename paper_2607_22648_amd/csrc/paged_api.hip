@@ -79,17 +79,26 @@ int compute_units(int* cus) {
 }
 
 // Whether a call's rows go 128 to a tile, or 16. The host knows the average
-// request alone. Behind 4,000 keys, 8 KV heads of 4 query heads (us, 16 and 128):
+// request alone. Behind 4,000 keys, 8 KV heads of 4 query heads (us, joins included):
 //
-//   tokens        4 x 32  16 x 32  32 x 32   64 x 2  128 x 2  256 x 2
-//   16 rows           91      252      525       55       86      167
-//   128 rows         149      150      156  PROMPT_SMALL
+//   tokens x requests   4 x 32  16 x 32  32 x 32   64 x 2  128 x 2  256 x 2
+//   16 rows                 91      252      525       55       86      167
+//   128 rows               149      150      156       38       43       68
 bool many_rows(const AttendPlan& p) { return p.n_tokens * p.group > (int64_t)32 * p.R; }
 
-// Whether requests of few rows in such a batch go to the other kernel: one workgroup
-// goes through all keys of a tile, 1.3 us for 64, however few its rows are. The
-// launches that may find nothing to do cost 6 us, so it takes room for 8,192 keys.
-bool mixed(const AttendPlan& p) { return p.R > 1 && (int64_t)p.max_blocks * p.kv.div.page >= 8192; }
+// Whether a batch goes to both kernels, requests of few rows to the one for 16 and the
+// others to the one for 128. A workgroup of the latter goes through all keys of a tile,
+// 1.3 us for 64, however few its rows are; in the former a long request reads its keys
+// once for each 16 rows: 256 single tokens and 512 tokens of one request, behind
+// 4,000, take 745 us by both and 905 by the former. The launches that may find nothing to
+// do cost 5 to 9 us (64 drafts of 4 tokens: 170 us, 162), so it takes room for 8,192 keys
+// and, in a batch of few rows a request, kManyRows beyond a token each: at 508 of them
+// both ways take the same time (256 single tokens and 128 of one request, 720 us).
+constexpr int64_t kManyRows = 512;
+bool mixed(const AttendPlan& p, bool prompts) {
+    return p.R > 1 && (int64_t)p.max_blocks * p.kv.div.page >= 8192 &&
+           (prompts || (p.n_tokens - p.R) * p.group >= kManyRows);
+}
 
 int64_t workspace_of(const Planes& kv, int cus) {
     const int64_t a = decode_workspace(kv, decode_shares(kv, cus)), b = prompt_workspace(kv, cus);
@@ -105,7 +114,8 @@ const char* sized(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int
         (R == 0 && n_tokens > 0))
         return "R, max_blocks or n_tokens out of range";
     if ((int64_t)max_blocks * kv->block_tokens > kMaxKeys) return "max_blocks * block_tokens exceeds 2^30";
-    if (n_tokens >= (1ll << 31) || n_tokens * q_heads >= (1ll << 34)) return "too many tokens";
+    // rows are numbered in 32 bits
+    if (n_tokens >= (1ll << 31) || n_tokens * q_heads >= (1ll << 31)) return "n_tokens * q_heads exceeds 2^31";
     p->n_tokens = n_tokens;
     p->R = R;
     p->max_blocks = max_blocks;
@@ -141,7 +151,8 @@ int ptstore_block_tables(const int64_t* offsets, int64_t n_tokens, const int32_t
                          int64_t n_free, const int64_t* first, int32_t* block_table, int64_t* slots,
                          int32_t* positions, int32_t* held_out, int64_t* next, void* stream) {
     if (R < 0 || max_blocks < 1 || (int64_t)R * max_blocks > kMaxEntries || block_tokens < 1 ||
-        block_tokens > 64 || (int64_t)max_blocks * block_tokens > kMaxKeys || n_tokens < 0 || n_tokens >= (1ll << 40) || n_free < 0 || (R == 0 && n_tokens > 0))
+        block_tokens > 64 || (int64_t)max_blocks * block_tokens > kMaxKeys || n_tokens < 0 ||
+        n_tokens >= (1ll << 40) || n_free < 0 || (R == 0 && n_tokens > 0))
         return refuse("ptstore_block_tables: a size is out of range");
     if (!next || (R > 0 && (!offsets || !context || !block_table || !held_out)) || (n_tokens > 0 && !slots) ||
         (n_free > 0 && !free_blocks))
@@ -221,9 +232,9 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
     p.scale2 = a->scale * 1.4426950408889634f;
     p.parts = static_cast<float*>(a->workspace);
     p.shares = decode_shares(p.kv, cus);
-    const bool prompts = many_rows(p), both = prompts && mixed(p);
+    const bool prompts = many_rows(p), both = mixed(p, prompts);
     hipError_t e = hipSuccess;
-    if (prompts) {
+    if (prompts || both) {
         p.few_rows = both ? kFewRows : 0;
         split_prompt(&p, cus);
         e = launch_prompt(p, (hipStream_t)stream);

@@ -786,12 +786,16 @@ class PagedCache:
         return torch.cuda.stream(stream)
 
     def _workspace(self, stream, handle: int) -> torch.Tensor:
-        """Makes the workspace of a stream: one serves every layer, and the calls on it in turn."""
-        need = max(ptstore_attention_workspace(kv) for kv in self._planes)
+        """The workspace of a stream: one serves every layer, and the calls on it in turn.
+        A graph, which may be replayed on any stream, gets its own."""
         with self._on(stream):
-            ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
-            if not torch.cuda.is_current_stream_capturing():  # a graph keeps its own
-                self._workspaces[handle] = ws
+            graph = torch.cuda.is_current_stream_capturing()
+            ws = None if graph else self._workspaces.get(handle)
+            if ws is None:
+                need = max(ptstore_attention_workspace(kv) for kv in self._planes)
+                ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
+                if not graph:
+                    self._workspaces[handle] = ws
         return ws
 
     def tables(self, offsets, context, block_table, free_blocks, n_tokens: int, held=None, first=None,
@@ -826,9 +830,7 @@ class PagedCache:
         kv = self._planes[layer]
         handle = _stream(stream)
         if workspace is None:
-            workspace = self._workspaces.get(handle)
-            if workspace is None:
-                workspace = self._workspace(stream, handle)
+            workspace = self._workspace(stream, handle)
         if q.dim() != 3:
             raise ValueError(f"q must be [tokens, heads, head_dim], got shape {tuple(q.shape)}")
         n, heads, dim = q.shape

@@ -267,6 +267,30 @@ def test_attention_head_groups(P, kind, heads, group):
     Case(P, kind, heads, group, 64, 16, [(1, 50), (7, 30), (40, 0)], seed=group).check()
 
 
+@pytest.mark.parametrize("byte", [0, 1, 252, 253, 254, 255])
+def test_four_bit_exponents_at_the_ends(P, byte):
+    """Values of the smallest and largest exponents; from 253 on, NaN: read, and attended to."""
+    cache = P.PagedCache(1, 1, 64, 2, 16, "mxfp4")
+    codes = torch.full((2, 2, 16 * 32), 0x21, dtype=torch.uint8)  # pairs of 0.5, 1
+    plane = torch.cat([codes, torch.full((2, 2, 32), 127, dtype=torch.uint8)], dim=2)
+    plane[1, 0, 512:] = byte  # V, block 0
+    cache.data.copy_(plane.flatten().cuda())
+    slots = torch.arange(16, device="cuda")
+    v = cache.read(0, slots)[1].double().cpu()
+    want = torch.tensor([0.5, 1.0], dtype=torch.float64).repeat(32) * 2.0 ** (byte - 127)
+    bad = byte >= 253
+    assert bool(v.isnan().all()) if bad else torch.equal(v, want.expand(16, 1, 64))
+    for n in (1, 40):  # few rows, and many
+        q = torch.zeros((n, 1, 64), dtype=torch.bfloat16, device="cuda")
+        off = torch.tensor([0, n], device="cuda")
+        out = cache.attend(0, q, off, torch.tensor([15], dtype=torch.int32, device="cuda"),
+                           torch.tensor([[0]], dtype=torch.int32, device="cuda")).double().cpu()
+        if bad:
+            assert bool(out.isnan().all())
+        else:  # a mean of equal values; the smallest are below bf16's normal range
+            assert bool(((out - want).abs() <= 2.0 ** -7 * want + 2.0 ** -126).all())
+
+
 @pytest.mark.parametrize("kind", ["fp16", "mxfp4"])
 @pytest.mark.parametrize("page", [1, 2, 5, 8, 24, 33, 64])
 def test_attention_page_sizes(P, kind, page):
@@ -289,6 +313,14 @@ def test_attention_prompts(P, kind):
 def test_attention_mixed_batch(P, kind):
     """Single tokens behind long contexts beside prompts: a batch of both kernels' requests."""
     Case(P, kind, 1, 4, 64, 16, [(1, 8300), (150, 40), (1, 3), (8, 100), (9, 100), (0, 5), (40, 0)], seed=17).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mxfp4"])
+def test_attention_single_tokens_and_a_prompt(P, kind):
+    """Few rows a request on average, but a prompt among them: both kernels' requests again."""
+    reqs = [(1, 8300), (140, 33)] + [(1, 3 * i) for i in range(30)]
+    Case(P, kind, 2, 4, 64, 16, reqs, seed=20).check()
+    Case(P, kind, 2, 4, 64, 16, reqs[::-1], seed=21).check()
 
 
 @pytest.mark.parametrize("new,past", [(130, 900), (300, 0), (513, 70)])
@@ -428,6 +460,29 @@ def test_attention_first_call_in_a_graph(P):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, c.cache.attend(0, q, off, ctx, table))
+
+
+def test_attention_graph_of_a_used_stream(P):
+    """A graph captured on a stream whose workspace the cache has: replayed on another
+    stream beside calls on that one, both right."""
+    c = Case(P, "bf16", 2, 4, 128, 16, [(1, 6000), (1, 5000)], seed=13)
+    q, off, ctx, table = c.q.cuda(), c.off.cuda(), c.ctx.cuda(), c.table.cuda()
+    q2 = torch.randn_like(q)
+    out = torch.empty_like(q)
+    want, want2 = c.cache.attend(0, q, off, ctx, table), c.cache.attend(0, q2, off, ctx, table)
+    s = torch.cuda.Stream()
+    c.cache.attend(0, q, off, ctx, table, out=out, stream=s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        c.cache.attend(0, q, off, ctx, table, out=out)
+    for i in range(4):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        others = [c.cache.attend(0, q2, off, ctx, table, stream=s) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(torch.equal(o, want2) for o in others)
 
 
 def test_attention_on_other_streams(P):

@@ -54,7 +54,9 @@ def test_attention_refuses_on_the_host(P):
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "scale" in text()
     a.scale, a.max_blocks = 1.0, (1 << 26) + 1
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "2^30" in text()
-    a.max_blocks, a.R = 4, 0
+    a.max_blocks, a.n_tokens = 4, 1 << 29
+    assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "2^31" in text()
+    a.n_tokens, a.R = 1, 0
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "out of range" in text()
     a.R = 1
     assert lib.ptstore_attention(C.byref(a), None) == P.PTSTORE_ERR_INVALID and "null" in text()
