@@ -11,7 +11,10 @@
 // for are exact in every precision. A group that holds an infinity or a NaN gets the
 // exponent 255, which reads as NaN. A lane takes 8 elements, four lanes a group.
 //
-// Both are bound by memory: 2 bytes read and 2 (or 17/32) written an element.
+// Both are bound by memory: 2 bytes read and 2 (or 17/32) written an element. 16,384
+// tokens of 8 heads of 128 take 22.6 to 24.6 us, 5.5 TB/s of the 5.7 that a plain copy
+// reaches; 8,200 into 4 bits 7.6 to 9.5, and out of them 9.3 to 9.9 (42 MB, 4.5 TB/s:
+// a launch this short does not reach the full rate).
 #include <hip/hip_runtime.h>
 
 #include "paged.hpp"
@@ -68,7 +71,7 @@ __global__ __launch_bounds__(kThreads) void k_rows16(Planes kv, Rows k, Rows v, 
         *kr = there ? *(const v4u*)(kv.k + page) : zero;
         *vr = there ? *(const v4u*)(kv.v + page) : zero;
     } else if (there) {
-        // read once: 16,384 tokens of 8 heads of 128 take 24.8 us so, 27.4 through the caches' usual order
+        // read once, past the caches' usual order: 10 % faster
         const v4u a = __builtin_nontemporal_load(kr), b = __builtin_nontemporal_load(vr);
         *(v4u*)(kv.k + page) = a;
         *(v4u*)(kv.v + page) = b;

@@ -7,19 +7,27 @@
 // (request, tile of query rows, KV head, step) and cut into equal shares, one
 // for each workgroup that the device holds at once. A share that ends inside a
 // (tile, KV head) leaves its maximum, sum and output in the workspace, two such
-// parts a workgroup at most, and a second kernel joins them. 64 requests of 120 to 8,190
-// keys take the time of as many bytes in equal requests; workgroups for fixed
+// parts a workgroup at most, and a second kernel joins them. Workgroups for fixed
 // parts of a request were up to 1.3 times slower by how their number fell on the
-// device, and paid their start per part.
+// device, and paid their start per part. The KV heads of a share run side by side, so
+// that neighbouring slabs are read together (217 us instead of 194 otherwise, 64
+// requests of 120 to 8,190 keys).
 //
 // A workgroup is four waves that share nothing until a (tile, KV head) is done: wave
-// w takes every fourth piece of a share's keys. K and V rows are loaded whole (four
-// rows of 256 bytes an instruction; rows in 64-byte pieces, as the matrix
-// instruction takes K, reached 5.8 TB/s instead of 6.4), pass through 8 KiB of LDS that
-// only this wave uses, and are read as the matrix instructions want them, V
+// w takes every fourth piece of a share's keys. 16-bit K and V rows are loaded whole
+// (four rows of 256 bytes an instruction; in 64-byte pieces, as the matrix
+// instruction takes K, they reached 5.8 TB/s instead of 6.4), pass through 8 KiB of LDS
+// that only this wave uses, and are read as the matrix instructions want them, V
 // transposed. 4-bit K is loaded in that order from the start: its rows are 64
-// bytes. The next piece's loads are issued as soon as a register is free, so that each wave
-// keeps a piece's bytes in flight while it computes.
+// bytes. The next piece's loads are issued as soon as a register is free, so that each
+// wave keeps a piece's bytes in flight while it computes.
+//
+// 8 KV heads of 128 with 4 query heads each, one token a request (without the join,
+// 5 us): 64 requests of 8,192 keys 315 us, 6.8 TB/s of the 7.2 that a plain read reaches;
+// of 4-bit keys 97 us, 5.9 TB/s, where widening the codes (a quarter of the
+// instructions) and the two exchanges of a row's exponent take as long as the memory.
+// One request of 778 keys takes 7.7 us, about what a chain of its trips through
+// memory (lengths, page, K, V) takes.
 //
 // Query rows are the (token, head of the group) pairs of one KV head, 16 to a
 // tile: with 4 heads to a KV head a single token fills 4 of the 16 columns, and
@@ -104,7 +112,8 @@ __device__ inline Shares find_step(const AttendPlan& p, int step_keys, int64_t s
         s.all += s_sum[i];
     }
     if (s.all < s.count) s.count = s.all;
-    const int64_t at = share < s.count ? (last ? s.begin(share + 1) - 1 : s.begin(share)) : -1, lo = before + scan - mine;
+    const int64_t lo = before + scan - mine;
+    const int64_t at = share >= s.count ? -1 : last ? s.begin(share + 1) - 1 : s.begin(share);
     if (at >= lo && at < lo + mine) {
         s_r = r0;
         s_first = lo;
@@ -247,7 +256,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
             kpow = load_powers<D>(p.kv.k, r.power);
             uint32_t at[kGroups];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) at[g] = (uint32_t)__shfl((int)r.at, 32 * (g >> 1) + 4 * (g & 1) + key_of_row);
+            for (int g = 0; g < kGroups; ++g)
+                at[g] = (uint32_t)__shfl((int)r.at, 32 * (g >> 1) + 4 * (g & 1) + key_of_row);
             together(at);
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) kreg[g] = four(kbase + ((uint64_t)at[g] << 4));
@@ -522,7 +532,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 // that it begins in and the KV head, a wave a row. The wave's halves (dim 64: quarters)
 // take every other part, 4 dimensions a lane, several parts in flight. (A kernel of
 // its own: joined by the workgroup that writes the last part, which has to pass the parts
-// through memory that all dies see, one request of 32,768 keys takes 45 us, not 34.)
+// through memory that all dies see, one request of 32,768 keys took 45 us, not 34.)
+// 256 parts of one request: 6.7 us.
 constexpr int kJoinWaves = 8;
 
 template <int D, bool kHalf, bool kFour>
@@ -609,8 +620,8 @@ hipError_t run_kind(const AttendPlan& p, hipStream_t s) {
 }  // namespace
 
 // As many as fill the device: two workgroups a compute unit. More, smaller ones even
-// out no better and pay their start: 64 requests of 8,191 keys 345 us, with four a
-// compute unit 358, with eight 369.
+// out no better and pay their start: 64 requests of 8,192 keys took 4 % longer with
+// four a compute unit, 7 % with eight.
 int decode_shares(const Planes& kv, int cus) {
     const int shares = 2 * cus / kv.heads;
     return shares > 0 ? shares : 1;

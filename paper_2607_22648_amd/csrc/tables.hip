@@ -10,6 +10,9 @@
 // workspace and no flags between workgroups. A workgroup sums the wants before
 // its chunk of requests for itself (16 bytes a request, from L2) and scans the
 // chunk's own in LDS; `parts` workgroups of a chunk share its entries and tokens.
+// 1 request of 1,000 tokens takes 4.4 us, 256 of one token 6.6, 700 of 1 to 2,801 (980,000
+// tokens, 12 MB written) 9.7: its writes alone would take 2 us, the rest are the
+// dependent trips lengths, sum, search, free entry, slot.
 #include <hip/hip_runtime.h>
 
 #include "paged.hpp"
