@@ -148,13 +148,16 @@ __device__ inline int turn_k(int row) {
 
 // And of V's: two groups of 16 lanes read rows {0-3} and {8-11} (or {16-19} and {24-27}), 32
 // bytes each, in one pass of the banks: eight rows have to differ in the upper
-// bits. Rows of 128 bytes (dim 64) already differ by parity.
-template <int D>
+// bits. Rows of 128 bytes (dim 64) already differ by parity. The lowest bit is free,
+// since a read takes both columns of a pair: 4-bit rows, whose lanes write columns 2
+// or 4 apart, turn by it too.
+template <int D, bool kFour>
 __device__ inline int turn_v(int row) {
+    const int low = kFour ? (row >> 1) & 1 : 0;
     if constexpr (D == 128)
-        return 2 * ((row & 3) + 4 * ((row >> 3) & 1));
+        return 2 * ((row & 3) + 4 * ((row >> 3) & 1)) + low;
     else
-        return 2 * (((row >> 1) & 1) + 2 * ((row >> 3) & 1));
+        return 2 * (((row >> 1) & 1) + 2 * ((row >> 3) & 1)) + low;
 }
 
 template <int D, bool kHalf, bool kFour>
@@ -424,21 +427,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 for (int i = 0; i < 2; ++i) {
                     const int key = i * kVKeys + (here >> 2), j = 2 * b + i;
                     const float step = step_of(power(vword[j], here & 3));
-                    // every other pair of rows takes a lane's words in the order 1 0 3 2: turn_v
-                    // leaves the lowest bit of the columns that 16 lanes write alike
-                    const int swap = (key >> 1) & 1;
 #pragma unroll
                     for (int c = 0; c < kWords; ++c) {
-                        const int col = (here & 3) * kWords + (c ^ swap);
-                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D>(key)) * 16)) =
-                            widen8(swap ? vreg[j][c ^ 1] : vreg[j][c], step);
+                        const int col = (here & 3) * kWords + c;
+                        *(v4u*)(lds + key * kRow + ((col ^ turn_v<D, kFour>(key)) * 16)) = widen8(vreg[j][c], step);
                     }
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                     const int key = i * (64 / kLanes) + here / kLanes;
-                    *(v4u*)(lds + key * kRow + (((here % kLanes) ^ turn_v<D>(key)) * 16)) = vreg[i];
+                    *(v4u*)(lds + key * kRow + (((here % kLanes) ^ turn_v<D, kFour>(key)) * 16)) = vreg[i];
                 }
             }
             __builtin_amdgcn_wave_barrier();
@@ -453,8 +452,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 const int col = 2 * i + ((m & 3) >> 1), in = (m & 1) * 8;
-                const v2u lo = read_transposed(lds + vrow * kRow + ((col ^ turn_v<D>(vrow)) * 16) + in);
-                const v2u hi = read_transposed(lds + (vrow + 4) * kRow + ((col ^ turn_v<D>(vrow + 4)) * 16) + in);
+                const v2u lo = read_transposed(lds + vrow * kRow + ((col ^ turn_v<D, kFour>(vrow)) * 16) + in);
+                const v2u hi = read_transposed(lds + (vrow + 4) * kRow + ((col ^ turn_v<D, kFour>(vrow + 4)) * 16) + in);
                 vt[i] = join(lo, hi);
             }
 #pragma unroll

@@ -39,9 +39,12 @@ template <int D>
 __device__ inline int turn_k(int row) {
     return D == 128 ? row & 15 : (row >> 1) & 7;
 }
-template <int D>
+template <int D, bool kFour>
 __device__ inline int turn_v(int row) {
-    return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+    // the low bits are free, since a read takes all four columns: 4-bit rows, whose lanes
+    // write columns 2 or 4 apart, turn by them too
+    const int low = !kFour ? 0 : D == 128 ? row & 3 : (row >> 1) & 1;
+    return (D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2) + low;
 }
 
 // A running maximum that is behind by up to this much (in powers of two) is kept:
@@ -144,20 +147,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
     // 16 wave + i rows of a load + .. (K: turned by i, too).
     const int at_row = 16 * wave + lane / kLanes;
     uint32_t k_write[kFour ? kPieces : kLoads], v_write[kFour ? kPieces : 1];
-    const int turned = kFour ? (D == 128 ? at_row & 3 : (at_row >> 1) & 1) : 0;
     if constexpr (kFour) {
-        // V: turn_v leaves the low bits of the columns that 16 lanes write alike, so rows
-        // take a lane's words in orders of their own
 #pragma unroll
         for (int c = 0; c < kPieces; ++c) {
             k_write[c] = at_row * kRow + ((((lane & 3) * kPieces + c) ^ turn_k<D>(at_row)) * 16);
-            v_write[c] = at_row * kRow + ((((lane & 3) * kPieces + (c ^ turned)) ^ turn_v<D>(at_row)) * 16);
+            v_write[c] = at_row * kRow + ((((lane & 3) * kPieces + c) ^ turn_v<D, kFour>(at_row)) * 16);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             k_write[i] = at_row * kRow + (((lane % kLanes) ^ turn_k<D>(at_row + i * (64 / kLanes))) * 16);
-        v_write[0] = at_row * kRow + (((lane % kLanes) ^ turn_v<D>(at_row)) * 16);
+        v_write[0] = at_row * kRow + (((lane % kLanes) ^ turn_v<D, kFour>(at_row)) * 16);
     }
     // K reads: row of K that accumulator row m of a 32-key piece stands for, so that lanes
     // then hold 8 consecutive keys of each 16; column 2 i + half.
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         const int g = lane >> 4, l16 = lane & 15, row = 8 * (g >> 1) + (l16 >> 2);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
-            v_read[i] = row * kRow + (((4 * i + 2 * (g & 1) + ((l16 & 3) >> 1)) ^ turn_v<D>(row)) * 16) + (l16 & 1) * 8;
+            v_read[i] = row * kRow + (((4 * i + 2 * (g & 1) + ((l16 & 3) >> 1)) ^ turn_v<D, kFour>(row)) * 16) + (l16 & 1) * 8;
     }
 
     // step t to LDS; V's rows that are not there as zeros (4-bit: as finite values)
@@ -201,12 +201,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             const int shift = (lane & 3) * (D / 4) / kGroup * 8;
             const float ks = step_of(((uint32_t)__shfl((int)kpow, at_row) >> shift) & 255u);
             const float vs = step_of(((uint32_t)__shfl((int)vpow, at_row) >> shift) & 255u);
-            const v4u a = turned & 1 ? v4u{vreg[0][1], vreg[0][0], vreg[0][3], vreg[0][2]} : vreg[0];
-            const v4u w = turned & 2 ? v4u{a[2], a[3], a[0], a[1]} : a;
 #pragma unroll
             for (int c = 0; c < kPieces; ++c) {
                 *(v4u*)(km + k_write[c]) = widen8(kreg[0][c], ks);
-                *(v4u*)(vm + v_write[c]) = widen8(w[c], vs);
+                *(v4u*)(vm + v_write[c]) = widen8(vreg[0][c], vs);
             }
         } else {
 #pragma unroll
