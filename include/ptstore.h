@@ -571,7 +571,7 @@ typedef struct {
 } ptstore_attention_t;
 
 /* Bytes of workspace that an attention over a layer needs, 16-byte aligned. It
- * follows from the layer's heads and head_dim and the device alone (some 34 MB at
+ * follows from the layer's heads and head_dim and the device alone (some 41 MB at
  * most for 8 heads of 128): one serves every call on it. Host only. Errors: INVALID,
  * HIP. */
 int ptstore_attention_workspace(const ptstore_kv_t *kv, int64_t *bytes);

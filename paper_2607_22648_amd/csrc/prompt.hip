@@ -441,11 +441,15 @@ hipError_t run_kind(const AttendPlan& p, hipStream_t s) {
 
 }  // namespace
 
+// (tile, KV head) pairs of a last turn that are still split: 0.6 of the turn's places.
+static int64_t most_rest(int cus) { return 2ll * cus * 3 / 5; }
+
 // Two workgroups a compute unit run at once. Where a batch has fewer tiles than
 // that, their keys are split so that all work; the tiles of a last turn that would be
-// at most half full, likewise, up to four turns (past that, short tiles fill the end).
-// The host knows the number of tiles to within half a tile a request. 2 requests of 128
-// tokens behind 4,000 (8 KV heads of 4) take 35 + 9 us split, 98 whole.
+// at most 0.6 full, likewise, up to four turns (past that, short tiles fill the
+// end): with a second turn 0.55 full, 178 + 10 us so and 198 whole, 0.63 full, 150 + 10
+// and 159. 2 requests of 128 tokens behind 4,000 (8 KV heads of 4) take 35 + 9 us split, 98
+// whole. The host knows the number of tiles to within half a tile a request.
 void split_prompt(AttendPlan* p, int cus) {
     const int64_t heads = p->kv.heads, slots = 2 * cus;
     const int64_t rows = p->n_tokens * p->group;
@@ -458,6 +462,7 @@ void split_prompt(AttendPlan* p, int cus) {
     else if (likely * heads < 4 * slots)
         rest = likely * heads % slots / heads;
     int64_t splits = rest ? slots / (rest * heads) : 1;
+    if (splits < 2 && rest < bound && rest * heads <= most_rest(cus)) splits = 2;
     // ten steps a part at least, where the table is full: a prompt of 1,024 tokens takes
     // 26 + 8 us in two parts, 31 whole
     const int64_t most = (int64_t)p->max_blocks * p->kv.div.page / (10 * kKeys);
@@ -469,7 +474,7 @@ void split_prompt(AttendPlan* p, int cus) {
 }
 
 int64_t prompt_workspace(const Planes& kv, int cus) {
-    return 2ll * cus * part_floats(kv.dim) * (int64_t)sizeof(float);
+    return 2ll * most_rest(cus) * part_floats(kv.dim) * (int64_t)sizeof(float);
 }
 
 hipError_t launch_prompt(const AttendPlan& p, hipStream_t s) {

@@ -330,6 +330,13 @@ def test_attention_prompt_in_parts(P, new, past):
     Case(P, "fp16", 2, 1, 64, 16, [(new, past), (90, past + 33)], seed=19).check()
 
 
+@pytest.mark.parametrize("kind", ["fp16", "mxfp4"])
+@pytest.mark.parametrize("requests", [24, 33, 40])
+def test_attention_last_turn_in_parts(P, kind, requests):
+    """More tiles than run at once: those of the last turn are split, or not."""
+    Case(P, kind, 8, 1, 64, 16, [(300, 1000)] + [(300, 7 * i) for i in range(requests - 1)], seed=22).check()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 def test_attention_large_scores(P, kind):
     """Scores in the hundreds: one key takes nearly all the weight, in either order."""
