@@ -48,7 +48,10 @@ struct Elem<true> {
     typedef _Float16 v2 __attribute__((ext_vector_type(2)));
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExpMask = 0x7C007C00u;
-    static constexpr float kRoom = 0.f;  // no sum of its values leaves a float
+    // The largest weight is 2^7, and 2^15 where a maximum may be behind (prompt.hip): the
+    // type ends at 2^16, and its smallest value is then 2^-31 of the largest weight, so that
+    // many keys of little weight each still count. No sum of its values leaves a float.
+    static constexpr float kRoom = -7.f;
     static __device__ v4f mma16(v8 a, v8 b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }

@@ -303,6 +303,37 @@ def test_attention_long(P, kind):
     Case(P, kind, 1, 4, 128, 16, [(1, 5000), (1, 3), (2, 2600)], seed=5).check()
 
 
+@pytest.mark.parametrize("kind,dim", [("bf16", 128), ("fp16", 64), ("mxfp4", 128)])
+@pytest.mark.parametrize("group,reqs", [
+    (1, [(1, 9000)]), (8, [(1, 40000)]), (16, [(1, 20000), (1, 100)]), (5, [(3, 30000)]), (8, [(4, 6000), (2, 70)])])
+def test_attention_many_parts(P, kind, dim, group, reqs):
+    """Tiles of 1 to 16 rows whose parts are joined from a few to hundreds of shares."""
+    Case(P, kind, 1, group, dim, 16, reqs, seed=23).check()
+
+
+@pytest.mark.parametrize("n", [1, 90])
+def test_attention_half_precision_tail(P, n):
+    """One key of nearly all the weight and value 0, thousands of 2^-26 of it and value 64: their
+    part of the output is kept, though a 16-bit float has no weight that small. Its steps
+    below 2^-14 are 2^-24: a weight of 2^-19 is off by 2^-6 of itself at most."""
+    past, dim, page = 3000, 64, 16
+    blocks = (past + n + page - 1) // page
+    cache = P.PagedCache(1, 1, dim, blocks, page, "fp16")
+    slots = torch.arange(blocks * page, device="cuda")
+    k = torch.zeros((blocks * page, 1, dim), dtype=torch.float16, device="cuda")
+    v = torch.full_like(k, 64.0)
+    k[0, 0, 0], v[0] = 16.0, 0.0
+    cache.append(0, k, v, slots)
+    q = torch.zeros((n, 4, dim), dtype=torch.float16, device="cuda")
+    q[..., 0] = 1.125  # 18 nats, 2^25.97
+    ctx = torch.tensor([past], dtype=torch.int32, device="cuda")
+    table = torch.arange(blocks, dtype=torch.int32, device="cuda")[None]
+    out = cache.attend(0, q, torch.tensor([0, n], device="cuda"), ctx, table, scale=1.0).double().cpu()
+    tail = torch.arange(past, past + n, dtype=torch.float64)[:, None, None]
+    want = 64 * tail / (tail + np.exp(18.0))
+    assert bool(((out - want).abs() <= (2.0 ** -6 + 2.0 ** -10) * want).all())
+
+
 @pytest.mark.parametrize("kind", ["bf16", "mxfp4"])
 def test_attention_prompts(P, kind):
     """Whole prompts and prompts behind a prefix, over several tiles of rows."""
