@@ -527,76 +527,124 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     }
 }
 
-// Joins the parts of a tile that several shares have: the workgroup of the share
-// that it begins in and the KV head, a wave a row. The wave's halves (dim 64: quarters)
-// take every other part, 4 dimensions a lane, several parts in flight. (A kernel of
-// its own: joined by the workgroup that writes the last part, which has to pass the parts
+// A row's parts so far: 4 dimensions of the output, the maximum, the sum.
+struct Joined {
+    v4f acc = {0, 0, 0, 0};
+    float all = kLowest, total = 0.f;
+    // to a maximum of at least `top`; what then weighs nothing is dropped, since 0 * infinity
+    // would count
+    __device__ void raise(float top) {
+        const float to = fmaxf(all, top), less = exp2_of(all - to);
+        total = less != 0.f ? total * less : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = less != 0.f ? acc[e] * less : 0.f;
+        all = to;
+    }
+    // a part whose maximum is not above `all`
+    __device__ void add(v4f o, float top, float sum) {
+        const float part_of = exp2_of(top - all);
+        if (part_of == 0.f) return;
+        total += part_of * sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += part_of * o[e];
+    }
+};
+
+// Joins the parts of a tile that several shares have. The workgroups of all these
+// shares but the last take the tile's rows in turn; a workgroup's waves, and each wave's
+// halves (dim 64: quarters), divide a row's parts, 4 dimensions a lane, several parts in
+// flight, so that 64 parts of a row are one trip to memory. (A kernel of its own:
+// joined by the workgroup that writes the last part, which has to pass the parts
 // through memory that all dies see, one request of 32,768 keys took 45 us, not 34.)
-// 256 parts of one request: 6.7 us.
 constexpr int kJoinWaves = 8;
 
 template <int D, bool kHalf, bool kFour>
 __global__ __launch_bounds__(kJoinWaves * 64) void k_join(AttendPlan p) {
     constexpr int kRowLanes = D / 4, kPhases = 64 / kRowLanes, kFlight = 8;
-    const int lane = threadIdx.x & 63, phase = lane / kRowLanes, c = lane % kRowLanes;
+    __shared__ v4f s_acc[kJoinWaves][kRowLanes];
+    __shared__ float s_all[kJoinWaves], s_total[kJoinWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int phase = lane / kRowLanes, c = lane % kRowLanes;
     const int head = blockIdx.x % p.kv.heads, share = blockIdx.x / p.kv.heads;
     int r;
     int64_t first;
     Work f;
     const Shares shares = find_step<kJoinWaves>(p, step_keys(kFour), share, true, r, f, first);
     if (share >= shares.count) return;
-    const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
+    const int64_t share1 = shares.begin(share + 1);
     const int tile = (int)((share1 - 1 - first) / f.steps);
     const int64_t tile0 = first + (int64_t)tile * f.steps, tile1 = tile0 + f.steps;
-    if (tile0 < share0 || tile1 <= share1) return;
-    const int parts = (int)(shares.of(tile1 - 1) - share + 1);
+    if (tile1 <= share1) return;
+    const int share0 = (int)shares.of(tile0);  // the tile's first
+    const int parts = (int)(shares.of(tile1 - 1) - share0 + 1);
     const int rows_left = f.n * p.group - tile * kDecodeRows;
     const int rows = rows_left < kDecodeRows ? rows_left : kDecodeRows;
-    // this share's second part, then the first of each following
-    const float* from = p.parts + (2 * (int64_t)blockIdx.x + 1) * part_floats(D);
+    // rows row0, row0 + parts - 1, ... are this workgroup's
+    const int row0 = share - share0;
+    if (row0 >= rows) return;
+    const int mine = (rows - row0 + parts - 2) / (parts - 1);
+    // waves a row: as many as there are, and its parts keep busy
+    int slices = mine == 1 ? 8 : mine == 2 ? 4 : mine <= 4 ? 2 : 1;
+    while (slices > 1 && slices / 2 * kPhases * kFlight >= parts) slices /= 2;
+    const int slice = wave % slices;
+    // the first share's second part, then the first of each following
+    const float* from = p.parts + (2 * ((int64_t)share0 * p.kv.heads + head) + 1) * part_floats(D);
     const int64_t next = 2ll * p.kv.heads * part_floats(D);
     auto part_at = [&](int i) { return from + i * next - (i > 0 ? part_floats(D) : 0); };
-    for (int row = threadIdx.x >> 6; row < rows; row += kJoinWaves) {
-        float all = kLowest;
-        for (int i = lane; i < parts; i += 64) all = fmaxf(all, part_at(i)[kDecodeRows * D + 2 * row]);
-        for (int d = 32; d; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
-        v4f acc = {0, 0, 0, 0};
-        float total = 0.f;
-        for (int i0 = phase; i0 < parts; i0 += kPhases * kFlight) {
+    for (int at = 0; at < mine; at += kJoinWaves / slices) {
+        const int row = row0 + (at + wave / slices) * (parts - 1);
+        Joined sum;
+        for (int i0 = slice * kPhases + phase; i0 < parts && row < rows; i0 += slices * kPhases * kFlight) {
             v4f o[kFlight];
             v2f ms[kFlight];
+            float top = kLowest;
 #pragma unroll
             for (int u = 0; u < kFlight; ++u) {
-                const int i = i0 + u * kPhases;
+                const int i = i0 + u * slices * kPhases;
                 const float* part = part_at(i < parts ? i : i0);
                 o[u] = *(const v4f*)(part + row * D + c * 4);
                 ms[u] = *(const v2f*)(part + kDecodeRows * D + 2 * row);
                 if (i >= parts) ms[u][0] = -INFINITY;
             }
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) {
-                const float part_of = exp2_of(ms[u][0] - all);
-                if (part_of == 0.f) continue;  // nothing of it counts, and 0 * infinity would
-                total += part_of * ms[u][1];
+            for (int u = 0; u < kFlight; ++u) top = fmaxf(top, ms[u][0]);
+            sum.raise(top);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += part_of * o[u][e];
-            }
+            for (int u = 0; u < kFlight; ++u) sum.add(o[u], ms[u][0], ms[u][1]);
         }
         for (int d = kRowLanes; d < 64; d <<= 1) {
-            total += __shfl_xor(total, d);
+            v4f o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
+            for (int e = 0; e < 4; ++e) o[e] = __shfl_xor(sum.acc[e], d);
+            const float top = __shfl_xor(sum.all, d), total = __shfl_xor(sum.total, d);
+            sum.raise(top);
+            sum.add(o, top, total);
         }
-        if (phase) continue;
+        if (slices > 1) {
+            __syncthreads();
+            if (phase == 0) s_acc[wave][c] = sum.acc;
+            if (lane == 0) {
+                s_all[wave] = sum.all;
+                s_total[wave] = sum.total;
+            }
+            __syncthreads();
+            if (slice == 0)
+                for (int u = 1; u < slices; ++u) {
+                    sum.raise(s_all[wave + u]);
+                    sum.add(s_acc[wave + u][c], s_all[wave + u], s_total[wave + u]);
+                }
+        }
+        if (slice || phase || row >= rows) continue;
         const int out_row = tile * kDecodeRows + row;
         const int ot = out_row / p.group, os = out_row - ot * p.group;
         const int64_t oh = (int64_t)head * p.group + os;
-        const float inv = total != 0.f ? 1.f / total : 0.f;
-        const v2u x = {pack2<kHalf>(acc[0] * inv, acc[1] * inv), pack2<kHalf>(acc[2] * inv, acc[3] * inv)};
+        const float total = sum.total, inv = total != 0.f ? 1.f / total : 0.f;
+        const v2u x = {pack2<kHalf>(sum.acc[0] * inv, sum.acc[1] * inv),
+                       pack2<kHalf>(sum.acc[2] * inv, sum.acc[3] * inv)};
         *(v2u*)((uint8_t*)p.out.p + ((f.begin + ot) * p.out.token + oh * p.out.head + c * 4) * 2) = x;
         if (p.lse && c == 0)
             p.lse[(f.begin + ot) * p.q_heads + oh] =
-                total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+                total != 0.f ? (sum.all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
     }
 }
 
