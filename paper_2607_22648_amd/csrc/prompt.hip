@@ -244,13 +244,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
         const int32_t at = t * kKeys;
         v16f s[2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i)
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
                 s[c] = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(km + k_read[i] + c * 32 * kRow)), q[i], s[c]);
-        }
         if (t + 1 < steps) store(std::integral_constant<int, buf ^ 1>{}, ok_next, t + 1);
         const uint64_t ok_now = ok;
         ok = ok_next;
