@@ -422,21 +422,29 @@ def ptstore_kv_slab_bytes(kind: int, kv_heads: int, head_dim: int, block_tokens:
     return n.value
 
 
-def ptstore_block_tables(offsets, context, held, block_tokens, free_blocks, first, block_table, slots,
-                         positions, held_out, next_free, stream=None) -> None:
-    """n_tokens is the length of `slots`; `held`, `first` and `positions` may be None."""
-    R, maxb = _table(offsets, block_table)
-    n, i32, i64 = slots.numel(), torch.int32, torch.int64
+def _block_tables(R, maxb, offsets, context, held, block_tokens, free_blocks, first, block_table, n, outputs,
+                  stream) -> None:
+    """outputs: the addresses of slots, positions, held_out and next_free."""
+    i32, i64 = torch.int32, torch.int64
     rc = _lib.ptstore_block_tables(
         _arg(offsets, i64, R + 1, "offsets"), n, _arg(context, i32, R, "context"),
         None if held is None else _arg(held, i32, R, "held"), R, maxb, block_tokens,
         _arg(free_blocks, i32, 0, "free_blocks"), free_blocks.numel(),
         None if first is None else _arg(first, i64, 1, "first"),
-        _arg(block_table, i32, 0, "block_table"), _arg(slots, i64, 0, "slots"),
-        None if positions is None else _arg(positions, i32, n, "positions"),
-        _arg(held_out, i32, R, "held_out"), _arg(next_free, i64, 1, "next_free"), _stream(stream))
+        _arg(block_table, i32, 0, "block_table"), *outputs, _stream(stream))
     if rc:
         _check("ptstore_block_tables", rc)
+
+
+def ptstore_block_tables(offsets, context, held, block_tokens, free_blocks, first, block_table, slots,
+                         positions, held_out, next_free, stream=None) -> None:
+    """n_tokens is the length of `slots`; `held`, `first` and `positions` may be None."""
+    R, maxb = _table(offsets, block_table)
+    n, i32, i64 = slots.numel(), torch.int32, torch.int64
+    outputs = (_arg(slots, i64, 0, "slots"), None if positions is None else _arg(positions, i32, n, "positions"),
+               _arg(held_out, i32, R, "held_out"), _arg(next_free, i64, 1, "next_free"))
+    _block_tables(R, maxb, offsets, context, held, block_tokens, free_blocks, first, block_table, n, outputs,
+                  stream)
 
 
 _KV_DTYPES = {PTSTORE_KV_BF16: torch.bfloat16, PTSTORE_KV_FP16: torch.float16,
@@ -802,11 +810,14 @@ class PagedCache:
                stream=None):
         """Give the batch's requests their blocks: fills the new entries of `block_table` and
         returns (slots, positions, held after, next free entry)."""
+        R, maxb = _table(offsets, block_table)
         with self._on(stream):
             slots, next_free = offsets.new_empty(n_tokens), offsets.new_empty(1)
-            positions, held_out = context.new_empty(n_tokens), context.new_empty(block_table.shape[0])
-        ptstore_block_tables(offsets, context, held, self.block_tokens, free_blocks, first, block_table,
-                             slots, positions, held_out, next_free, stream)
+            positions, held_out = context.new_empty(n_tokens), context.new_empty(R)
+        # offsets and context are checked to be int64 and int32 arrays on the device: so are these
+        _block_tables(R, maxb, offsets, context, held, self.block_tokens, free_blocks, first, block_table,
+                      n_tokens, (slots.data_ptr(), positions.data_ptr(), held_out.data_ptr(),
+                                 next_free.data_ptr()), stream)
         return slots, positions, held_out, next_free
 
     def append(self, layer: int, k, v, slots, stream=None) -> None:
@@ -816,10 +827,15 @@ class PagedCache:
     def read(self, layer: int, slots, stream=None):
         """The K and V that `slots` of a layer hold, [tokens, kv_heads, head_dim] each."""
         kv = self._planes[layer]
+        n, heads, dim = slots.numel(), kv.kv_heads, kv.head_dim
         with self._on(stream):
-            k, v = (torch.empty((slots.numel(), kv.kv_heads, kv.head_dim), dtype=self.dtype,
-                                device=slots.device) for _ in range(2))
-        ptstore_kv_read(kv, k, v, slots, stream)
+            k = slots.new_empty((n, heads, dim), dtype=self.dtype)
+            v = slots.new_empty((n, heads, dim), dtype=self.dtype)
+        row = heads * dim
+        rc = _lib.ptstore_kv_read(C.byref(kv), k.data_ptr(), row, dim, v.data_ptr(), row, dim,
+                                  _arg(slots, torch.int64, n, "slots"), n, _stream(stream))
+        if rc:
+            _check("ptstore_kv_read", rc)
         return k, v
 
     def attend(self, layer: int, q, offsets, context, block_table, scale: Optional[float] = None, out=None,
