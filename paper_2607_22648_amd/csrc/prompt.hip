@@ -16,9 +16,10 @@
 // wants them (see attend.hpp), and V is read from LDS transposed. Two workgroups share a
 // compute unit, so that one's exponentials run beside the other's products.
 //
-// 8 KV heads of 4 query heads, dim 128: a prompt of 8,192 tokens 593 to 650 us by the
-// machine's clock under this load (1.9 to 2.0 GHz), 850 to 930 TFLOP/s; from 4-bit
-// pages 547 to 615; dim 64 347 to 366. A large library product reaches 1,350; here the
+// 8 KV heads of 4 query heads, dim 128: a prompt of 8,192 tokens 586 to 650 us by the
+// machine's clock under this load (1.9 to 2.0 GHz), 850 to 940 TFLOP/s; fp16 626, from 4-bit
+// pages 540 to 615, values of zero 500: the same instructions at other power; dim 64
+// 345 to 366. A large library product reaches 1,350; here the
 // matrix units work in 43 % of the cycles, the vector units in about 40 % (a third of it
 // exponentials), LDS in 35 %: two waves overlap little of the two.
 #include <type_traits>
