@@ -543,7 +543,9 @@ int ptstore_kv_read(const ptstore_kv_t *kv, void *k, int64_t k_token_stride, int
  *   lse[t][h] = log(sum_j w_j).
  * A row that sees no key, or only keys of weight zero (scores of minus
  * infinity), gets zeros and minus infinity. What lies in keys a row does not see,
- * NaN included, never reaches it. One token a request, whole prompts, prompts
+ * NaN included, never reaches it; of those it sees, a score that is NaN makes the row and
+ * its lse NaN, and a value that is not finite makes that element of the row infinite or NaN,
+ * however little its key weighs. One token a request, whole prompts, prompts
  * behind a loaded prefix and mixes of them are all this call. Products take
  * 16-bit factors and sum in 32 bits; maxima, sums and the output are kept in 32
  * bits until they are written. The same inputs give the same bits.

@@ -531,19 +531,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 struct Joined {
     v4f acc = {0, 0, 0, 0};
     float all = kLowest, total = 0.f;
-    // to a maximum of at least `top`; what then weighs nothing is dropped, since 0 * infinity
-    // would count
+    // To a maximum of at least `top`. Sums that then weigh nothing stay in as zeros, and as NaN
+    // where they are not finite: a part whose scores are all NaN has the lowest maximum.
     __device__ void raise(float top) {
         const float to = fmaxf(all, top), less = exp2_of(all - to);
-        total = less != 0.f ? total * less : 0.f;
+        total *= less;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = less != 0.f ? acc[e] * less : 0.f;
+        for (int e = 0; e < 4; ++e) acc[e] *= less;
         all = to;
     }
     // a part whose maximum is not above `all`
     __device__ void add(v4f o, float top, float sum) {
         const float part_of = exp2_of(top - all);
-        if (part_of == 0.f) return;
         total += part_of * sum;
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += part_of * o[e];
@@ -604,7 +603,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_join(AttendPlan p) {
                 const float* part = part_at(i < parts ? i : i0);
                 o[u] = *(const v4f*)(part + row * D + c * 4);
                 ms[u] = *(const v2f*)(part + kDecodeRows * D + 2 * row);
-                if (i >= parts) ms[u][0] = -INFINITY;
+                if (i >= parts) {
+                    o[u] = v4f{0, 0, 0, 0};
+                    ms[u] = v2f{-INFINITY, 0.f};
+                }
             }
 #pragma unroll
             for (int u = 0; u < kFlight; ++u) top = fmaxf(top, ms[u][0]);

@@ -405,7 +405,6 @@ __global__ __launch_bounds__(kJoinRows* D / 8) void k_prompt_join(AttendPlan p) 
         const v4f a = *(const v4f*)(part + (2 * c * kPromptRows + r) * 4);
         const v4f b = *(const v4f*)(part + ((2 * c + 1) * kPromptRows + r) * 4);
         const float part_of = exp2_of(ms[0] - all);
-        if (part_of == 0.f) continue;  // nothing of it counts, and 0 * infinity would
         total += part_of * ms[1];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
