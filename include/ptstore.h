@@ -492,7 +492,7 @@ int ptstore_kv_slab_bytes(int32_t kind, int32_t kv_heads, int32_t head_dim, int3
  * in use (held NULL: none), and offsets[r+1] - offsets[r] new tokens. It needs
  * ceil((context[r] + new) / block_tokens) blocks, at most max_blocks; those
  * beyond held[r] are taken, requests in order, from free_blocks[*first],
- * free_blocks[*first + 1], ... (first NULL: 0) up to free_blocks[n_free - 1], and
+ * free_blocks[*first + 1], ... (first NULL, or *first negative: 0) up to free_blocks[n_free - 1], and
  * written to its row; an entry for which no free block is left gets -1. Other
  * entries are not touched. held_out[r] = held[r] plus the blocks it got; *next =
  * *first plus all that were taken. Token t of request r is at position

@@ -115,13 +115,15 @@ __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
     if (first < 0) first = 0;
     const int64_t avail = p.n_free > first ? p.n_free - first : 0;
     const int32_t total = s_want[nr];
-    const int64_t base = first + before;
+    // of them this chunk's wants get the first `left`: `first` may be any number, so it is added
+    // only for those
+    const int64_t left = avail - before;
 
     if (part == 0) {
         for (int l = tid; l < nr; l += kThreads) {
-            const int64_t left = avail - before - s_want[l];
+            const int64_t rest = left - s_want[l];
             const int32_t w = s_want[l + 1] - s_want[l];
-            const int64_t given = left < 0 ? 0 : (left < w ? left : w);
+            const int64_t given = rest < 0 ? 0 : (rest < w ? rest : w);
             p.held_out[r0 + l] = s_held[l] + (int32_t)given;
         }
         if (tid == 0 && r0 + nr == p.R) {
@@ -140,9 +142,8 @@ __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
             else
                 hi = mid - 1;
         }
-        const int64_t at_free = base + e;
         p.table[(int64_t)(r0 + lo) * p.max_blocks + s_held[lo] + (e - s_want[lo])] =
-            at_free < p.n_free ? p.free_blocks[at_free] : -1;
+            e < left ? p.free_blocks[first + before + e] : -1;
     }
 
     // tokens of the chunk: [the first request's first, the next chunk's first);
@@ -182,8 +183,8 @@ __global__ __launch_bounds__(kThreads) void k_tables(TablesPlan p, int parts) {
             if ((int32_t)b < s_held[lo]) {
                 entry = p.table[(int64_t)(r0 + lo) * p.max_blocks + b];
             } else {
-                const int64_t at_free = base + s_want[lo] + ((int32_t)b - s_held[lo]);
-                entry = at_free < p.n_free ? p.free_blocks[at_free] : -1;
+                const int32_t e = s_want[lo] + ((int32_t)b - s_held[lo]);
+                entry = e < left ? p.free_blocks[first + before + e] : -1;
             }
             if (entry >= 0) slot[i] = entry * p.div.page + ((uint32_t)at_pos - b * p.div.page);
         }
