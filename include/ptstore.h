@@ -568,7 +568,8 @@ typedef struct {
     int32_t q_heads;            /* a multiple of kv.kv_heads */
     float scale;                /* positive, usually 1 / sqrt(head_dim) */
     void *workspace;            /* need not be cleared; calls that overlap in time need one
-                                   each */
+                                   each, and so do host threads that call at once, on one
+                                   stream too: a call's kernels must not mix with another's */
     int64_t workspace_bytes;
 } ptstore_attention_t;
 

@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import threading
 from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple, Union
 
@@ -748,7 +749,8 @@ class PagedCache:
     operators on it. ``data`` is what the store's loads and ``scatter`` take; a store
     for its blocks is made with ``shape``. ``kv_heads`` is a number, or one per layer.
 
-    Outputs and workspaces that a call makes are made for the stream it runs on."""
+    Outputs and workspaces that a call makes are made for the stream it runs on. Several host
+    threads may use one cache."""
 
     def __init__(self, layers: int, kv_heads: Union[int, Sequence[int]], head_dim: int, cache_blocks: int,
                  block_tokens: int = 16, kind: str = "bf16", data: Optional[torch.Tensor] = None,
@@ -772,6 +774,7 @@ class PagedCache:
         self.data = data
         self.dtype = _KV_DTYPES[_KV_KINDS[kind]]
         self._workspaces = {}
+        self._turn = threading.Lock()
         self._scale = head_dim ** -0.5
         self._planes = []
         at = data.data_ptr()
@@ -794,7 +797,7 @@ class PagedCache:
         return torch.cuda.stream(stream)
 
     def _workspace(self, stream, handle: int) -> torch.Tensor:
-        """The workspace of a stream: one serves every layer, and the calls on it in turn.
+        """The workspace of a stream: one serves every layer, and the calls on it in turn (_turn).
         A graph, which may be replayed on any stream, gets its own."""
         with self._on(stream):
             graph = torch.cuda.is_current_stream_capturing()
@@ -845,8 +848,6 @@ class PagedCache:
         instead of the one that the cache keeps for the stream."""
         kv = self._planes[layer]
         handle = _stream(stream)
-        if workspace is None:
-            workspace = self._workspace(stream, handle)
         if q.dim() != 3:
             raise ValueError(f"q must be [tokens, heads, head_dim], got shape {tuple(q.shape)}")
         n, heads, dim = q.shape
@@ -854,12 +855,17 @@ class PagedCache:
         with self._on(stream):
             sums = q.new_empty((n, heads), dtype=torch.float32) if lse else None
             made = q.new_empty((n, heads, dim)) if out is None else None
-        if made is None:
-            ptstore_attention(kv, q, out, sums, offsets, context, block_table, scale, workspace, handle)
-        else:  # contiguous, and of the right shape and place
-            out = made
-            _attention(kv, q, (out.data_ptr(), heads * dim, dim), sums.data_ptr() if lse else None, offsets,
-                       context, block_table, scale, workspace, handle)
+        # An attention is several kernels that hand parts on in the workspace, and the library's call
+        # lets other host threads run: those of two threads on one stream must not mix.
+        with self._turn if workspace is None else _CURRENT:
+            if workspace is None:
+                workspace = self._workspace(stream, handle)
+            if made is None:
+                ptstore_attention(kv, q, out, sums, offsets, context, block_table, scale, workspace, handle)
+            else:  # contiguous, and of the right shape and place
+                out = made
+                _attention(kv, q, (out.data_ptr(), heads * dim, dim), sums.data_ptr() if lse else None,
+                           offsets, context, block_table, scale, workspace, handle)
         return (out, sums) if lse else out
 
 
