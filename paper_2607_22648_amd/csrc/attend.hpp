@@ -121,9 +121,23 @@ __device__ inline void together(uint32_t (&x)[8]) {
                  "+v"(x[7]));
 }
 
-// Lowest score kept: what a row starts from instead of minus infinity, so that
-// the differences of two such rows stay numbers.
-constexpr float kLowest = -3.0e38f;
+// Lowest score kept, a float's lowest number: what a row starts from instead of minus
+// infinity, so that the differences of two such rows stay numbers.
+constexpr float kLowest = -0x1.fffffep127f;
+
+// A weight is 2^(score * scale - maximum), one fused operation whose product is exact, while
+// the maximum is a rounded product. Where a float's steps are large, the difference of the
+// two is no small number even for the largest score: at 2^31, up to 2^7, and its weight
+// leaves the type. So from a maximum 2^20 away from zero on (a step is then 2^-3) a wave
+// rounds the scaled scores first, each by itself, and a maximum is one of them.
+constexpr float kFar = 0x1p20f;
+__device__ inline bool is_far(float top) { return __builtin_fabsf(top) > kFar && top > kLowest; }
+
+// A product that is rounded, whatever sum it enters.
+__device__ inline float product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 

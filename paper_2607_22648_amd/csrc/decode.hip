@@ -235,6 +235,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i] = v4f{0, 0, 0, 0};
     float top = kLowest, sum = 0.f;
+    bool far = false;  // scores are scaled before the maximum is taken
 
     // K row of this lane within a row group: key_of_row
     const int key_of_row = 8 * (n >> 2) + (n & 3);
@@ -391,20 +392,34 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, s[g][i]);
         most = larger_16_32(most);
-        const float top2 = fmaxf(top, __builtin_fmaf(most, p.scale2, E::kRoom));
+        auto scale_now = [&] {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[g][i] = product(s[g][i], p.scale2);
+            most = product(most, p.scale2);
+        };
+        if (far) scale_now();
+        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, E::kRoom));
         if (__any(top2 > top)) {
+            if (!far && __any(is_far(top2))) {
+                far = true;
+                scale_now();
+                top2 = fmaxf(top, most + E::kRoom);
+            }
             const float less = exp2_of(top - top2);
             sum *= less;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[i] *= less;
             top = top2;
         }
+        const float scale = far ? 1.f : p.scale2;
         v4u w[kKeys / 32];
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[g][i] = exp2_of(__builtin_fmaf(s[g][i], p.scale2, -top));
+                s[g][i] = exp2_of(__builtin_fmaf(s[g][i], scale, -top));
                 sum += s[g][i];
             }
             // weights enter the second product as 16-bit values, as V does: the error

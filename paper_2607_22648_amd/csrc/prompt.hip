@@ -120,6 +120,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float top = kLowest, sum = 0.f;
+    bool far = false;  // scores are scaled before the maximum is taken
 
     // a step's keys, one a lane; rows 16 wave .. + 15 are this wave's to load
     v4u kreg[kLoads], vreg[kLoads];
@@ -283,8 +284,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
         most = larger_32(most);
-        const float top2 = fmaxf(top, __builtin_fmaf(most, p.scale2, E::kRoom));
-        if (__any(top2 > top + kBehind)) {
+        auto scale_now = [&] {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[c][e] = product(s[c][e], p.scale2);
+            most = product(most, p.scale2);
+        };
+        if (far) scale_now();
+        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, E::kRoom));
+        // (far away, steps of the maximum can be 8 themselves: none is kept behind)
+        if (__any(top2 > top + (far ? 0.f : kBehind))) {
+            if (!far && __any(is_far(top2))) {
+                far = true;
+                scale_now();
+                top2 = fmaxf(top, most + E::kRoom);
+            }
             const float less = exp2_of(top - top2);
             sum *= less;
 #pragma unroll
@@ -293,12 +308,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                 for (int e = 0; e < 16; ++e) o[i][e] *= less;
             top = top2;
         }
+        const float scale = far ? 1.f : p.scale2;
         v4u w[4];  // weights of 16 keys each
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[c][e] = exp2_of(__builtin_fmaf(s[c][e], p.scale2, -top));
+                s[c][e] = exp2_of(__builtin_fmaf(s[c][e], scale, -top));
                 sum += s[c][e];
             }
             // weights enter the second product as 16-bit values, as V does: the error
