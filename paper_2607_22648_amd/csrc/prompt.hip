@@ -50,9 +50,12 @@ __device__ inline int turn_v(int row) {
 }
 
 // A running maximum that is behind by up to this much (in powers of two) is kept:
-// weights then reach 2^8 times the largest otherwise, which no type here minds, and the
-// output is rescaled a few times a row instead of at every new maximum.
+// weights then reach 2^8 times the largest otherwise, and the output is rescaled a few
+// times a row instead of at every new maximum. fp16 weights have the room for it; bf16 ones
+// start that much lower, so that their sums stay in a float all the same.
 constexpr float kBehind = 8.f;
+template <bool kHalf>
+constexpr float kRoom = Elem<kHalf>::kRoom + (kHalf ? 0.f : kBehind);
 
 constexpr int kMostParts = 16;  // of a tile
 
@@ -292,13 +295,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
             most = product(most, p.scale2);
         };
         if (far) scale_now();
-        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, E::kRoom));
+        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, kRoom<kHalf>));
         // (far away, steps of the maximum can be 8 themselves: none is kept behind)
         if (__any(top2 > top + (far ? 0.f : kBehind))) {
             if (!far && __any(is_far(top2))) {
                 far = true;
                 scale_now();
-                top2 = fmaxf(top, most + E::kRoom);
+                top2 = fmaxf(top, most + kRoom<kHalf>);
             }
             const float less = exp2_of(top - top2);
             sum *= less;

@@ -1,4 +1,4 @@
-"""Attention where scores are as large as their types allow (MI355X)."""
+"""Attention where scores, or sums of values, are as large as their types allow (MI355X)."""
 from __future__ import annotations
 
 import math
@@ -17,18 +17,19 @@ def P():
     return ptstore
 
 
-@pytest.mark.parametrize("kind", ["bf16", "fp16", "mxfp4"])
+SIZES = [2.0 ** 21, 2.0 ** 25, 1.5e9, 2.0 ** 60, 3.3e38]  # the last two are past fp16's products
+
+
+@pytest.mark.parametrize("kind,size", [(k, x) for x in SIZES for k in ("bf16", "fp16", "mxfp4")
+                                       if k != "fp16" or x < 2e9])
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("n,past", [(1, 40), (1, 3000), (90, 10), (40, 2100)])
-@pytest.mark.parametrize("size", [2.0 ** 21, 2.0 ** 25, 1.5e9, 2.0 ** 60, 3.3e38])
 @pytest.mark.parametrize("sign", [1, -1])
 def test_scores_far_from_zero(P, kind, dim, n, past, size, sign):
     """Scores of `size` in powers of two, where a float's steps are larger than the differences that
     matter to an exponential. Only a key's first dimension is not zero, so that a score is one exact
     product, and those that are not equal are hundreds apart: a row's output is the mean of the
     values of its largest score's keys, its logarithm that score."""
-    if kind == "fp16" and size > 2e9:
-        pytest.skip("past the products of fp16 values")
     page, scale = 16, 0.95
     size /= 1.3706  # scale in powers of two
     g = torch.Generator().manual_seed(n + past)
@@ -59,3 +60,26 @@ def test_scores_far_from_zero(P, kind, dim, n, past, size, sign):
     assert bool(((out.double().cpu() - want).abs() <= (u + 2.0 ** -16) * mean + u * want.abs() + 2.0 ** -24).all())
     near = most[..., 0] + tied.sum(-1).log()
     assert bool(((lse.double().cpu() - near).abs() <= 2.0 ** -21 * near.abs()).all())
+
+
+def test_sums_of_the_largest_values(P):
+    """2^28 keys, whose values' sum leaves a float unless weights are small: each sixteenth of them
+    begins with a page of scores 2^8 below the rest. All values are alike, and so is the output."""
+    page, dim, n = 64, 64, 40
+    pages = 1 << 22
+    cache = P.PagedCache(1, 1, dim, 2, page, "bf16")
+    k = torch.zeros((2 * page, 1, dim), dtype=torch.bfloat16, device="cuda")
+    k[:page, 0, 0] = 8.0
+    value = 1.5 * 2.0 ** 127
+    cache.append(0, k, torch.full_like(k, value), torch.arange(2 * page, device="cuda"))
+    table = torch.zeros((1, pages), dtype=torch.int32, device="cuda")
+    table[0, torch.arange(16) * (pages // 16)] = 1
+    q = torch.zeros((n, 1, dim), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    out, lse = cache.attend(0, q, torch.tensor([0, n], device="cuda"),
+                            torch.tensor([pages * page - n], dtype=torch.int32, device="cuda"), table,
+                            scale=0.6931472, lse=True)
+    # the sum of 2^20 equal steps of a part in 32 bits, then the output's rounding
+    assert bool(((out.double() / value - 1).abs() <= 2.0 ** -4 + 2.0 ** -8).all())
+    want = math.log((pages - 16.0) * page * 2.0 ** 8 + 16.0 * page)
+    assert bool(((lse.double() - want).abs() <= 2.0 ** -4).all())
