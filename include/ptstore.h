@@ -520,7 +520,8 @@ int ptstore_block_tables(const int64_t *offsets, int64_t n_tokens, const int32_t
  * which their largest magnitude is at most 7 * 2^e (-126 <= e <= 125), and each the
  * level nearest to its magnitude / 2^e, ties to the even code, above 6 to 6; a
  * group that holds an infinity or a NaN reads as NaN.
- * Errors: INVALID, HIP.
+ * Errors: INVALID (a cache or strides other than stated; n_tokens * kv_heads * head_dim >
+ * 2^35 - 2^11), HIP.
  */
 int ptstore_kv_append(const ptstore_kv_t *kv, const void *k, int64_t k_token_stride,
                       int64_t k_head_stride, const void *v, int64_t v_token_stride,
@@ -580,8 +581,10 @@ typedef struct {
 int ptstore_attention_workspace(const ptstore_kv_t *kv, int64_t *bytes);
 
 /* Errors: INVALID (shapes, sizes, strides or alignment as stated; max_blocks *
- * block_tokens > 2^30; n_tokens * q_heads >= 2^31; no cache blocks; a workspace too
- * small), HIP. */
+ * block_tokens > 2^30; n_tokens * q_heads > 2^31 - 128; 2^23 KV heads or more; prompts
+ * (over 32 rows a KV head and request on average, or a table of 8,192 keys) with
+ * (n_tokens * q_heads / 128 + R * kv_heads) > 2^24 - 2^13; no cache blocks; a workspace
+ * too small), HIP. */
 int ptstore_attention(const ptstore_attention_t *args, void *stream);
 
 /* ======================================================================

@@ -20,7 +20,10 @@ namespace {
 
 constexpr int64_t kMaxEntries = 1ll << 29;  // (request, block) entries of a call
 constexpr int64_t kMaxKeys = 1ll << 30;     // keys of a request: block-table columns * page size
-constexpr int64_t kMaxGrid = 1ll << 31;
+constexpr int64_t kMaxItems = 1ll << 32;    // work-items of a launch, fewer than that
+constexpr int64_t kMaxUnits = kMaxItems / 256 - 8192;  // (tile, KV head) pairs of prompt.hip, and room for
+                                                       // parts of the last ones
+constexpr int64_t kMaxHeads = kMaxItems / 512;         // decode.hip: a workgroup a head at least, 512 threads
 
 int refuse(const char* what) { return set_last_error(PTSTORE_ERR_INVALID, what); }
 
@@ -114,14 +117,18 @@ const char* sized(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int
         (R == 0 && n_tokens > 0))
         return "R, max_blocks or n_tokens out of range";
     if ((int64_t)max_blocks * kv->block_tokens > kMaxKeys) return "max_blocks * block_tokens exceeds 2^30";
-    // rows are numbered in 32 bits
-    if (n_tokens >= (1ll << 31) || n_tokens * q_heads >= (1ll << 31)) return "n_tokens * q_heads exceeds 2^31";
+    if (kv->kv_heads >= kMaxHeads) return "too many heads for one call (2^23 or more)";
+    // rows are numbered in 32 bits, up to the end of a last tile
+    constexpr int64_t most = (1ll << 31) - kPromptRows;
+    if (n_tokens > most || n_tokens * q_heads > most) return "n_tokens * q_heads exceeds 2^31 - 128";
     p->n_tokens = n_tokens;
     p->R = R;
     p->max_blocks = max_blocks;
     p->q_heads = q_heads;
     p->group = q_heads / kv->kv_heads;
-    if (tile_bound(n_tokens, p->group, R, kDecodeRows) * kv->kv_heads >= kMaxGrid)
+    const bool prompts = many_rows(*p);
+    if ((prompts || mixed(*p, prompts)) &&
+        tile_bound(n_tokens, p->group, R, kPromptRows) * kv->kv_heads > kMaxUnits)
         return "too many tiles for one call";
     return nullptr;
 }
@@ -171,7 +178,9 @@ static int move_rows(const char* call, const ptstore_kv_t* kv, const void* k, in
                      bool read, void* stream) {
     Planes pl;
     if (const char* bad = planes_of(kv, &pl)) return refuse_as(call, bad);
-    if (n < 0 || n * (int64_t)pl.heads >= (1ll << 31)) return refuse_as(call, "n_tokens * heads out of range");
+    // a work-item moves 8 elements; the last workgroup may be partly filled
+    if (n < 0 || n > (kMaxItems - 256) / (pl.dim / 8) / pl.heads)
+        return refuse_as(call, "n_tokens * kv_heads * head_dim exceeds 2^35 - 2^11");
     if (n == 0) return PTSTORE_OK;
     if (!slots || !rows_ok(k, k_token, k_head) || !rows_ok(v, v_token, v_head))
         return refuse_as(call, "null argument, or rows of k or v not 16-byte aligned");
