@@ -226,6 +226,8 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
     if (!rows_ok(a->q, a->q_token_stride, a->q_head_stride) ||
         !rows_ok(a->out, a->out_token_stride, a->out_head_stride))
         return refuse("ptstore_attention: rows of q or out null or not 16-byte aligned");
+    // no order is promised between a row's output and the reads of other rows' queries
+    if (a->out == a->q) return refuse("ptstore_attention: out must not be q");
     if (p.kv.blocks < 1) return refuse("ptstore_attention: the cache has no blocks");
     int cus = 0;
     if (const int rc = compute_units(&cus)) return rc;
