@@ -13,8 +13,9 @@
 //
 // Both are bound by memory: 2 bytes read and 2 (or 17/32) written an element. 16,384
 // tokens of 8 heads of 128 take 22.6 to 24.6 us, 5.5 TB/s of the 5.7 that a plain copy
-// reaches; 8,200 into 4 bits 7.6 to 9.5, and out of them 9.3 to 9.9 (42 MB, 4.5 TB/s:
-// a launch this short does not reach the full rate).
+// reaches, and back out in the same time (21.9 and 21.5 us in a graph); 8,200 into 4 bits 7.6
+// to 9.5, and out of them 8.6 to 9.9 (42 MB, 4.5 TB/s: a launch this short does not reach the
+// full rate).
 #include <hip/hip_runtime.h>
 
 #include "paged.hpp"

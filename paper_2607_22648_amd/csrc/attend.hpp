@@ -32,8 +32,9 @@ struct Elem<false> {
     typedef __bf16 v2 __attribute__((ext_vector_type(2)));
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExpMask = 0x7F807F80u;  // all ones: infinity or NaN
-    // The largest weight is 2^-kRoom, so that sums of 2^30 values near the type's
-    // largest, 2^128, stay in a float. Weights keep their bits: bf16 has a float's range.
+    // The largest weight is 2^-kRoom (prompt.hip: where a maximum is behind), so that sums of
+    // 2^30 values near the type's largest, 2^128, stay in a float. Weights keep their bits: bf16
+    // has a float's range.
     static constexpr float kRoom = 31.f;
     static __device__ v4f mma16(v8 a, v8 b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

@@ -422,8 +422,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 s[g][i] = exp2_of(__builtin_fmaf(s[g][i], scale, -top));
                 sum += s[g][i];
             }
-            // weights enter the second product as 16-bit values, as V does: the error
-            // of a weight is below the output's own rounding and averages over the keys
+            // Weights enter the second product as 16-bit values, as V does; the sum takes them
+            // as they are. Each is off by half a step of the type at most, as much as the
+            // output's own rounding adds; over many keys the errors average out, and the largest
+            // weight of a row, a power of two, has next to none.
             w[g >> 1][2 * (g & 1)] = pack2<kHalf>(s[g][0], s[g][1]);
             w[g >> 1][2 * (g & 1) + 1] = pack2<kHalf>(s[g][2], s[g][3]);
         }

@@ -96,7 +96,9 @@ bool many_rows(const AttendPlan& p) { return p.n_tokens * p.group > (int64_t)32 
 // 4,000, take 745 us by both and 905 by the former. The launches that may find nothing to
 // do cost 5 to 9 us (64 drafts of 4 tokens: 170 us, 162), so it takes room for 8,192 keys
 // and, in a batch of few rows a request, kManyRows beyond a token each: at 508 of them
-// both ways take the same time (256 single tokens and 128 of one request, 720 us).
+// both ways take the same time (256 single tokens and 128 of one request, 720 us). The room
+// is the table's, not the requests': in a wide table every batch of several prompts pays for
+// the launches (4 prompts of 256 tokens take 19.1 us beside 14.2 in a tight one).
 constexpr int64_t kManyRows = 512;
 bool mixed(const AttendPlan& p, bool prompts) {
     return p.R > 1 && (int64_t)p.max_blocks * p.kv.div.page >= 8192 &&

@@ -16,10 +16,10 @@
 // wants them (see attend.hpp), and V is read from LDS transposed. Two workgroups share a
 // compute unit, so that one's exponentials run beside the other's products.
 //
-// 8 KV heads of 4 query heads, dim 128: a prompt of 8,192 tokens 586 to 650 us by the
-// machine's clock under this load (1.9 to 2.0 GHz), 850 to 940 TFLOP/s; fp16 626, from 4-bit
-// pages 540 to 615, values of zero 500: the same instructions at other power; dim 64
-// 345 to 366. A large library product reaches 1,350; here the
+// 8 KV heads of 4 query heads, dim 128: a prompt of 8,192 tokens 582 to 650 us by the
+// machine's clock under this load (1.9 to 2.0 GHz), 850 to 940 TFLOP/s; fp16 616 to 626, from
+// 4-bit pages 530 to 615, values of zero 505: the same instructions at other power; dim 64
+// 340 to 366. A large library product reaches 1,350; here the
 // matrix units work in 43 % of the cycles, the vector units in about 40 % (a third of it
 // exponentials), LDS in 35 %: two waves overlap little of the two.
 #include <type_traits>
@@ -320,8 +320,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendPlan p) {
                 s[c][e] = exp2_of(__builtin_fmaf(s[c][e], scale, -top));
                 sum += s[c][e];
             }
-            // weights enter the second product as 16-bit values, as V does: the error
-            // of a weight is below the output's own rounding and averages over the keys
+            // Weights enter the second product as 16-bit values, as V does; the sum takes them
+            // as they are. Each is off by half a step of the type at most, as much as the
+            // output's own rounding adds. Over many keys the errors average out; where one key has
+            // nearly all the weight and the maximum is behind, they do not.
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
@@ -484,8 +486,14 @@ void split_prompt(AttendPlan* p, int cus) {
         rest = likely * heads % slots / heads;
     int64_t splits = rest ? slots / (rest * heads) : 1;
     if (splits < 2 && rest < bound && rest * heads <= most_rest(cus)) splits = 2;
-    // ten steps a part at least, where the table is full: a prompt of 1,024 tokens takes
-    // 26 + 8 us in two parts, 31 whole
+    // Ten steps a part at least, where the table is full: a prompt of 1,024 tokens takes
+    // 26 + 8 us in two parts, 31 whole. The host knows the table's width and no request's
+    // keys: in a table that is far wider than its requests short prompts get parts of a step,
+    // or of none, and lose. Tight table, and one of 131,072 keys (in a graph, us):
+    //
+    //   tokens behind keys   64    256   1,024   4 x 256   8 x 200 / 800   64 / 1,000   512 / 4,000
+    //   tight               8.2   12.5    31.0      14.2            45.0         30.5          65.0
+    //   wide               24.4   27.4    36.2      19.1            48.8         26.5          60.8
     const int64_t most = (int64_t)p->max_blocks * p->kv.div.page / (10 * kKeys);
     if (splits > most) splits = most;
     if (splits < 2) rest = 0;
