@@ -588,6 +588,82 @@ int ptstore_attention_workspace(const ptstore_kv_t *kv, int64_t *bytes);
 int ptstore_attention(const ptstore_attention_t *args, void *stream);
 
 /* ======================================================================
+ * Latent caches: models whose layers keep one row a token, a latent vector from which
+ * all heads' keys and values follow, and a part of the keys that all heads share (it carries
+ * the position). Conventions as for the paged cache's operators above; block tables are the same
+ * call. A store holds latent blocks, too: two layers' planes stand as the K and V of one of its
+ * layers, so that a store for L layers has ceil(L / 2) layers of 1 KV head of
+ * latent_dim + rope_dim, and a cache for it that many pairs of planes.
+ * ====================================================================== */
+
+/* One layer: [cache_blocks][slot][latent_dim + rope_dim] values, 16-byte aligned. */
+typedef struct {
+    void *rows;
+    int64_t cache_blocks; /* 0 .. 2^30, and at most 64 GiB a plane */
+    int32_t latent_dim;   /* 256 or 512 */
+    int32_t rope_dim;     /* 64 */
+    int32_t block_tokens; /* 1 .. 64 */
+    int32_t kind;         /* PTSTORE_KV_BF16 or PTSTORE_KV_FP16 */
+} ptstore_latent_t;
+
+/*
+ * Write new tokens' rows to `slots` (as ptstore_kv_append): latent [token][latent_dim] and rope
+ * [token][rope_dim], 16-byte aligned rows, strides in elements (multiples of 8).
+ * Errors: INVALID (a cache or strides other than stated; n_tokens * (latent_dim + rope_dim) > 2^34),
+ * HIP.
+ */
+int ptstore_latent_append(const ptstore_latent_t *cache, const void *latent, int64_t latent_stride,
+                          const void *rope, int64_t rope_stride, const int64_t *slots,
+                          int64_t n_tokens, void *stream);
+
+/* The reverse; zeros for a slot below 0 or past the cache. Errors as ptstore_latent_append. */
+int ptstore_latent_read(const ptstore_latent_t *cache, void *latent, int64_t latent_stride,
+                        void *rope, int64_t rope_stride, const int64_t *slots, int64_t n_tokens,
+                        void *stream);
+
+/*
+ * Causal attention of a batch's new tokens in the latent space (the absorbed form: q_latent is
+ * a head's query times its key matrix, and the caller multiplies the output by its value
+ * matrix). Rows, positions and pages as in ptstore_attention; with c_j and p_j the latent and the
+ * shared part of key j,
+ *   out[t][h] = sum_j w_j c_j / sum_j w_j,
+ *   w_j = exp(scale * (q_latent[t][h] . c_j + q_rope[t][h] . p_j)),   lse[t][h] = log(sum_j w_j).
+ * Rows that see nothing, and values that are not finite, as there. For single tokens, drafts and short
+ * prompts; ptstore_latent_attention_expanded takes fewer operations for long ones.
+ */
+typedef struct {
+    ptstore_latent_t cache;
+    const void *q_latent; /* [n_tokens][heads][latent_dim], 16-byte aligned rows */
+    int64_t q_latent_token_stride; /* in elements, multiples of 8 */
+    int64_t q_latent_head_stride;
+    const void *q_rope;   /* [n_tokens][heads][rope_dim] */
+    int64_t q_rope_token_stride;
+    int64_t q_rope_head_stride;
+    void *out;            /* as q_latent; neither of the queries */
+    int64_t out_token_stride;
+    int64_t out_head_stride;
+    float *lse;                 /* [n_tokens][heads], or NULL */
+    const int64_t *offsets;     /* [R + 1] */
+    const int32_t *context;     /* [R] tokens in the cache before the new ones */
+    const int32_t *block_table; /* [R][max_blocks] */
+    int64_t n_tokens;
+    int32_t R;
+    int32_t max_blocks;
+    int32_t heads;
+    float scale;                /* positive */
+    void *workspace;            /* as for ptstore_attention */
+    int64_t workspace_bytes;
+} ptstore_latent_attention_t;
+
+/* Bytes of workspace that ptstore_latent_attention needs on this device, 16-byte aligned (135 MB for
+ * latent_dim 512): one serves every call. Host only. Errors: INVALID, HIP. */
+int ptstore_latent_attention_workspace(const ptstore_latent_t *cache, int64_t *bytes);
+
+/* Errors: INVALID (shapes, sizes, strides or alignment as stated; max_blocks * block_tokens
+ * > 2^30; n_tokens * heads > 2^31 - 128; no cache blocks; a workspace too small), HIP. */
+int ptstore_latent_attention(const ptstore_latent_attention_t *args, void *stream);
+
+/* ======================================================================
  * Tuning and diagnostics: not store operations. Counters, timing, the
  * store's buffers for tests, copy launch shapes, and a bandwidth probe.
  * ====================================================================== */

@@ -33,6 +33,7 @@
 // tile: with 4 heads to a KV head a single token fills 4 of the 16 columns, and
 // the matrix instructions idle for the rest, which costs nothing here.
 #include "attend.hpp"
+#include "shares.hpp"
 
 namespace ptsd {
 namespace {
@@ -45,94 +46,6 @@ constexpr int step_keys(bool four) { return kWaves * (four ? 64 : 32); }
 
 // Floats of a part in the workspace: rows, then each one's maximum and sum.
 constexpr int part_floats(int dim) { return kDecodeRows * (dim + 2); }
-
-// A request's work for a KV head: its steps of keys for each of its tiles. A
-// request that sees no key has one step, which writes its zeros.
-struct Work {
-    int64_t begin;  // first token
-    int32_t n;
-    int64_t past;
-    int32_t steps, tiles;
-    __device__ int64_t all() const { return (int64_t)steps * tiles; }
-};
-
-__device__ inline Work work_of(const AttendPlan& p, int r, int step_keys) {
-    Work w;
-    const int64_t a = p.offsets[r], b = p.offsets[r + 1];
-    const bool ok = a >= 0 && b > a && b <= p.n_tokens && (b - a) * p.group <= p.few_rows;
-    w.begin = ok ? a : 0;
-    w.n = ok ? (int32_t)(b - a) : 0;
-    w.past = p.context[r];
-    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
-    int64_t end = w.past + w.n;
-    end = end < 1 ? 1 : (end > limit ? limit : end);
-    w.steps = (int32_t)((end + step_keys - 1) / step_keys);
-    w.tiles = (w.n * p.group + kDecodeRows - 1) / kDecodeRows;
-    return w;
-}
-
-// The shares: share w of `count` has steps [w all / count, (w + 1) all / count).
-struct Shares {
-    int64_t all, count;
-    __device__ int64_t begin(int64_t w) const { return w * all / count; }
-    // the share that has step x: the last that begins at or before it
-    __device__ int64_t of(int64_t x) const { return ((x + 1) * count + all - 1) / all - 1; }
-};
-
-// Sums the batch's work and finds the request `r` that the first (or last) step of
-// share `share` is in, its work and its first step. Every workgroup does so for
-// itself: thread t takes the requests from t ceil(R / threads) on.
-template <int kWavesOf>
-__device__ inline Shares find_step(const AttendPlan& p, int step_keys, int64_t share, bool last, int& r, Work& f,
-                                   int64_t& first) {
-    __shared__ int64_t s_sum[kWavesOf], s_first;
-    __shared__ int s_r;
-    __shared__ Work s_work;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int per = (p.R + kWavesOf * 64 - 1) / (kWavesOf * 64);
-    const int r0 = threadIdx.x * per;
-    Work w;
-    int64_t mine = 0;
-    for (int i = 0; i < per && r0 + i < p.R; ++i) {
-        w = work_of(p, r0 + i, step_keys);
-        mine += w.all();
-    }
-    int64_t scan = mine;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t o = __shfl_up(scan, d);
-        if (lane >= d) scan += o;
-    }
-    if (lane == 63) s_sum[wave] = scan;
-    __syncthreads();
-    Shares s{0, p.shares};
-    int64_t before = 0;
-#pragma unroll
-    for (int i = 0; i < kWavesOf; ++i) {
-        if (i < wave) before += s_sum[i];
-        s.all += s_sum[i];
-    }
-    if (s.all < s.count) s.count = s.all;
-    const int64_t lo = before + scan - mine;
-    const int64_t at = share >= s.count ? -1 : last ? s.begin(share + 1) - 1 : s.begin(share);
-    if (at >= lo && at < lo + mine) {
-        s_r = r0;
-        s_first = lo;
-        s_work = w;  // of the only request, if `per` is 1
-    }
-    __syncthreads();
-    if (at < 0) return s;
-    r = __builtin_amdgcn_readfirstlane(s_r);
-    first = s_first;
-    if (per == 1) {
-        f = s_work;
-        return s;
-    }
-    while (f = work_of(p, r, step_keys), first + f.all() <= at) {
-        first += f.all();
-        ++r;
-    }
-    return s;
-}
 
 // K and V are read once: past the caches' usual order, so that they leave the
 // parts' results there.
@@ -188,13 +101,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
     int r;
     int64_t first;  // the request's first step
     Work f;
-    const Shares shares = find_step<kWaves>(p, kStepKeys, share, false, r, f, first);
+    const Shares shares = find_step<kDecodeRows, kWaves>(p, kStepKeys, share, false, r, f, first);
     if (share >= shares.count) return;
     const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
     for (int64_t done = share0; done < share1;) {
     while (done >= first + f.all()) {  // on to the next request with work
         first += f.all();
-        f = work_of(p, ++r, kStepKeys);
+        f = work_of<kDecodeRows>(p, ++r, kStepKeys);
     }
     const int tile = (int)((done - first) / f.steps);
     const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
@@ -585,7 +498,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_join(AttendPlan p) {
     int r;
     int64_t first;
     Work f;
-    const Shares shares = find_step<kJoinWaves>(p, step_keys(kFour), share, true, r, f, first);
+    const Shares shares = find_step<kDecodeRows, kJoinWaves>(p, step_keys(kFour), share, true, r, f, first);
     if (share >= shares.count) return;
     const int64_t share1 = shares.begin(share + 1);
     const int tile = (int)((share1 - 1 - first) / f.steps);

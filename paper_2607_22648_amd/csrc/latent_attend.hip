@@ -1,0 +1,527 @@
+// Attention in the latent space: a token's row is every head's key, and its latent part
+// every head's value. Query rows are (token, head) pairs.
+//
+// A row of 1,152 bytes gives 4 * 512 + 2 * 64 operations a query row: with 16 heads a
+// single token is bound by reading the rows, with 128 by the matrix units as much. The batch's
+// work is cut into equal shares, as in decode.hip, one workgroup of eight waves a compute
+// unit, for tiles of 128 query rows. Two waves take 32 rows, each one half of the dimensions: queries
+// (72 registers) and outputs (128) stay in registers. Each sums its half of the scores, S^T = C Q^T; they
+// trade these sums through LDS, form the same weights, and each its half of the output,
+// O^T = C^T P^T (see attend.hpp). Waves whose rows do not exist only fetch. (A wave for 32 rows
+// and all dimensions needs 400 registers, which the compiler spills.)
+//
+// Rows go from memory to LDS without passing through registers, 32 keys a piece, three pieces in
+// turn, and are read there as they lie for the first product, transposed for the second.
+#include <type_traits>
+
+#include "attend.hpp"
+#include "latent.hpp"
+#include "shares.hpp"
+
+namespace ptsd {
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * 64;
+constexpr int kKeys = 32;    // of a piece
+constexpr int kTile = 128;   // query rows
+constexpr int kStages = 3;   // pieces in LDS: one is computed while two are on their way
+constexpr int kAhead = kStages - 1;
+constexpr int kEntries = 2 * kAhead + 2;  // pieces whose page entries are in LDS
+
+// Floats of a part in the workspace: [4 dimensions][row], then rows' maxima and sums.
+constexpr int part_floats(int latent) { return kTile * (latent + 2); }
+
+// Swizzles of a piece in LDS: 16-byte column c of row r is at c ^ turn(r), in 16 columns of the latent
+// part and 8 of the shared one. 16 lanes read one column of 16 rows as keys: all 16 places of 256
+// bytes. As values, 32 lanes read 64 bytes of rows r .. r + 3, which differ in the upper two bits.
+__device__ inline int turn_latent(int row) { return (row & 3) << 2 | ((row >> 2) & 3); }
+__device__ inline int turn_rope(int row) { return (row >> 1) & 7; }
+
+// Memory to LDS, 16 bytes (4) a lane: lane i's go to `lds` + 16 i (4 i). The compiler does not
+// count these loads, so that it waits for none of them by itself: `arrive` does.
+__device__ inline void fetch16(const uint8_t* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds)
+                 : "memory", "m0");
+}
+__device__ inline void fetch16_at(const uint8_t* at, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds) : "memory", "m0");
+}
+__device__ inline void fetch4_at(const int32_t* at, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(lds) : "memory", "m0");
+}
+// A running maximum that is behind by up to this much (in powers of two) is kept, as in prompt.hip.
+constexpr float kBehind = 8.f;
+template <bool kHalf>
+constexpr float kRoom = Elem<kHalf>::kRoom + (kHalf ? 0.f : kBehind);
+
+// Waits until at most kLeft of the wave's loads are under way; its LDS reads are done, too.
+template <int kLeft>
+__device__ inline void arrive() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
+}
+__device__ inline void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// A value that all lanes hold, in scalar registers.
+__device__ inline int64_t uniform(int64_t x) {
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
+           (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+__device__ inline Work uniform(const Work& w) {
+    return {uniform(w.begin), __builtin_amdgcn_readfirstlane(w.n), uniform(w.past),
+            __builtin_amdgcn_readfirstlane(w.steps), __builtin_amdgcn_readfirstlane(w.tiles)};
+}
+
+template <int L, bool kHalf>
+__global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
+    using E = Elem<kHalf>;
+    using V8 = typename E::v8;
+    constexpr int kSteps = L / 32, kRopeSteps = kRope / 32;  // of a half of the dimensions, 16 each
+    constexpr int kTiles = L / 64;                           // of a half of the output, 32 dimensions each
+    constexpr int kRow = L * 2;                              // bytes of a latent part in LDS
+    constexpr int kPiece = kKeys * (kRow + kRope * 2);
+    constexpr int kRows = kKeys / kWaves;                    // that a wave fetches of a piece
+    constexpr int kFetches = kRows * L / 512 + 1;
+
+    __shared__ __attribute__((aligned(1024))) uint8_t s_rows[kStages * kPiece];
+    __shared__ v4f s_score[kWaves][4 * 64];  // a wave's sums over its half
+    __shared__ int32_t s_entry[kWaves][kEntries * 64];
+    __shared__ int s_endless;  // a value that is not finite lies behind the first row's last key
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int rg = wave >> 1, dh = wave & 1;  // rows, dimensions
+    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
+    const int share = blockIdx.x;
+    int r;
+    int64_t first;  // the request's first step
+    Work f;
+    Shares shares = find_step<kTile, kWaves>(p, kKeys, share, false, r, f, first);
+    shares = {uniform(shares.all), uniform(shares.count)};
+    if (share >= shares.count) return;
+    first = uniform(first);
+    f = uniform(f);
+
+    const uint32_t rows_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_rows;
+    const uint32_t entry_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int32_t*)s_entry[wave];
+    const int32_t* const entries = s_entry[wave];
+
+    const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
+    for (int64_t done = share0; done < share1;) {
+    while (done >= first + f.all()) {  // on to the next request with work
+        first += f.all();
+        f = uniform(work_of<kTile>(p, ++r, kKeys));
+    }
+    const int tile = (int)((done - first) / f.steps);
+    const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
+    const int step0 = (int)(done - tile0);
+    const int step1 = share1 - tile0 < f.steps ? (int)(share1 - tile0) : f.steps;
+    done = tile0 + step1;
+
+    // the tile's rows see keys up to `end`; those of this share are [k0, k1)
+    const int all_rows = f.n * p.group;
+    const int row0 = tile * kTile + rg * 32;
+    const bool active = row0 < all_rows;
+    const int row = row0 + n < all_rows ? row0 + n : all_rows - 1;
+    const int token = row / p.group, head = row - token * p.group;
+    const int last_row = tile * kTile + kTile - 1 < all_rows ? tile * kTile + kTile - 1 : all_rows - 1;
+    int64_t seen64 = f.past + last_row / p.group + 1;
+    seen64 = seen64 < 0 ? 0 : (seen64 > limit ? limit : seen64);
+    const int32_t end = __builtin_amdgcn_readfirstlane((int32_t)seen64);
+    const int32_t k0 = step0 * kKeys;
+    const int32_t k1 = end - k0 < (step1 - step0) * kKeys ? end : step1 * kKeys;
+    const int64_t pos64 = f.past + token;  // the last key this lane's query sees
+    const int32_t pos = pos64 < limit ? (int32_t)pos64 : (int32_t)limit;
+    // the last key that the first row of the wave and of the tile sees
+    auto clip = [&](int64_t x) { return __builtin_amdgcn_readfirstlane((int32_t)(x < limit ? x : limit)); };
+    const int32_t all_see = clip(f.past + (active ? row0 : all_rows - 1) / p.group);
+    const int32_t tile_sees = clip(f.past + tile * kTile / p.group);
+    const int pieces = k1 > k0 ? (k1 - k0 + kKeys - 1) / kKeys : 0;
+    const int32_t* const table = p.table + (int64_t)r * p.max_blocks;
+
+    // queries: column n, 8 consecutive dimensions of each 16 a lane
+    V8 q[kSteps + kRopeSteps];
+    {
+        const uint8_t* a = (const uint8_t*)p.ql.p + ((f.begin + token) * p.ql.token + head * p.ql.head) * 2 + dh * L;
+        const uint8_t* b = (const uint8_t*)p.qr.p + ((f.begin + token) * p.qr.token + head * p.qr.head) * 2 + dh * kRope;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(V8, *(const v4u*)(a + (s * 16 + half * 8) * 2));
+#pragma unroll
+        for (int s = 0; s < kRopeSteps; ++s)
+            q[kSteps + s] = __builtin_bit_cast(V8, *(const v4u*)(b + (s * 16 + half * 8) * 2));
+    }
+    v16f o[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float top = kLowest, sum = 0.f;
+    bool far = false;      // scores are scaled before the maximum is taken
+
+    // the page entries of a piece's keys into LDS (past the end: the last one's)
+    auto fetch_entries = [&](int piece, int lane) {
+        const int32_t key = k0 + piece * kKeys + (lane & 31), last = k1 - 1;
+        fetch4_at(table + div_page((uint32_t)(key < last ? key : last), p.kv.div),
+                  entry_at + (uint32_t)(piece % kEntries) * 256);
+    };
+    // a lane's key of a piece: its row, in units of 16 bytes, and whether it is there
+    auto place = [&](int piece, int lane, bool& there) {
+        const int32_t key = k0 + piece * kKeys + (lane & 31);
+        const int32_t entry = entries[piece % kEntries * 64 + lane];
+        there = key < k1 && entry >= 0 && entry < (int32_t)p.kv.blocks;
+        const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
+        return there ? ((uint32_t)entry * p.kv.div.page + slot) * p.kv.line : 0u;
+    };
+    // this wave's rows of a piece into LDS
+    auto fetch_rows = [&](int piece, int lane) {
+        bool there;
+        const uint32_t at = place(piece, lane, there);
+        const uint32_t to = rows_at + (uint32_t)(piece % kStages) * kPiece;
+        const int j0 = wave * kRows;
+        if constexpr (L == 512) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int j = j0 + i;
+                const uint32_t row_at = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
+                fetch16(p.kv.rows + ((uint64_t)row_at << 4), (uint32_t)((lane ^ turn_latent(j)) << 4), to + j * kRow);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; i += 2) {  // two rows of 512 bytes
+                const int j = j0 + i;
+                const uint32_t a = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
+                const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)at, j + 1);
+                const int up = lane >> 5, c = (lane & 31) ^ turn_latent(j + up);
+                fetch16_at(p.kv.rows + (((uint64_t)(up ? b : a) + c) << 4), to + j * kRow);
+            }
+        }
+        // the shared parts, 8 lanes a row
+        const int mine = j0 + ((lane & 31) >> 3);
+        const uint32_t a = (uint32_t)__shfl((int)at, mine);
+        const int c = L / 8 + ((lane & 7) ^ turn_rope(mine));
+        if (lane < 32) fetch16_at(p.kv.rows + (((uint64_t)a + c) << 4), to + kKeys * kRow + j0 * kRope * 2);
+    };
+
+    if (pieces > 0) {
+        // (the tile before is done with all of LDS but s_endless, which is read behind its last barrier)
+        barrier();
+        for (int i = 0; i <= kAhead; ++i) fetch_entries(i, lane);
+        if (threadIdx.x == 0) s_endless = 0;
+        arrive<0>();
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {  // as in the loop's two turns before the first
+            fetch_entries(kAhead + 1 + i, lane);
+            if (i < pieces) fetch_rows(i, lane);
+        }
+    }
+    for (int piece = 0; piece < pieces; ++piece) {
+        // Behind the barrier the piece is whole, and all waves are done with the one before, whose
+        // place the next to be fetched takes. Left under way: the next piece and an entry.
+        if (piece + 1 < pieces)
+            arrive<(kAhead - 1) * (kFetches + 1)>();
+        else
+            arrive<0>();
+        barrier();
+        // what follows from the lane is formed anew each time: kept, it takes two dozen registers
+        int here = lane;
+        asm volatile("" : "+v"(here));
+        fetch_entries(piece + kEntries - 1, here);
+        if (piece + kAhead < pieces) fetch_rows(piece + kAhead, here);
+        bool there;
+        place(piece, here, there);
+        const uint32_t ok = (uint32_t)__ballot(there);
+        const uint8_t* const mem = s_rows + piece % kStages * kPiece;
+        const int32_t at = k0 + piece * kKeys;
+
+        // LDS places of a lane. As keys: the row that accumulator row n stands for, so that lanes then
+        // hold 8 consecutive keys of each 16.
+        const int n = here & 31, half = here >> 5;
+        const int m8 = n >> 3, krow = 16 * (m8 >> 1) + 8 * ((n >> 2) & 1) + 4 * (m8 & 1) + (n & 3);
+        const uint32_t k_read = krow * kRow + dh * L + (half ^ turn_latent(krow)) * 16;
+        const uint32_t r_read = kKeys * kRow + krow * kRope * 2 + ((4 * dh + half) ^ turn_rope(krow)) * 16;
+        v16f s;
+        if (active) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                s = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + ((k_read ^ (32 * (i & 7))) + 256 * (i >> 3)))),
+                             q[i], s);
+#pragma unroll
+            for (int i = 0; i < kRopeSteps; ++i)
+                s = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + (r_read ^ (32 * i)))), q[kSteps + i], s);
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                s_score[wave][a * 64 + lane] = v4f{s[4 * a], s[4 * a + 1], s[4 * a + 2], s[4 * a + 3]};
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (ok != ~0u || at + kKeys - 1 > tile_sees) {
+            // As values, rows that are not there become zeros, and so do values that are not finite where
+            // the tile's first row does not see them: a weight of zero would make them NaN.
+            bool endless = false;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int j = wave * kRows + i;
+                v4u* const x = (v4u*)(s_rows + piece % kStages * kPiece + j * kRow) + lane;
+                if (!((ok >> j) & 1)) {
+                    if (lane < L / 8) *x = v4u{0u, 0u, 0u, 0u};
+                } else if (at + j > tile_sees && lane < L / 8) {
+                    v4u y = *x;
+                    if (drop_endless<kHalf>(y)) {
+                        endless = true;
+                        *x = y;
+                    }
+                }
+            }
+            if (endless) s_endless = 1;
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+        if (!active) continue;
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const v4f x = s_score[wave ^ 1][a * 64 + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * a + e] += x[e];
+        }
+
+        // keys 16 (e >> 3) + 8 half + (e & 7) in s[e]
+        const bool some_hidden = ok != ~0u || at + kKeys - 1 > all_see;
+        if (some_hidden) {
+            // the keys that are there and that the row sees, from bit 0 those of s[0] on
+            const int32_t ahead = pos - at;
+            uint32_t seen = ahead < 0 ? 0 : (ahead > 30 ? ~0u : (2u << ahead) - 1);
+            seen = (seen & ok) >> (8 * half);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (!(seen & (1u << (16 * (e >> 3) + (e & 7))))) s[e] = -INFINITY;
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, s[e]);
+        most = larger_32(most);
+        auto scale_now = [&] {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = product(s[e], p.scale2);
+            most = product(most, p.scale2);
+        };
+        if (far) scale_now();
+        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, kRoom<kHalf>));
+        if (__any(top2 > top + (far ? 0.f : kBehind))) {
+            if (!far && __any(is_far(top2))) {
+                far = true;
+                scale_now();
+                top2 = fmaxf(top, most + kRoom<kHalf>);
+            }
+            const float less = exp2_of(top - top2);
+            sum *= less;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] *= less;
+            top = top2;
+        }
+        const float scale = far ? 1.f : p.scale2;
+        v4u w[2];  // weights of 16 keys each, rounded to 16 bits as in prompt.hip; the sum takes them as they are
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = exp2_of(__builtin_fmaf(s[e], scale, -top));
+            sum += s[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e >> 2][e & 3] = pack2<kHalf>(s[2 * e], s[2 * e + 1]);
+
+        // as values: dimensions 16 (g & 1) .., keys 8 (g >> 1) .. of each 16, and those 4 further on
+        const int g = here >> 4, l16 = here & 15, vrow = 8 * (g >> 1) + (l16 >> 2), vcol = 2 * (g & 1) + ((l16 & 3) >> 1);
+        const uint32_t v_read = vrow * kRow + dh * L + (vcol ^ turn_latent(vrow)) * 16 + (l16 & 1) * 8;
+        const uint32_t v_read4 = (vrow + 4) * kRow + dh * L + (vcol ^ turn_latent(vrow + 4)) * 16 + (l16 & 1) * 8;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                const uint32_t c = 256 * (i >> 2) + 16 * b * kRow;
+                const v4u vt = join(read_transposed(mem + ((v_read ^ (64 * (i & 3))) + c)),
+                                    read_transposed(mem + ((v_read4 ^ (64 * (i & 3))) + c)));
+                o[i] = E::mma32(__builtin_bit_cast(V8, vt), __builtin_bit_cast(V8, w[b]), o[i]);
+            }
+    }
+    sum += __shfl_xor(sum, 32);
+    // loads of entries past the last piece may be under way; then every wave is done with its pieces
+    arrive<0>();
+    barrier();
+    if (!active) continue;
+    if (s_endless) {
+        for (int32_t key = tile_sees + 1 > k0 ? tile_sees + 1 : k0; key < k1; ++key) {
+            const int32_t entry = table[div_page((uint32_t)key, p.kv.div)];
+            if (key > pos || entry < 0 || entry >= (int32_t)p.kv.blocks) continue;
+            const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
+            const uint16_t* x = (const uint16_t*)(p.kv.rows +
+                ((uint64_t)(((uint32_t)entry * p.kv.div.page + slot) * p.kv.line) << 4)) + dh * (L / 2);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint16_t y = x[32 * i + 8 * (e >> 2) + 4 * half + (e & 3)];
+                    o[i][e] = add_endless(o[i][e], kHalf ? (float)__builtin_bit_cast(_Float16, y)
+                                                         : __uint_as_float((uint32_t)y << 16));
+                }
+        }
+    }
+
+    const int trow = rg * 32 + n;  // in the tile
+    if (step0 > 0 || step1 < f.steps) {
+        // a part: of a tile that began in an earlier share, or one that goes on
+        float* const to = p.parts + (2 * (int64_t)share + (step0 > 0 ? 0 : 1)) * part_floats(L);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                *(v4f*)(to + ((L / 8 * dh + 8 * i + 2 * a + half) * kTile + trow) * 4) =
+                    v4f{o[i][4 * a], o[i][4 * a + 1], o[i][4 * a + 2], o[i][4 * a + 3]};
+        if (dh == 0 && half == 0) *(v2f*)(to + kTile * L + 2 * trow) = v2f{top, sum};
+        continue;
+    }
+    if (row0 + n >= all_rows) continue;  // both halves of a row
+    // no key, or none with a weight: zeros, and the logarithm of nothing
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    uint8_t* const out = (uint8_t*)p.out.p + ((f.begin + token) * p.out.token + head * p.out.head) * 2 + dh * L;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int a = 0; a < 4; a += 2) {
+            // 4 dimensions here, the next 4 in the other half: trade, and write 8 a lane
+            v4u y;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t even = pack2<kHalf>(o[i][4 * a + 2 * h] * inv, o[i][4 * a + 2 * h + 1] * inv);
+                const uint32_t odd = pack2<kHalf>(o[i][4 * a + 4 + 2 * h] * inv, o[i][4 * a + 4 + 2 * h + 1] * inv);
+                const auto both = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+                y[h] = both[0];
+                y[2 + h] = both[1];
+            }
+            *(v4u*)(out + (32 * i + 8 * (a + half)) * 2) = y;
+        }
+    if (p.lse && dh == 0 && half == 0)
+        p.lse[(f.begin + token) * p.group + head] =
+            sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+// Joins the parts of a tile that several shares have: the workgroups of all these shares but the last
+// take its (8 dimensions, row) items in turn. Where a tile has many parts, several lanes
+// divide them, so that each has few trips to memory.
+constexpr int kJoinThreads = 512;
+
+template <int L, bool kHalf>
+__global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
+    constexpr int kItems = kTile * L / 8;
+    __shared__ v4f s_acc[2][kJoinThreads];
+    __shared__ float s_all[kJoinThreads], s_total[kJoinThreads];
+    int r;
+    int64_t first;
+    Work f;
+    const int share = blockIdx.x;
+    const Shares shares = find_step<kTile, kJoinThreads / 64>(p, kKeys, share, true, r, f, first);
+    if (share >= shares.count) return;
+    const int64_t share1 = shares.begin(share + 1);
+    const int tile = (int)((share1 - 1 - first) / f.steps);
+    const int64_t tile0 = first + (int64_t)tile * f.steps, tile1 = tile0 + f.steps;
+    if (tile1 <= share1) return;
+    const int share0 = (int)shares.of(tile0);  // the tile's first
+    const int parts = (int)(shares.of(tile1 - 1) - share0 + 1);
+    const int all_rows = f.n * p.group;
+    int slices = 1;  // lanes that divide an item's parts
+    while (slices < 32 && slices * 8 < parts) slices *= 2;
+    const int at_once = kJoinThreads / slices;
+    const int slice = threadIdx.x / at_once, lane_item = threadIdx.x % at_once;
+    // the first share's second part, then the first of each following
+    const float* const from = p.parts + (2 * (int64_t)share0 + 1) * part_floats(L);
+    auto part_at = [&](int i) { return from + (int64_t)(2 * i - (i > 0)) * part_floats(L); };
+    for (int item0 = (share - share0) * at_once; item0 < kItems; item0 += (parts - 1) * at_once) {
+        const int item = item0 + lane_item, trow = item % kTile, c = item / kTile;
+        const bool in = item < kItems && tile * kTile + trow < all_rows;
+        v4f acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        float all = kLowest, total = 0.f;
+        if (in) {
+            for (int i = slice; i < parts; i += slices) all = fmaxf(all, part_at(i)[kTile * L + 2 * trow]);
+#pragma unroll 4
+            for (int i = slice; i < parts; i += slices) {
+                const float* part = part_at(i);
+                const v2f ms = *(const v2f*)(part + kTile * L + 2 * trow);
+                const v4f a = *(const v4f*)(part + (2 * c * kTile + trow) * 4);
+                const v4f b = *(const v4f*)(part + ((2 * c + 1) * kTile + trow) * 4);
+                const float part_of = exp2_of(ms[0] - all);
+                total += part_of * ms[1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[0][e] += part_of * a[e];
+                    acc[1][e] += part_of * b[e];
+                }
+            }
+        }
+        if (slices > 1) {
+            __syncthreads();
+            s_acc[0][threadIdx.x] = acc[0];
+            s_acc[1][threadIdx.x] = acc[1];
+            s_all[threadIdx.x] = all;
+            s_total[threadIdx.x] = total;
+            __syncthreads();
+            if (slice == 0) {
+                float most = all;
+                for (int i = 1; i < slices; ++i) most = fmaxf(most, s_all[i * at_once + lane_item]);
+                const float less = exp2_of(all - most);
+                total *= less;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[h][e] *= less;
+                for (int i = 1; i < slices; ++i) {
+                    const int t = i * at_once + lane_item;
+                    const float part_of = exp2_of(s_all[t] - most);
+                    total += part_of * s_total[t];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[h][e] += part_of * s_acc[h][t][e];
+                }
+                all = most;
+            }
+        }
+        if (!in || slice) continue;
+        const int row = tile * kTile + trow, token = row / p.group, head = row - token * p.group;
+        const float inv = total != 0.f ? 1.f / total : 0.f;
+        v4u y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = pack2<kHalf>(acc[e >> 1][2 * (e & 1)] * inv, acc[e >> 1][2 * (e & 1) + 1] * inv);
+        *(v4u*)((uint8_t*)p.out.p + ((f.begin + token) * p.out.token + head * p.out.head + c * 8) * 2) = y;
+        if (p.lse && c == 0)
+            p.lse[(f.begin + token) * p.group + head] =
+                total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+template <int L, bool kHalf>
+hipError_t run(const LatentPlan& p, hipStream_t s) {
+    hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_latent_join<L, kHalf>), dim3((unsigned)p.shares), dim3(kJoinThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+template <int L>
+hipError_t run_kind(const LatentPlan& p, hipStream_t s) {
+    return p.kv.kind == PTSTORE_KV_FP16 ? run<L, true>(p, s) : run<L, false>(p, s);
+}
+
+}  // namespace
+
+// One workgroup a compute unit, two parts each.
+int64_t latent_workspace(int latent, int cus) {
+    return 2ll * cus * part_floats(latent) * (int64_t)sizeof(float);
+}
+
+hipError_t launch_latent(const LatentPlan& p, hipStream_t s) {
+    return p.kv.latent == 512 ? run_kind<512>(p, s) : run_kind<256>(p, s);
+}
+
+}  // namespace ptsd

@@ -2,32 +2,20 @@
 // host, launch rules, no allocation and no state.
 #include <hip/hip_runtime.h>
 
-#include <atomic>
 #include <cmath>
 #include <cstdint>
-#include <cstdio>
 
+#include "checks.hpp"
 #include "paged.hpp"
 #include "ptstore.h"
-
-namespace ptsd {
-int set_last_error(int code, const char* what);  // csrc/api.hip
-}
 
 using namespace ptsd;
 
 namespace {
 
-constexpr int64_t kMaxEntries = 1ll << 29;  // (request, block) entries of a call
-constexpr int64_t kMaxKeys = 1ll << 30;     // keys of a request: block-table columns * page size
-constexpr int64_t kMaxItems = 1ll << 32;    // work-items of a launch, fewer than that
 constexpr int64_t kMaxUnits = kMaxItems / 256 - 8192;  // (tile, KV head) pairs of prompt.hip, and room for
                                                        // parts of the last ones
 constexpr int64_t kMaxHeads = kMaxItems / 512;         // decode.hip: a workgroup a head at least, 512 threads
-
-int refuse(const char* what) { return set_last_error(PTSTORE_ERR_INVALID, what); }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 int64_t slab_bytes(int32_t kind, int32_t heads, int32_t dim, int32_t page) {
     if (heads < 1 || (dim != 64 && dim != 128) || page < 1 || page > 64) return -1;
@@ -61,24 +49,6 @@ const char* planes_of(const ptstore_kv_t* kv, Planes* out) {
     out->exponents = (uint32_t)(kv->kv_heads * kv->block_tokens * (kv->head_dim / 2));
     out->kind = kv->kind;
     return nullptr;
-}
-
-// Rows of a packed tensor: 16-byte aligned rows, so strides of 8 elements.
-bool rows_ok(const void* p, int64_t token, int64_t head) {
-    return p && aligned16(p) && token % 8 == 0 && head % 8 == 0;
-}
-
-// Compute units of the current device, asked for once a device.
-int compute_units(int* cus) {
-    constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return set_last_error(PTSTORE_ERR_HIP, "ptstore_attention: device query");
-    if (dev >= 0 && dev < kDevices && (*cus = known[dev].load(std::memory_order_relaxed)) > 0) return PTSTORE_OK;
-    if (hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
-        return set_last_error(PTSTORE_ERR_HIP, "ptstore_attention: device query");
-    if (dev >= 0 && dev < kDevices) known[dev].store(*cus, std::memory_order_relaxed);
-    return PTSTORE_OK;
 }
 
 // Whether a call's rows go 128 to a tile, or 16. The host knows the average
@@ -133,12 +103,6 @@ const char* sized(const ptstore_kv_t* kv, int32_t q_heads, int64_t n_tokens, int
         tile_bound(n_tokens, p->group, R, kPromptRows) * kv->kv_heads > kMaxUnits)
         return "too many tiles for one call";
     return nullptr;
-}
-
-int refuse_as(const char* call, const char* what) {
-    char text[256];
-    snprintf(text, sizeof text, "%s: %s", call, what);
-    return refuse(text);
 }
 
 }  // namespace
@@ -211,7 +175,7 @@ int ptstore_attention_workspace(const ptstore_kv_t* kv, int64_t* bytes) {
     if (!bytes) return refuse("ptstore_attention_workspace: null argument");
     if (const char* bad = planes_of(kv, &pl)) return refuse_as("ptstore_attention_workspace", bad);
     int cus = 0;
-    if (const int rc = compute_units(&cus)) return rc;
+    if (const int rc = compute_units("ptstore_attention", &cus)) return rc;
     *bytes = workspace_of(pl, cus);
     return PTSTORE_OK;
 }
@@ -232,7 +196,7 @@ int ptstore_attention(const ptstore_attention_t* a, void* stream) {
     if (a->out == a->q) return refuse("ptstore_attention: out must not be q");
     if (p.kv.blocks < 1) return refuse("ptstore_attention: the cache has no blocks");
     int cus = 0;
-    if (const int rc = compute_units(&cus)) return rc;
+    if (const int rc = compute_units("ptstore_attention", &cus)) return rc;
     if (a->workspace_bytes < workspace_of(p.kv, cus) || !a->workspace || !aligned16(a->workspace))
         return refuse("ptstore_attention: workspace too small or not 16-byte aligned "
                       "(ptstore_attention_workspace)");

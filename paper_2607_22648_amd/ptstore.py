@@ -68,6 +68,24 @@ class ptstore_attention_t(C.Structure):
                 ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
+class ptstore_latent_t(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("cache_blocks", C.c_int64), ("latent_dim", C.c_int32),
+                ("rope_dim", C.c_int32), ("block_tokens", C.c_int32), ("kind", C.c_int32)]
+
+
+def _strided(name):
+    """A [token][head] array of rows and its strides."""
+    return [(name, C.c_void_p), (name + "_token_stride", C.c_int64), (name + "_head_stride", C.c_int64)]
+
+
+class ptstore_latent_attention_t(C.Structure):
+    _fields_ = [("cache", ptstore_latent_t), *_strided("q_latent"), *_strided("q_rope"), *_strided("out"),
+                ("lse", C.c_void_p), ("offsets", C.c_void_p), ("context", C.c_void_p),
+                ("block_table", C.c_void_p), ("n_tokens", C.c_int64), ("R", C.c_int32),
+                ("max_blocks", C.c_int32), ("heads", C.c_int32), ("scale", C.c_float),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 class PTStoreError(RuntimeError):
     def __init__(self, fn: str, code: int, detail: str):
         super().__init__(f"{fn} failed: code {code} ({detail})")
@@ -84,7 +102,8 @@ EXPORTS = ("ptstore_create", "ptstore_destroy", "ptstore_lookup", "ptstore_gathe
            "ptstore_set_timing_kinds",
            "ptstore_insert_sync", "ptstore_kv_slab_bytes", "ptstore_block_tables",
            "ptstore_kv_append", "ptstore_kv_read", "ptstore_attention_workspace",
-           "ptstore_attention")
+           "ptstore_attention", "ptstore_latent_append", "ptstore_latent_read",
+           "ptstore_latent_attention_workspace", "ptstore_latent_attention")
 
 
 def _load() -> C.CDLL:
@@ -123,6 +142,10 @@ def _load() -> C.CDLL:
         "ptstore_kv_read": [C.POINTER(ptstore_kv_t), p, i64, i64, p, i64, i64, p, i64, p],
         "ptstore_attention_workspace": [C.POINTER(ptstore_kv_t), C.POINTER(i64)],
         "ptstore_attention": [C.POINTER(ptstore_attention_t), p],
+        "ptstore_latent_append": [C.POINTER(ptstore_latent_t), p, i64, p, i64, p, i64, p],
+        "ptstore_latent_read": [C.POINTER(ptstore_latent_t), p, i64, p, i64, p, i64, p],
+        "ptstore_latent_attention_workspace": [C.POINTER(ptstore_latent_t), C.POINTER(i64)],
+        "ptstore_latent_attention": [C.POINTER(ptstore_latent_attention_t), p],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -519,6 +542,61 @@ def ptstore_attention(kv: ptstore_kv_t, q, out, lse, offsets, context, block_tab
                context, block_table, scale, workspace, _stream(stream))
 
 
+def _strided_rows(t: torch.Tensor, shape, kind: int, name: str):
+    """Address and strides of a device tensor [.., dim] of the kind's type whose rows are contiguous;
+    None in `shape` stands for any size."""
+    want = _KV_DTYPES[kind]
+    if not t.is_cuda or t.dtype is not want or t.dim() != len(shape):
+        raise ValueError(f"{name} must be a {len(shape)}-dimensional device tensor of {want}")
+    if any(a is not None and a != b for a, b in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    # a dimension of one row may have any stride: none of its others is reached
+    return (t.data_ptr(), *(s if n > 1 else 0 for n, s in zip(t.shape[:-1], t.stride()[:-1])))
+
+
+def _latent_rows(cache: ptstore_latent_t, latent, rope, slots):
+    n = slots.numel()
+    return (*_strided_rows(latent, (n, cache.latent_dim), cache.kind, "latent"),
+            *_strided_rows(rope, (n, cache.rope_dim), cache.kind, "rope"), _arg(slots, torch.int64, n, "slots"), n)
+
+
+def ptstore_latent_append(cache: ptstore_latent_t, latent, rope, slots, stream=None) -> None:
+    _check("ptstore_latent_append", _lib.ptstore_latent_append(
+        C.byref(cache), *_latent_rows(cache, latent, rope, slots), _stream(stream)))
+
+
+def ptstore_latent_read(cache: ptstore_latent_t, latent, rope, slots, stream=None) -> None:
+    _check("ptstore_latent_read", _lib.ptstore_latent_read(
+        C.byref(cache), *_latent_rows(cache, latent, rope, slots), _stream(stream)))
+
+
+def ptstore_latent_attention_workspace(cache: ptstore_latent_t) -> int:
+    n = C.c_int64()
+    _check("ptstore_latent_attention_workspace",
+           _lib.ptstore_latent_attention_workspace(C.byref(cache), C.byref(n)))
+    return n.value
+
+
+def ptstore_latent_attention(cache: ptstore_latent_t, q_latent, q_rope, out, lse, offsets, context,
+                             block_table, scale: float, workspace, stream=None) -> None:
+    """`lse` may be None; `workspace`: a uint8 tensor of ptstore_latent_attention_workspace(cache) bytes."""
+    R, maxb = _table(offsets, block_table)
+    ql = _strided_rows(q_latent, (None, None, cache.latent_dim), cache.kind, "q_latent")
+    n, heads, _ = q_latent.shape
+    a = ptstore_latent_attention_t(
+        cache, *ql, *_strided_rows(q_rope, (n, heads, cache.rope_dim), cache.kind, "q_rope"),
+        *_strided_rows(out, (n, heads, cache.latent_dim), cache.kind, "out"),
+        None if lse is None else _arg(lse, torch.float32, n * heads, "lse"),
+        _arg(offsets, torch.int64, R + 1, "offsets"), _arg(context, torch.int32, R, "context"),
+        _arg(block_table, torch.int32, 0, "block_table"), n, R, maxb, heads, scale,
+        _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
+    rc = _lib.ptstore_latent_attention(C.byref(a), _stream(stream))
+    if rc:
+        _check("ptstore_latent_attention", rc)
+
+
 # ---------------------------------------------------------------------------
 # Convenience wrappers
 # ---------------------------------------------------------------------------
@@ -744,7 +822,46 @@ _CURRENT = contextlib.nullcontext()  # tensors for the current stream
 _KV_KINDS = {"bf16": PTSTORE_KV_BF16, "fp16": PTSTORE_KV_FP16, "mxfp4": PTSTORE_KV_MXFP4}
 
 
-class PagedCache:
+class _Paged:
+    """What the paged caches share: pages for a batch, workspaces of streams."""
+
+    @staticmethod
+    def _on(stream):
+        """A context in which tensors are allocated for `stream` (a torch stream or a raw handle)."""
+        if stream is None:
+            return _CURRENT
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream))
+        return torch.cuda.stream(stream)
+
+    def _workspace(self, stream, handle: int) -> torch.Tensor:
+        """The workspace of a stream: one serves every layer, and the calls on it in turn (_turn).
+        A graph, which may be replayed on any stream, gets its own."""
+        with self._on(stream):
+            graph = torch.cuda.is_current_stream_capturing()
+            ws = None if graph else self._workspaces.get(handle)
+            if ws is None:
+                ws = torch.empty(self._workspace_bytes(), dtype=torch.uint8, device=self.data.device)
+                if not graph:
+                    self._workspaces[handle] = ws
+        return ws
+
+    def tables(self, offsets, context, block_table, free_blocks, n_tokens: int, held=None, first=None,
+               stream=None):
+        """Give the batch's requests their blocks: fills the new entries of `block_table` and
+        returns (slots, positions, held after, next free entry)."""
+        R, maxb = _table(offsets, block_table)
+        with self._on(stream):
+            slots, next_free = offsets.new_empty(n_tokens), offsets.new_empty(1)
+            positions, held_out = context.new_empty(n_tokens), context.new_empty(R)
+        # offsets and context are checked to be int64 and int32 arrays on the device: so are these
+        _block_tables(R, maxb, offsets, context, held, self.block_tokens, free_blocks, first, block_table,
+                      n_tokens, (slots.data_ptr(), positions.data_ptr(), held_out.data_ptr(),
+                                 next_free.data_ptr()), stream)
+        return slots, positions, held_out, next_free
+
+
+class PagedCache(_Paged):
     """A paged cache [layer][K|V][cache block][slab] on the current device, and the
     operators on it. ``data`` is what the store's loads and ``scatter`` take; a store
     for its blocks is made with ``shape``. ``kv_heads`` is a number, or one per layer.
@@ -787,41 +904,8 @@ class PagedCache:
         """The K and V planes of a layer, as the C calls take them."""
         return self._planes[layer]
 
-    @staticmethod
-    def _on(stream):
-        """A context in which tensors are allocated for `stream` (a torch stream or a raw handle)."""
-        if stream is None:
-            return _CURRENT
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream))
-        return torch.cuda.stream(stream)
-
-    def _workspace(self, stream, handle: int) -> torch.Tensor:
-        """The workspace of a stream: one serves every layer, and the calls on it in turn (_turn).
-        A graph, which may be replayed on any stream, gets its own."""
-        with self._on(stream):
-            graph = torch.cuda.is_current_stream_capturing()
-            ws = None if graph else self._workspaces.get(handle)
-            if ws is None:
-                need = max(ptstore_attention_workspace(kv) for kv in self._planes)
-                ws = torch.empty(need, dtype=torch.uint8, device=self.data.device)
-                if not graph:
-                    self._workspaces[handle] = ws
-        return ws
-
-    def tables(self, offsets, context, block_table, free_blocks, n_tokens: int, held=None, first=None,
-               stream=None):
-        """Give the batch's requests their blocks: fills the new entries of `block_table` and
-        returns (slots, positions, held after, next free entry)."""
-        R, maxb = _table(offsets, block_table)
-        with self._on(stream):
-            slots, next_free = offsets.new_empty(n_tokens), offsets.new_empty(1)
-            positions, held_out = context.new_empty(n_tokens), context.new_empty(R)
-        # offsets and context are checked to be int64 and int32 arrays on the device: so are these
-        _block_tables(R, maxb, offsets, context, held, self.block_tokens, free_blocks, first, block_table,
-                      n_tokens, (slots.data_ptr(), positions.data_ptr(), held_out.data_ptr(),
-                                 next_free.data_ptr()), stream)
-        return slots, positions, held_out, next_free
+    def _workspace_bytes(self) -> int:
+        return max(ptstore_attention_workspace(kv) for kv in self._planes)
 
     def append(self, layer: int, k, v, slots, stream=None) -> None:
         """Write k, v [tokens, kv_heads, head_dim] to `slots` of a layer."""
@@ -866,6 +950,74 @@ class PagedCache:
                 out = made
                 _attention(kv, q, (out.data_ptr(), heads * dim, dim), sums.data_ptr() if lse else None,
                            offsets, context, block_table, scale, workspace, handle)
+        return (out, sums) if lse else out
+
+
+class LatentCache(_Paged):
+    """A paged cache of latent rows, [layer][cache block][slot][latent_dim + rope_dim], on the current
+    device, and the operators on it. ``data`` is what a store's loads and ``scatter`` take; a store for
+    its blocks is made with ``shape``, in which two layers stand as K and V of one: an odd number of
+    layers has room for one more.
+
+    Outputs and workspaces as with PagedCache. Several host threads may use one cache."""
+
+    def __init__(self, layers: int, latent_dim: int, rope_dim: int, cache_blocks: int, block_tokens: int = 16,
+                 kind: str = "bf16", data: Optional[torch.Tensor] = None, device="cuda"):
+        if kind not in ("bf16", "fp16"):
+            raise ValueError(f"kind must be bf16 or fp16, got {kind!r}")
+        if layers < 1 or cache_blocks < 0 or latent_dim not in (256, 512) or rope_dim != 64 or not 1 <= block_tokens <= 64:
+            raise ValueError("a latent cache has layers, 0 or more blocks of 1 to 64 tokens, a latent_dim of 256 or "
+                             "512 and a rope_dim of 64")
+        self.kind, self.cache_blocks, self.block_tokens = kind, cache_blocks, block_tokens
+        pairs, dim = -(-layers // 2), latent_dim + rope_dim
+        self.shape = StoreShape(pairs, 1, dim, block_tokens, 2)
+        plane = cache_blocks * block_tokens * dim * 2
+        if data is None:
+            data = torch.empty(2 * pairs * plane, dtype=torch.uint8, device=device)
+        if not data.is_cuda or not data.is_contiguous() or data.numel() * data.element_size() != 2 * pairs * plane:
+            raise ValueError(f"data must be a contiguous device tensor of {2 * pairs * plane} bytes")
+        self.data = data
+        self.dtype = _KV_DTYPES[_KV_KINDS[kind]]
+        self._workspaces = {}
+        self._turn = threading.Lock()
+        at = data.data_ptr()
+        self._planes = [ptstore_latent_t(at + i * plane, cache_blocks, latent_dim, rope_dim, block_tokens,
+                                         _KV_KINDS[kind]) for i in range(layers)]
+
+    def layer(self, layer: int) -> ptstore_latent_t:
+        """The plane of a layer, as the C calls take it."""
+        return self._planes[layer]
+
+    def _workspace_bytes(self) -> int:
+        return ptstore_latent_attention_workspace(self._planes[0])
+
+    def append(self, layer: int, latent, rope, slots, stream=None) -> None:
+        """Write latent [tokens, latent_dim] and rope [tokens, rope_dim] to `slots` of a layer."""
+        ptstore_latent_append(self._planes[layer], latent, rope, slots, stream)
+
+    def read(self, layer: int, slots, stream=None):
+        """The rows that `slots` of a layer hold: [tokens, latent_dim], [tokens, rope_dim]."""
+        c = self._planes[layer]
+        with self._on(stream):
+            latent = slots.new_empty((slots.numel(), c.latent_dim), dtype=self.dtype)
+            rope = slots.new_empty((slots.numel(), c.rope_dim), dtype=self.dtype)
+        ptstore_latent_read(c, latent, rope, slots, stream)
+        return latent, rope
+
+    def attend(self, layer: int, q_latent, q_rope, offsets, context, block_table, scale: float, out=None,
+               lse: bool = False, workspace=None, stream=None):
+        """Causal attention in the latent space (the absorbed form) of q_latent [tokens, heads, latent_dim]
+        and q_rope [tokens, heads, rope_dim] over a layer: out [tokens, heads, latent_dim], or (out, lse)."""
+        handle = _stream(stream)
+        with self._on(stream):
+            sums = q_latent.new_empty(q_latent.shape[:2], dtype=torch.float32) if lse else None
+            out = torch.empty_like(q_latent, memory_format=torch.contiguous_format) if out is None else out
+        # as in PagedCache.attend: the kernels of two threads' calls on one stream must not mix
+        with self._turn if workspace is None else _CURRENT:
+            if workspace is None:
+                workspace = self._workspace(stream, handle)
+            ptstore_latent_attention(self._planes[layer], q_latent, q_rope, out, sums, offsets, context,
+                                     block_table, scale, workspace, handle)
         return (out, sums) if lse else out
 
 
