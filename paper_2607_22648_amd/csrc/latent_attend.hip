@@ -32,23 +32,25 @@ constexpr int kEntries = 2 * kAhead + 2;  // pieces whose page entries are in LD
 // Floats of a part in the workspace: [4 dimensions][row], then rows' maxima and sums.
 constexpr int part_floats(int latent) { return kTile * (latent + 2); }
 
-// Swizzles of a piece in LDS: 16-byte column c of row r is at c ^ turn(r), in 16 columns of the latent
-// part and 8 of the shared one. 16 lanes read one column of 16 rows as keys: all 16 places of 256
-// bytes. As values, 32 lanes read 64 bytes of rows r .. r + 3, which differ in the upper two bits.
-__device__ inline int turn_latent(int row) { return (row & 3) << 2 | ((row >> 2) & 3); }
+// A piece in LDS: rows' latent parts, padded by 16 bytes, row r in place place_of(r). 16 lanes read one
+// 16-byte column of 16 rows as keys: all 16 places of 256 bytes. As values, 32 lanes read 64
+// bytes of rows r .. r + 3, which are 4 places apart. And every address is a lane's own
+// plus a constant: turned columns took a register for each. The shared parts, eight rows to a load, are not
+// padded: 16-byte column c of row r is at c ^ turn_rope(r).
+__device__ inline int place_of(int row) { return (row & 16) | (row & 3) << 2 | ((row >> 2) & 3); }
 __device__ inline int turn_rope(int row) { return (row >> 1) & 7; }
 
 // Memory to LDS, 16 bytes (4) a lane: lane i's go to `lds` + 16 i (4 i). The compiler does not
 // count these loads, so that it waits for none of them by itself: `arrive` does.
 __device__ inline void fetch16(const uint8_t* base, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds)
-                 : "memory", "m0");
+                 : "memory");
 }
 __device__ inline void fetch16_at(const uint8_t* at, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds) : "memory");
 }
 __device__ inline void fetch4_at(const int32_t* at, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(lds) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(lds) : "memory");
 }
 // A running maximum that is behind by up to this much (in powers of two) is kept, as in prompt.hip.
 constexpr float kBehind = 8.f;
@@ -61,6 +63,28 @@ __device__ inline void arrive() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
 }
 __device__ inline void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// Products 0 .. kProducts - 1 in groups of kDeep: the LDS reads of the next group are under way while one is
+// computed. Left to itself the compiler, short of registers, reads and waits one by one.
+template <int kDeep, int kProducts, class Read, class Multiply>
+__device__ inline void pipelined(const Read& read, const Multiply& multiply) {
+    v4u x[2][kDeep];
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) x[0][i] = read(i);
+#pragma unroll
+    for (int c = 0; c < kProducts; c += kDeep) {
+        const int now = c / kDeep & 1;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i)
+            if (c + kDeep + i < kProducts) x[now ^ 1][i] = read(c + kDeep + i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i)
+            if (c + i < kProducts) multiply(c + i, x[now][i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // A value that all lanes hold, in scalar registers.
 __device__ inline int64_t uniform(int64_t x) {
@@ -78,14 +102,15 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     using V8 = typename E::v8;
     constexpr int kSteps = L / 32, kRopeSteps = kRope / 32;  // of a half of the dimensions, 16 each
     constexpr int kTiles = L / 64;                           // of a half of the output, 32 dimensions each
-    constexpr int kRow = L * 2;                              // bytes of a latent part in LDS
+    constexpr int kRow = L * 2 + 16;                         // bytes of a latent part in LDS
     constexpr int kPiece = kKeys * (kRow + kRope * 2);
     constexpr int kRows = kKeys / kWaves;                    // that a wave fetches of a piece
-    constexpr int kFetches = kRows * L / 512 + 1;
+    constexpr int kFetches = kRows + 1;
 
-    __shared__ __attribute__((aligned(1024))) uint8_t s_rows[kStages * kPiece];
+    __shared__ __attribute__((aligned(256))) uint8_t s_rows[kStages * kPiece];
     __shared__ v4f s_score[kWaves][4 * 64];  // a wave's sums over its half
-    __shared__ int32_t s_entry[kWaves][kEntries * 64];
+    __shared__ v4u s_query[kWaves][kRopeSteps * 64];  // the shared part of a wave's queries: registers are short
+    __shared__ int32_t s_entry[kEntries * 64];
     __shared__ int s_endless;  // a value that is not finite lies behind the first row's last key
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -103,8 +128,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     f = uniform(f);
 
     const uint32_t rows_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_rows;
-    const uint32_t entry_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int32_t*)s_entry[wave];
-    const int32_t* const entries = s_entry[wave];
+    const uint32_t entry_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int32_t*)s_entry;
 
     const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
     for (int64_t done = share0; done < share1;) {
@@ -123,14 +147,14 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     const int row0 = tile * kTile + rg * 32;
     const bool active = row0 < all_rows;
     const int row = row0 + n < all_rows ? row0 + n : all_rows - 1;
-    const int token = row / p.group, head = row - token * p.group;
+    const int row_token = row / p.group, row_head = row - row_token * p.group;
     const int last_row = tile * kTile + kTile - 1 < all_rows ? tile * kTile + kTile - 1 : all_rows - 1;
     int64_t seen64 = f.past + last_row / p.group + 1;
     seen64 = seen64 < 0 ? 0 : (seen64 > limit ? limit : seen64);
     const int32_t end = __builtin_amdgcn_readfirstlane((int32_t)seen64);
     const int32_t k0 = step0 * kKeys;
     const int32_t k1 = end - k0 < (step1 - step0) * kKeys ? end : step1 * kKeys;
-    const int64_t pos64 = f.past + token;  // the last key this lane's query sees
+    const int64_t pos64 = f.past + row_token;  // the last key this lane's query sees
     const int32_t pos = pos64 < limit ? (int32_t)pos64 : (int32_t)limit;
     // the last key that the first row of the wave and of the tile sees
     auto clip = [&](int64_t x) { return __builtin_amdgcn_readfirstlane((int32_t)(x < limit ? x : limit)); };
@@ -140,15 +164,14 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     const int32_t* const table = p.table + (int64_t)r * p.max_blocks;
 
     // queries: column n, 8 consecutive dimensions of each 16 a lane
-    V8 q[kSteps + kRopeSteps];
+    V8 q[kSteps];
     {
-        const uint8_t* a = (const uint8_t*)p.ql.p + ((f.begin + token) * p.ql.token + head * p.ql.head) * 2 + dh * L;
-        const uint8_t* b = (const uint8_t*)p.qr.p + ((f.begin + token) * p.qr.token + head * p.qr.head) * 2 + dh * kRope;
+        const uint8_t* a = (const uint8_t*)p.ql.p + ((f.begin + row_token) * p.ql.token + row_head * p.ql.head) * 2 + dh * L;
+        const uint8_t* b = (const uint8_t*)p.qr.p + ((f.begin + row_token) * p.qr.token + row_head * p.qr.head) * 2 + dh * kRope;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(V8, *(const v4u*)(a + (s * 16 + half * 8) * 2));
 #pragma unroll
-        for (int s = 0; s < kRopeSteps; ++s)
-            q[kSteps + s] = __builtin_bit_cast(V8, *(const v4u*)(b + (s * 16 + half * 8) * 2));
+        for (int s = 0; s < kRopeSteps; ++s) s_query[wave][s * 64 + lane] = *(const v4u*)(b + (s * 16 + half * 8) * 2);
     }
     v16f o[kTiles];
 #pragma unroll
@@ -158,8 +181,9 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     float top = kLowest, sum = 0.f;
     bool far = false;      // scores are scaled before the maximum is taken
 
-    // the page entries of a piece's keys into LDS (past the end: the last one's)
+    // the page entries of a piece's keys into LDS (past the end: the last one's), by the first wave
     auto fetch_entries = [&](int piece, int lane) {
+        if (wave) return;
         const int32_t key = k0 + piece * kKeys + (lane & 31), last = k1 - 1;
         fetch4_at(table + div_page((uint32_t)(key < last ? key : last), p.kv.div),
                   entry_at + (uint32_t)(piece % kEntries) * 256);
@@ -167,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     // a lane's key of a piece: its row, in units of 16 bytes, and whether it is there
     auto place = [&](int piece, int lane, bool& there) {
         const int32_t key = k0 + piece * kKeys + (lane & 31);
-        const int32_t entry = entries[piece % kEntries * 64 + lane];
+        const int32_t entry = s_entry[piece % kEntries * 64 + lane];
         there = key < k1 && entry >= 0 && entry < (int32_t)p.kv.blocks;
         const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
         return there ? ((uint32_t)entry * p.kv.div.page + slot) * p.kv.line : 0u;
@@ -178,26 +202,16 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
         const uint32_t at = place(piece, lane, there);
         const uint32_t to = rows_at + (uint32_t)(piece % kStages) * kPiece;
         const int j0 = wave * kRows;
-        if constexpr (L == 512) {
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int j = j0 + i;
-                const uint32_t row_at = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
-                fetch16(p.kv.rows + ((uint64_t)row_at << 4), (uint32_t)((lane ^ turn_latent(j)) << 4), to + j * kRow);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kRows; i += 2) {  // two rows of 512 bytes
-                const int j = j0 + i;
-                const uint32_t a = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
-                const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)at, j + 1);
-                const int up = lane >> 5, c = (lane & 31) ^ turn_latent(j + up);
-                fetch16_at(p.kv.rows + (((uint64_t)(up ? b : a) + c) << 4), to + j * kRow);
-            }
+        for (int i = 0; i < kRows; ++i) {
+            const int j = j0 + i;
+            const uint32_t row_at = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
+            const uint8_t* const row = p.kv.rows + ((uint64_t)row_at << 4);
+            if (L == 512 || lane < L / 8) fetch16(row, (uint32_t)lane * 16, to + place_of(j) * kRow);
         }
         // the shared parts, 8 lanes a row
         const int mine = j0 + ((lane & 31) >> 3);
-        const uint32_t a = (uint32_t)__shfl((int)at, mine);
+        const uint32_t a = (uint32_t)__builtin_amdgcn_ds_bpermute(mine * 4, (int)at);
         const int c = L / 8 + ((lane & 7) ^ turn_rope(mine));
         if (lane < 32) fetch16_at(p.kv.rows + (((uint64_t)a + c) << 4), to + kKeys * kRow + j0 * kRope * 2);
     };
@@ -205,20 +219,24 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     if (pieces > 0) {
         // (the tile before is done with all of LDS but s_endless, which is read behind its last barrier)
         barrier();
-        for (int i = 0; i <= kAhead; ++i) fetch_entries(i, lane);
+        int here = lane;
+        asm volatile("" : "+v"(here));
+        for (int i = 0; i <= kAhead; ++i) fetch_entries(i, here);
         if (threadIdx.x == 0) s_endless = 0;
         arrive<0>();
+        barrier();
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {  // as in the loop's two turns before the first
-            fetch_entries(kAhead + 1 + i, lane);
-            if (i < pieces) fetch_rows(i, lane);
+            fetch_entries(kAhead + 1 + i, here);
+            if (i < pieces) fetch_rows(i, here);
         }
     }
     for (int piece = 0; piece < pieces; ++piece) {
         // Behind the barrier the piece is whole, and all waves are done with the one before, whose
-        // place the next to be fetched takes. Left under way: the next piece and an entry.
+        // place the next to be fetched takes. Left under way: this wave's part of the next piece (and, so,
+        // of page entries only those fetched after it, which are used three turns later).
         if (piece + 1 < pieces)
-            arrive<(kAhead - 1) * (kFetches + 1)>();
+            arrive<(kAhead - 1) * kFetches>();
         else
             arrive<0>();
         barrier();
@@ -237,19 +255,21 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
         // hold 8 consecutive keys of each 16.
         const int n = here & 31, half = here >> 5;
         const int m8 = n >> 3, krow = 16 * (m8 >> 1) + 8 * ((n >> 2) & 1) + 4 * (m8 & 1) + (n & 3);
-        const uint32_t k_read = krow * kRow + dh * L + (half ^ turn_latent(krow)) * 16;
+        const uint32_t k_read = place_of(krow) * kRow + dh * L + half * 16;
         const uint32_t r_read = kKeys * kRow + krow * kRope * 2 + ((4 * dh + half) ^ turn_rope(krow)) * 16;
         v16f s;
         if (active) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i)
-                s = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + ((k_read ^ (32 * (i & 7))) + 256 * (i >> 3)))),
-                             q[i], s);
-#pragma unroll
-            for (int i = 0; i < kRopeSteps; ++i)
-                s = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + (r_read ^ (32 * i)))), q[kSteps + i], s);
+            pipelined<3, kSteps + kRopeSteps>(
+                [&](int i) {
+                    const int j = i - kSteps;
+                    return *(const v4u*)(mem + (j < 0 ? k_read + 32 * i : r_read ^ (32 * j)));
+                },
+                [&](int i, const v4u& x) {
+                    const V8 y = i < kSteps ? q[i < kSteps ? i : 0] : __builtin_bit_cast(V8, s_query[wave][(i - kSteps) * 64 + here]);
+                    s = E::mma32(__builtin_bit_cast(V8, x), y, s);
+                });
 #pragma unroll
             for (int a = 0; a < 4; ++a)
                 s_score[wave][a * 64 + lane] = v4f{s[4 * a], s[4 * a + 1], s[4 * a + 2], s[4 * a + 3]};
@@ -262,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const int j = wave * kRows + i;
-                v4u* const x = (v4u*)(s_rows + piece % kStages * kPiece + j * kRow) + lane;
+                v4u* const x = (v4u*)(s_rows + piece % kStages * kPiece + place_of(j) * kRow) + lane;
                 if (!((ok >> j) & 1)) {
                     if (lane < L / 8) *x = v4u{0u, 0u, 0u, 0u};
                 } else if (at + j > tile_sees && lane < L / 8) {
@@ -332,17 +352,17 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
 
         // as values: dimensions 16 (g & 1) .., keys 8 (g >> 1) .. of each 16, and those 4 further on
         const int g = here >> 4, l16 = here & 15, vrow = 8 * (g >> 1) + (l16 >> 2), vcol = 2 * (g & 1) + ((l16 & 3) >> 1);
-        const uint32_t v_read = vrow * kRow + dh * L + (vcol ^ turn_latent(vrow)) * 16 + (l16 & 1) * 8;
-        const uint32_t v_read4 = (vrow + 4) * kRow + dh * L + (vcol ^ turn_latent(vrow + 4)) * 16 + (l16 & 1) * 8;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                const uint32_t c = 256 * (i >> 2) + 16 * b * kRow;
-                const v4u vt = join(read_transposed(mem + ((v_read ^ (64 * (i & 3))) + c)),
-                                    read_transposed(mem + ((v_read4 ^ (64 * (i & 3))) + c)));
-                o[i] = E::mma32(__builtin_bit_cast(V8, vt), __builtin_bit_cast(V8, w[b]), o[i]);
-            }
+        const uint32_t v_read = place_of(vrow) * kRow + dh * L + vcol * 16 + (l16 & 1) * 8;
+        pipelined<2, 2 * kTiles>(
+            [&](int j) {
+                const int i = j % kTiles;
+                const uint8_t* const x = mem + v_read + 64 * i + 16 * (j / kTiles) * kRow;
+                return join(read_transposed(x), read_transposed(x + kRow));  // row + 4 is the next place
+            },
+            [&](int j, const v4u& x) {
+                const int i = j % kTiles;
+                o[i] = E::mma32(__builtin_bit_cast(V8, x), __builtin_bit_cast(V8, w[j / kTiles]), o[i]);
+            });
     }
     sum += __shfl_xor(sum, 32);
     // loads of entries past the last piece may be under way; then every wave is done with its pieces
@@ -354,20 +374,24 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
             const int32_t entry = table[div_page((uint32_t)key, p.kv.div)];
             if (key > pos || entry < 0 || entry >= (int32_t)p.kv.blocks) continue;
             const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
+            int up = half;
+            asm volatile("" : "+v"(up));  // no address is kept for this from before the pieces
             const uint16_t* x = (const uint16_t*)(p.kv.rows +
-                ((uint64_t)(((uint32_t)entry * p.kv.div.page + slot) * p.kv.line) << 4)) + dh * (L / 2);
+                ((uint64_t)(((uint32_t)entry * p.kv.div.page + slot) * p.kv.line) << 4)) + dh * (L / 2) + 4 * up;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const uint16_t y = x[32 * i + 8 * (e >> 2) + 4 * half + (e & 3)];
+                    const uint16_t y = x[32 * i + 8 * (e >> 2) + (e & 3)];
                     o[i][e] = add_endless(o[i][e], kHalf ? (float)__builtin_bit_cast(_Float16, y)
                                                          : __uint_as_float((uint32_t)y << 16));
                 }
         }
     }
 
-    const int trow = rg * 32 + n;  // in the tile
+    int column = n;
+    asm volatile("" : "+v"(column));
+    const int trow = rg * 32 + column;  // in the tile
     if (step0 > 0 || step1 < f.steps) {
         // a part: of a tile that began in an earlier share, or one that goes on
         float* const to = p.parts + (2 * (int64_t)share + (step0 > 0 ? 0 : 1)) * part_floats(L);
@@ -380,7 +404,8 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
         if (dh == 0 && half == 0) *(v2f*)(to + kTile * L + 2 * trow) = v2f{top, sum};
         continue;
     }
-    if (row0 + n >= all_rows) continue;  // both halves of a row
+    if (row0 + column >= all_rows) continue;  // both halves of a row
+    const int token = (row0 + column) / p.group, head = row0 + column - token * p.group;
     // no key, or none with a weight: zeros, and the logarithm of nothing
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     uint8_t* const out = (uint8_t*)p.out.p + ((f.begin + token) * p.out.token + head * p.out.head) * 2 + dh * L;
