@@ -431,20 +431,48 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     }
 }
 
-// Joins the parts of a tile that several shares have: the workgroups of all these shares but the last
-// take its (8 dimensions, row) items in turn. Where a tile has many parts, several lanes
-// divide them, so that each has few trips to memory.
+// Joins the parts of a tile that several shares have: the workgroups of all these shares but the last, kJoinGroups
+// each, take its (row, 8 dimensions) items in turn. A lane loads eight parts at once; where a tile has
+// more, several lanes divide them, so that each has few trips to memory.
 constexpr int kJoinThreads = 512;
+constexpr int kJoinGroups = 4;
+
+// A row's parts so far: 8 dimensions of the output, the maximum, the sum.
+struct Joined {
+    v4f acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    float all = kLowest, total = 0.f;
+    // To a maximum of at least `top`. Sums that then weigh nothing stay in, and are NaN where they are not
+    // finite: a part whose scores are all NaN has the lowest maximum.
+    __device__ void raise(float top) {
+        const float to = fmaxf(all, top), less = exp2_of(all - to);
+        total *= less;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[h][e] *= less;
+        all = to;
+    }
+    // a part whose maximum is not above `all`
+    __device__ void add(v4f a, v4f b, float top, float sum) {
+        const float part_of = exp2_of(top - all);
+        total += part_of * sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            acc[0][e] += part_of * a[e];
+            acc[1][e] += part_of * b[e];
+        }
+    }
+};
 
 template <int L, bool kHalf>
 __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
-    constexpr int kItems = kTile * L / 8;
+    constexpr int kFlight = 8;
     __shared__ v4f s_acc[2][kJoinThreads];
     __shared__ float s_all[kJoinThreads], s_total[kJoinThreads];
     int r;
     int64_t first;
     Work f;
-    const int share = blockIdx.x;
+    const int share = blockIdx.x / kJoinGroups;
     const Shares shares = find_step<kTile, kJoinThreads / 64>(p, kKeys, share, true, r, f, first);
     if (share >= shares.count) return;
     const int64_t share1 = shares.begin(share + 1);
@@ -453,74 +481,67 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     if (tile1 <= share1) return;
     const int share0 = (int)shares.of(tile0);  // the tile's first
     const int parts = (int)(shares.of(tile1 - 1) - share0 + 1);
-    const int all_rows = f.n * p.group;
+    const int rows_left = f.n * p.group - tile * kTile, rows = rows_left < kTile ? rows_left : kTile;
+    const int items = rows * (L / 8);
     int slices = 1;  // lanes that divide an item's parts
-    while (slices < 32 && slices * 8 < parts) slices *= 2;
+    while (slices < 32 && slices * kFlight < parts) slices *= 2;
     const int at_once = kJoinThreads / slices;
     const int slice = threadIdx.x / at_once, lane_item = threadIdx.x % at_once;
     // the first share's second part, then the first of each following
     const float* const from = p.parts + (2 * (int64_t)share0 + 1) * part_floats(L);
     auto part_at = [&](int i) { return from + (int64_t)(2 * i - (i > 0)) * part_floats(L); };
-    for (int item0 = (share - share0) * at_once; item0 < kItems; item0 += (parts - 1) * at_once) {
-        const int item = item0 + lane_item, trow = item % kTile, c = item / kTile;
-        const bool in = item < kItems && tile * kTile + trow < all_rows;
-        v4f acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-        float all = kLowest, total = 0.f;
-        if (in) {
-            for (int i = slice; i < parts; i += slices) all = fmaxf(all, part_at(i)[kTile * L + 2 * trow]);
-#pragma unroll 4
-            for (int i = slice; i < parts; i += slices) {
-                const float* part = part_at(i);
-                const v2f ms = *(const v2f*)(part + kTile * L + 2 * trow);
-                const v4f a = *(const v4f*)(part + (2 * c * kTile + trow) * 4);
-                const v4f b = *(const v4f*)(part + ((2 * c + 1) * kTile + trow) * 4);
-                const float part_of = exp2_of(ms[0] - all);
-                total += part_of * ms[1];
+    const int me = (share - share0) * kJoinGroups + blockIdx.x % kJoinGroups, workers = (parts - 1) * kJoinGroups;
+    for (int item0 = me * at_once; item0 < items; item0 += workers * at_once) {
+        const int item = item0 + lane_item < items ? item0 + lane_item : items - 1;
+        const int trow = item % rows, c = item / rows;
+        Joined sum;
+        for (int i0 = slice; i0 < parts; i0 += slices * kFlight) {
+            v4f a[kFlight], b[kFlight];
+            v2f ms[kFlight];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc[0][e] += part_of * a[e];
-                    acc[1][e] += part_of * b[e];
+            for (int u = 0; u < kFlight; ++u) {
+                const int i = i0 + u * slices;
+                const float* part = part_at(i < parts ? i : i0);
+                ms[u] = *(const v2f*)(part + kTile * L + 2 * trow);
+                a[u] = *(const v4f*)(part + (2 * c * kTile + trow) * 4);
+                b[u] = *(const v4f*)(part + ((2 * c + 1) * kTile + trow) * 4);
+                if (i >= parts) {
+                    ms[u] = v2f{-INFINITY, 0.f};
+                    a[u] = b[u] = v4f{0, 0, 0, 0};
                 }
             }
+            float top = kLowest;
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) top = fmaxf(top, ms[u][0]);
+            sum.raise(top);
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) sum.add(a[u], b[u], ms[u][0], ms[u][1]);
         }
         if (slices > 1) {
             __syncthreads();
-            s_acc[0][threadIdx.x] = acc[0];
-            s_acc[1][threadIdx.x] = acc[1];
-            s_all[threadIdx.x] = all;
-            s_total[threadIdx.x] = total;
+            s_acc[0][threadIdx.x] = sum.acc[0];
+            s_acc[1][threadIdx.x] = sum.acc[1];
+            s_all[threadIdx.x] = sum.all;
+            s_total[threadIdx.x] = sum.total;
             __syncthreads();
-            if (slice == 0) {
-                float most = all;
-                for (int i = 1; i < slices; ++i) most = fmaxf(most, s_all[i * at_once + lane_item]);
-                const float less = exp2_of(all - most);
-                total *= less;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[h][e] *= less;
+            if (slice == 0)
                 for (int i = 1; i < slices; ++i) {
                     const int t = i * at_once + lane_item;
-                    const float part_of = exp2_of(s_all[t] - most);
-                    total += part_of * s_total[t];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[h][e] += part_of * s_acc[h][t][e];
+                    sum.raise(s_all[t]);
+                    sum.add(s_acc[0][t], s_acc[1][t], s_all[t], s_total[t]);
                 }
-                all = most;
-            }
         }
-        if (!in || slice) continue;
+        if (item0 + lane_item >= items || slice) continue;
         const int row = tile * kTile + trow, token = row / p.group, head = row - token * p.group;
-        const float inv = total != 0.f ? 1.f / total : 0.f;
+        const float total = sum.total, inv = total != 0.f ? 1.f / total : 0.f;
         v4u y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = pack2<kHalf>(acc[e >> 1][2 * (e & 1)] * inv, acc[e >> 1][2 * (e & 1) + 1] * inv);
+        for (int e = 0; e < 4; ++e)
+            y[e] = pack2<kHalf>(sum.acc[e >> 1][2 * (e & 1)] * inv, sum.acc[e >> 1][2 * (e & 1) + 1] * inv);
         *(v4u*)((uint8_t*)p.out.p + ((f.begin + token) * p.out.token + head * p.out.head + c * 8) * 2) = y;
         if (p.lse && c == 0)
             p.lse[(f.begin + token) * p.group + head] =
-                total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+                total != 0.f ? (sum.all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
     }
 }
 
@@ -529,7 +550,7 @@ hipError_t run(const LatentPlan& p, hipStream_t s) {
     hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_latent_join<L, kHalf>), dim3((unsigned)p.shares), dim3(kJoinThreads), 0, s, p);
+    hipLaunchKernelGGL((k_latent_join<L, kHalf>), dim3((unsigned)(p.shares * kJoinGroups)), dim3(kJoinThreads), 0, s, p);
     return hipGetLastError();
 }
 
