@@ -663,6 +663,57 @@ int ptstore_latent_attention_workspace(const ptstore_latent_t *cache, int64_t *b
  * > 2^30; n_tokens * heads > 2^31 - 128; no cache blocks; a workspace too small), HIP. */
 int ptstore_latent_attention(const ptstore_latent_attention_t *args, void *stream);
 
+/*
+ * The same attention in the expanded form, for prompts: each head's keys and values are formed from the
+ * rows by the head's matrices, in the cache's type, and
+ *   k_hj = (w_k[h] c_j, p_j),  v_hj = w_v[h] c_j,
+ *   out[t][h] = sum_j w_j v_hj / sum_j w_j,  w_j = exp(scale * (q_nope[t][h], q_rope[t][h]) . k_hj).
+ * Keys have 128 values of a head's own beside the rope_dim shared ones, values 128. Request r has
+ * key_offsets[r+1] - key_offsets[r] keys of the n_keys that the workspace has room for: at least
+ * context[r] + its new tokens (keys past that do not exist); key_offsets rises from 0 to n_keys, and
+ * a request for which it does not has no keys. Cost grows with all keys, past and new: behind a long
+ * past and for few tokens the absorbed form is the shorter.
+ */
+typedef struct {
+    ptstore_latent_t cache;
+    const void *q_nope; /* [n_tokens][heads][128], 16-byte aligned rows */
+    int64_t q_nope_token_stride;
+    int64_t q_nope_head_stride;
+    const void *q_rope; /* [n_tokens][heads][rope_dim] */
+    int64_t q_rope_token_stride;
+    int64_t q_rope_head_stride;
+    const void *w_k;    /* [heads][128][latent_dim], rows 16-byte aligned */
+    int64_t w_k_head_stride;
+    int64_t w_k_row_stride;
+    const void *w_v;    /* as w_k */
+    int64_t w_v_head_stride;
+    int64_t w_v_row_stride;
+    void *out;          /* [n_tokens][heads][128]; neither of the queries */
+    int64_t out_token_stride;
+    int64_t out_head_stride;
+    float *lse;                 /* [n_tokens][heads], or NULL */
+    const int64_t *offsets;     /* [R + 1] */
+    const int32_t *context;     /* [R] */
+    const int32_t *block_table; /* [R][max_blocks] */
+    const int64_t *key_offsets; /* [R + 1] */
+    int64_t n_tokens;
+    int64_t n_keys;
+    int32_t R;
+    int32_t max_blocks;
+    int32_t heads;
+    float scale;                /* positive */
+    void *workspace;            /* as for ptstore_attention */
+    int64_t workspace_bytes;
+} ptstore_latent_expanded_t;
+
+/* Bytes of workspace for n_keys keys, 16-byte aligned: 512 a key and head, and 132 a key. Host only.
+ * Errors: INVALID. */
+int ptstore_latent_expanded_workspace(int32_t heads, int64_t n_keys, int64_t *bytes);
+
+/* Errors: INVALID (as ptstore_latent_attention; n_keys > 2^31 - 256; more than 2^24 - 2^13
+ * (n_tokens / 128 + R) * heads or (n_keys / 128 + 1) * heads), HIP. */
+int ptstore_latent_attention_expanded(const ptstore_latent_expanded_t *args, void *stream);
+
 /* ======================================================================
  * Tuning and diagnostics: not store operations. Counters, timing, the
  * store's buffers for tests, copy launch shapes, and a bandwidth probe.

@@ -154,7 +154,8 @@ struct Tile {
 // Finds tile number t of the batch. Every wave looks for itself, 64 requests at
 // a time: request r's tiles start at offsets[r] * group / rows + r, which
 // rises with r, so the lanes that start at or before t are counted.
-__device__ inline Tile find_tile(const AttendPlan& p, int64_t t, int rows) {
+template <class Plan>
+__device__ inline Tile find_tile(const Plan& p, int64_t t, int rows) {
     const int lane = threadIdx.x & 63;
     Tile f;
     f.tile = -1;

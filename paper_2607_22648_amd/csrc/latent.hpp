@@ -39,6 +39,32 @@ struct LatentPlan {
     int32_t shares;
 };
 
+constexpr int kNope = 128, kValue = 128;  // of a head: values of a key's own part, of a value
+
+// The expanded form: keys and values of all heads, packed [head][key], in the workspace.
+struct ExpandedPlan {
+    LatentPlane kv;
+    Rows qn, qr, out;  // queries: a head's own part, the shared part
+    Rows wk, wv;       // [head][row of the head][latent]: `token` is the row's stride
+    float* lse;
+    const int64_t* offsets;
+    const int32_t* context;
+    const int32_t* table;
+    const int64_t* key_offsets;
+    int64_t n_tokens, n_keys;
+    int32_t R, max_blocks, heads;
+    int32_t group, few_rows;  // rows of a token: one a head; no limit
+    float scale2;
+    uint8_t *k, *v;   // [head][key][128]
+    uint8_t* rope;    // [key][64]
+    int32_t* there;   // [key] whether its page exists
+    int32_t each;     // heads of a workgroup that forms keys and values
+};
+
+int64_t expanded_workspace(int32_t heads, int64_t n_keys);  // bytes
+void place_expanded(ExpandedPlan* p, void* workspace);
+hipError_t launch_expanded(const ExpandedPlan& p, int cus, hipStream_t s);
+
 const char* plane_of(const ptstore_latent_t* cache, LatentPlane* out);  // or why not
 const char* batch_of(int64_t n_tokens, int32_t R, int32_t max_blocks, int32_t block_tokens, int32_t heads);
 hipError_t launch_latent_append(const LatentPlane& kv, const void* latent, int64_t latent_stride, const void* rope,

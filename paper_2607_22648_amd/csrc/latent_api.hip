@@ -48,6 +48,9 @@ using namespace ptsd;
 
 namespace {
 
+constexpr int64_t kMostKeys = (1ll << 31) - 256;       // of a call's expanded keys: numbered in 31 bits
+constexpr int64_t kMaxUnits = kMaxItems / 256 - 8192;  // workgroups of latent_prompt.hip
+
 int move_rows(const char* call, const ptstore_latent_t* cache, const void* latent, int64_t latent_stride,
               const void* rope, int64_t rope_stride, const int64_t* slots, int64_t n, bool read, void* stream) {
     LatentPlane kv;
@@ -130,6 +133,65 @@ int ptstore_latent_attention(const ptstore_latent_attention_t* a, void* stream) 
     p.shares = cus;
     const hipError_t e = launch_latent(p, (hipStream_t)stream);
     return e == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, "ptstore_latent_attention: launch");
+}
+
+int ptstore_latent_expanded_workspace(int32_t heads, int64_t n_keys, int64_t* bytes) {
+    if (!bytes || heads < 1 || n_keys < 0 || n_keys > kMostKeys)
+        return refuse("ptstore_latent_expanded_workspace: heads or n_keys out of range, or a null argument");
+    *bytes = expanded_workspace(heads, n_keys);
+    return PTSTORE_OK;
+}
+
+int ptstore_latent_attention_expanded(const ptstore_latent_expanded_t* a, void* stream) {
+    const char* const call = "ptstore_latent_attention_expanded";
+    if (!a) return refuse_as(call, "null argument");
+    ExpandedPlan p;
+    if (const char* bad = plane_of(&a->cache, &p.kv)) return refuse_as(call, bad);
+    if (const char* bad = batch_of(a->n_tokens, a->R, a->max_blocks, a->cache.block_tokens, a->heads))
+        return refuse_as(call, bad);
+    if (a->n_keys < 0 || a->n_keys > kMostKeys) return refuse_as(call, "n_keys out of range");
+    if ((a->n_tokens / 128 + a->R + 1) * a->heads > kMaxUnits || (a->n_keys / 128 + 1) * a->heads > kMaxUnits)
+        return refuse_as(call, "too many tiles for one call");
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale * 1.4426950408889634f))
+        return refuse_as(call, "scale must be positive and finite");
+    if (a->n_tokens == 0) return PTSTORE_OK;
+    if (!a->offsets || !a->context || !a->block_table || !a->key_offsets) return refuse_as(call, "null argument");
+    if (!rows_ok(a->q_nope, a->q_nope_token_stride, a->q_nope_head_stride) ||
+        !rows_ok(a->q_rope, a->q_rope_token_stride, a->q_rope_head_stride) ||
+        !rows_ok(a->out, a->out_token_stride, a->out_head_stride))
+        return refuse_as(call, "rows of the queries or of out null or not 16-byte aligned");
+    if (!rows_ok(a->w_k, a->w_k_row_stride, a->w_k_head_stride) ||
+        !rows_ok(a->w_v, a->w_v_row_stride, a->w_v_head_stride))
+        return refuse_as(call, "rows of w_k or w_v null or not 16-byte aligned");
+    // no order is promised between a row's output and the reads of other rows' queries
+    if (a->out == a->q_nope || a->out == a->q_rope) return refuse_as(call, "out must be neither of the queries");
+    if (p.kv.blocks < 1) return refuse_as(call, "the cache has no blocks");
+    if (a->workspace_bytes < expanded_workspace(a->heads, a->n_keys) ||
+        (a->n_keys > 0 && (!a->workspace || !aligned16(a->workspace))))
+        return refuse_as(call, "workspace too small or not 16-byte aligned (ptstore_latent_expanded_workspace)");
+    int cus = 0;
+    if (const int rc = compute_units(call, &cus)) return rc;
+    p.qn = Rows{a->q_nope, a->q_nope_token_stride, a->q_nope_head_stride};
+    p.qr = Rows{a->q_rope, a->q_rope_token_stride, a->q_rope_head_stride};
+    p.out = Rows{a->out, a->out_token_stride, a->out_head_stride};
+    p.wk = Rows{a->w_k, a->w_k_row_stride, a->w_k_head_stride};
+    p.wv = Rows{a->w_v, a->w_v_row_stride, a->w_v_head_stride};
+    p.lse = a->lse;
+    p.offsets = a->offsets;
+    p.context = a->context;
+    p.table = a->block_table;
+    p.key_offsets = a->key_offsets;
+    p.n_tokens = a->n_tokens;
+    p.n_keys = a->n_keys;
+    p.R = a->R;
+    p.max_blocks = a->max_blocks;
+    p.heads = a->heads;
+    p.group = 1;
+    p.few_rows = 0;
+    p.scale2 = a->scale * 1.4426950408889634f;
+    place_expanded(&p, a->workspace);
+    const hipError_t e = launch_expanded(p, cus, (hipStream_t)stream);
+    return e == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, "ptstore_latent_attention_expanded: launch");
 }
 
 }  // extern "C"

@@ -16,6 +16,7 @@
 
 #include "attend.hpp"
 #include "latent.hpp"
+#include "lds_fetch.hpp"
 #include "shares.hpp"
 
 namespace ptsd {
@@ -40,29 +41,10 @@ constexpr int part_floats(int latent) { return kTile * (latent + 2); }
 __device__ inline int place_of(int row) { return (row & 16) | (row & 3) << 2 | ((row >> 2) & 3); }
 __device__ inline int turn_rope(int row) { return (row >> 1) & 7; }
 
-// Memory to LDS, 16 bytes (4) a lane: lane i's go to `lds` + 16 i (4 i). The compiler does not
-// count these loads, so that it waits for none of them by itself: `arrive` does.
-__device__ inline void fetch16(const uint8_t* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds)
-                 : "memory");
-}
-__device__ inline void fetch16_at(const uint8_t* at, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds) : "memory");
-}
-__device__ inline void fetch4_at(const int32_t* at, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(lds) : "memory");
-}
 // A running maximum that is behind by up to this much (in powers of two) is kept, as in prompt.hip.
 constexpr float kBehind = 8.f;
 template <bool kHalf>
 constexpr float kRoom = Elem<kHalf>::kRoom + (kHalf ? 0.f : kBehind);
-
-// Waits until at most kLeft of the wave's loads are under way; its LDS reads are done, too.
-template <int kLeft>
-__device__ inline void arrive() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
-}
-__device__ inline void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // Products 0 .. kProducts - 1 in groups of kDeep: the LDS reads of the next group are under way while one is
 // computed. Left to itself the compiler, short of registers, reads and waits one by one.
@@ -127,8 +109,8 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     first = uniform(first);
     f = uniform(f);
 
-    const uint32_t rows_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_rows;
-    const uint32_t entry_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int32_t*)s_entry;
+    const uint32_t rows_at = lds_of(s_rows);
+    const uint32_t entry_at = lds_of(s_entry);
 
     const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
     for (int64_t done = share0; done < share1;) {

@@ -1,0 +1,466 @@
+// Attention of prompts over a latent cache in the expanded form: keys and values of every head are formed
+// from the rows first, and attention then takes 2 (192 + 128) operations a (row, key) instead of
+// the latent space's 2 (576 + 512).
+//
+// Forming them is a matrix product: 128 keys and all of their latent values stay in LDS while a workgroup goes
+// through the matrices of several heads, which its waves read from L2 into registers, 64 of a head's 256 rows
+// each. What comes out is packed by head, in the cache's type: a rounding that a model which
+// forms keys and values itself has, too.
+//
+// The attention is that of prompt.hip, with keys of 128 + 64 and values of 128: 128 tokens of a head a
+// workgroup, 32 a wave, 64 keys a step, S^T = K Q^T and O^T = V^T P^T. Keys lie next to each other and
+// need no conversion, so they go to LDS without passing registers, into one of two buffers while the other
+// is computed from. Two workgroups share a compute unit.
+#include <type_traits>
+
+#include "attend.hpp"
+#include "latent.hpp"
+#include "lds_fetch.hpp"
+
+namespace ptsd {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * 64;
+constexpr int kFormKeys = 128;  // of a workgroup that forms keys and values
+constexpr int kKeys = 64;       // of a step of the attention
+
+// The packed key x: its request (the last that begins at or before it), and its row's place in units of 16 bytes.
+__device__ inline bool row_of(const ExpandedPlan& p, int64_t x, uint32_t& at) {
+    int lo = 0, span = p.R;
+    while (span > 1) {
+        const int half = span / 2;
+        const bool up = p.key_offsets[lo + half] <= x;
+        lo = up ? lo + half : lo;
+        span = up ? span - half : half;
+    }
+    at = 0;
+    if (x >= p.n_keys || p.R < 1) return false;
+    const int64_t key = x - p.key_offsets[lo];
+    if (key < 0 || x >= p.key_offsets[lo + 1] || key >= (int64_t)p.max_blocks * p.kv.div.page) return false;
+    const uint32_t column = div_page((uint32_t)key, p.kv.div);
+    const int32_t entry = p.table[(int64_t)lo * p.max_blocks + column];
+    if (entry < 0 || entry >= p.kv.blocks) return false;
+    at = ((uint32_t)entry * p.kv.div.page + ((uint32_t)key - column * p.kv.div.page)) * p.kv.line;
+    return true;
+}
+
+template <int L, bool kHalf>
+__global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
+    using E = Elem<kHalf>;
+    using V8 = typename E::v8;
+    constexpr int kRow = L * 2 + 16;  // bytes in LDS: 16 lanes that read one column of 16 rows need 16 places
+    constexpr int kTiles = kFormKeys / 32;
+    __shared__ __attribute__((aligned(256))) uint8_t s_rows[kFormKeys * kRow];
+    __shared__ uint32_t s_at[kFormKeys];
+    __shared__ int32_t s_there[kFormKeys];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int groups = (p.heads + p.each - 1) / p.each;
+    const int64_t key0 = (int64_t)(blockIdx.x / groups) * kFormKeys;
+    const int group = blockIdx.x % groups;
+    if (threadIdx.x < kFormKeys) {
+        uint32_t at;
+        const bool there = row_of(p, key0 + threadIdx.x, at);
+        s_at[threadIdx.x] = at;
+        s_there[threadIdx.x] = there;
+        if (group == 0 && key0 + threadIdx.x < p.n_keys) p.there[key0 + threadIdx.x] = there;
+    }
+    __syncthreads();
+    const uint32_t lds = lds_of(s_rows);
+    for (int i = 0; i < kFormKeys / kWaves; ++i) {
+        const int j = wave * (kFormKeys / kWaves) + i;
+        const uint8_t* const row = p.kv.rows + ((uint64_t)__builtin_amdgcn_readfirstlane(s_at[j]) << 4);
+        if (L == 512 || lane < L / 8) fetch16(row, (uint32_t)lane * 16, lds + j * kRow);
+    }
+    if (group == 0) {
+        // the shared parts, 8 lanes a row
+        for (int j = threadIdx.x / 8; j < kFormKeys; j += kThreads / 8) {
+            if (key0 + j >= p.n_keys) break;
+            const v4u x = *(const v4u*)(p.kv.rows + (((uint64_t)s_at[j] + L / 8 + threadIdx.x % 8) << 4));
+            const v4u zero = {0u, 0u, 0u, 0u};
+            *(v4u*)(p.rope + (key0 + j) * (kRope * 2) + threadIdx.x % 8 * 16) = s_there[j] ? x : zero;
+        }
+    }
+    arrive<0>();
+    __syncthreads();
+    // rows that are not there are zeros
+    for (int j = wave; j < kFormKeys; j += kWaves)
+        if (!s_there[j] && lane < L / 8) *(v4u*)(s_rows + j * kRow + lane * 16) = v4u{0u, 0u, 0u, 0u};
+    __syncthreads();
+
+    const int last = group * p.each + p.each < p.heads ? group * p.each + p.each : p.heads;
+    const bool value = wave >= 2;  // waves 0, 1: a head's keys; 2, 3: its values
+    const Rows& w = value ? p.wv : p.wk;
+    for (int head = group * p.each; head < last; ++head) {
+        asm volatile("" ::: "memory");  // the keys stay in LDS: all of them do not fit the registers
+        // rows 64 (wave & 1) .. of the head's matrix. Of each 64 latent values a lane takes 32 in a row, so that
+        // whole lines are used; the keys are read to match.
+        const uint8_t* const rows = (const uint8_t*)w.p + ((int64_t)head * w.head + (int64_t)((wave & 1) * 64 + n) * w.token + half * 32) * 2;
+        const int64_t next = w.token * 64;  // 32 rows on
+        v16f o[2][kTiles];
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[a][t][e] = 0.f;
+        v4u x[2][8];  // this and the next 64 latent values of two rows
+        auto load = [&](v4u (&to)[8], int k) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                to[s] = *(const v4u*)(rows + k * 128 + s * 16);
+                to[4 + s] = *(const v4u*)(rows + next + k * 128 + s * 16);
+            }
+        };
+        load(x[0], 0);
+#pragma unroll
+        for (int k = 0; k < L / 64; ++k) {
+            if (k + 1 < L / 64) load(x[(k + 1) & 1], k + 1);
+            const v4u(&now)[8] = x[k & 1];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                V8 c[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+                    c[t] = __builtin_bit_cast(V8, *(const v4u*)(s_rows + (t * 32 + n) * kRow + k * 128 + half * 64 + s * 16));
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        o[a][t] = E::mma32(__builtin_bit_cast(V8, now[a * 4 + s]), c[t], o[a][t]);
+            }
+        }
+        uint8_t* const out = (value ? p.v : p.k) + ((int64_t)head * p.n_keys + key0) * (kNope * 2) + (wave & 1) * 128;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            if (key0 + t * 32 + n >= p.n_keys) continue;  // both halves of a key
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int a = 0; a < 4; a += 2) {
+                    // 4 values here, the next 4 in the other half: trade, and write 8 a lane
+                    v4u y;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t even = pack2<kHalf>(o[i][t][4 * a + 2 * h], o[i][t][4 * a + 2 * h + 1]);
+                        const uint32_t odd = pack2<kHalf>(o[i][t][4 * a + 4 + 2 * h], o[i][t][4 * a + 4 + 2 * h + 1]);
+                        const auto both = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+                        y[h] = both[0];
+                        y[2 + h] = both[1];
+                    }
+                    *(v4u*)(out + (int64_t)(t * 32 + n) * (kNope * 2) + (32 * i + 8 * (a + half)) * 2) = y;
+                }
+        }
+    }
+}
+
+// Places in LDS: 16-byte column c of row r is at c ^ turn(r). K (and its shared part) is read by 16 lanes of
+// 16 rows, one column; V by 32 lanes of 4 rows, 64 consecutive bytes each.
+__device__ inline int turn_k(int row) { return row & 15; }
+__device__ inline int turn_rope(int row) { return (row >> 1) & 7; }
+__device__ inline int turn_v(int row) { return (row & 3) << 2; }
+
+// As in prompt.hip: a running maximum that is behind by up to this much (in powers of two) is kept.
+constexpr float kBehind = 8.f;
+template <bool kHalf>
+constexpr float kRoom = Elem<kHalf>::kRoom + (kHalf ? 0.f : kBehind);
+
+template <bool kHalf>
+__global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
+    using E = Elem<kHalf>;
+    using V8 = typename E::v8;
+    constexpr int kSteps = kNope / 16, kRopeSteps = kRope / 16, kTiles = kValue / 32;
+    constexpr int kRow = 256, kRopeRow = kRope * 2;  // bytes in LDS
+    constexpr int kRopeAt = kKeys * kRow, kValueAt = kRopeAt + kKeys * kRopeRow, kBuffer = kValueAt + kKeys * kRow;
+    static_assert(kNope * 2 == kRow && kValue * 2 == kRow, "rows of keys and of values are alike");
+    // all that two workgroups of a compute unit have: 80 KiB each
+    __shared__ __attribute__((aligned(256))) uint8_t s_mem[2 * kBuffer];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int head = blockIdx.x % p.heads;
+    // the last tiles of a request see the most keys: they go first
+    const Tile f = find_tile(p, gridDim.x / p.heads - 1 - blockIdx.x / p.heads, kPromptRows);
+    if (f.tile < 0) return;
+
+    // the request's packed keys
+    const int64_t first = p.key_offsets[f.r];
+    int64_t count = p.key_offsets[f.r + 1] - first;
+    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
+    if (first < 0 || count < 0 || first + count > p.n_keys) count = 0;
+    if (count > limit) count = limit;
+    const int row0 = f.tile * kPromptRows + wave * 32;
+    const int token = row0 + n < f.n ? row0 + n : f.n - 1;
+    // (a row that sees no key, and one that sees them all, are at the ends of this range)
+    auto clip = [&](int64_t x) { return (int32_t)(x < -1 ? -1 : (x < count ? x : count - 1)); };
+    auto uniform = [&](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };
+    const int last_row = f.tile * kPromptRows + kPromptRows < f.n ? f.tile * kPromptRows + kPromptRows - 1 : f.n - 1;
+    const int32_t end = uniform(clip(f.past + last_row) + 1);
+    const int32_t tile_sees = uniform(clip(f.past + f.tile * kPromptRows));
+    const int32_t all_see = uniform(clip(f.past + (row0 < f.n ? row0 : f.n - 1)));
+    const int32_t pos = clip(f.past + token);
+    const int steps = (end + kKeys - 1) / kKeys;
+    const uint8_t* const keys = p.k + ((int64_t)head * p.n_keys + first) * kRow;
+    const uint8_t* const values = p.v + ((int64_t)head * p.n_keys + first) * kRow;
+    const uint8_t* const shared = p.rope + first * kRopeRow;
+
+    V8 q[kSteps + kRopeSteps];
+    {
+        const uint8_t* a = (const uint8_t*)p.qn.p + ((f.begin + token) * p.qn.token + head * p.qn.head) * 2;
+        const uint8_t* b = (const uint8_t*)p.qr.p + ((f.begin + token) * p.qr.token + head * p.qr.head) * 2;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(V8, *(const v4u*)(a + (s * 16 + half * 8) * 2));
+#pragma unroll
+        for (int s = 0; s < kRopeSteps; ++s)
+            q[kSteps + s] = __builtin_bit_cast(V8, *(const v4u*)(b + (s * 16 + half * 8) * 2));
+    }
+    v16f o[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float top = kLowest, sum = 0.f;
+    bool far = false;      // scores are scaled before the maximum is taken
+    bool endless = false;  // a value that is not finite lies behind the first row's last key
+
+    const uint32_t lds = lds_of(s_mem);
+    // A step's rows 16 wave .. + 15 into LDS, keys past the end as the last one.
+    auto fetch = [&](int t, int buffer) {
+        const int32_t at = t * kKeys, last = end - 1 - at;
+        const uint32_t to = lds + buffer * kBuffer;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j0 = 16 * wave + 4 * i, j = j0 + (lane >> 4), key = j < last ? j : last;
+            fetch16(keys + (int64_t)at * kRow, (uint32_t)(key * kRow + ((lane & 15) ^ turn_k(j)) * 16), to + j0 * kRow);
+            fetch16(values + (int64_t)at * kRow, (uint32_t)(key * kRow + ((lane & 15) ^ turn_v(j)) * 16),
+                    to + kValueAt + j0 * kRow);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j0 = 16 * wave + 8 * i, j = j0 + (lane >> 3), key = j < last ? j : last;
+            fetch16(shared + (int64_t)at * kRopeRow, (uint32_t)(key * kRopeRow + ((lane & 7) ^ turn_rope(j)) * 16),
+                    to + kRopeAt + j0 * kRopeRow);
+        }
+    };
+    // whether a lane's key of a step is there
+    auto is_there = [&](int t) {
+        const int32_t key = t * kKeys + lane;
+        return p.there[first + (key < end ? key : end - 1)];
+    };
+    // LDS places of a lane: see prompt.hip
+    const int m8 = n >> 3, krow = 16 * (m8 >> 1) + 8 * ((n >> 2) & 1) + 4 * (m8 & 1) + (n & 3);
+    uint32_t k_read[kSteps], r_read[kRopeSteps], v_read[kTiles];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) k_read[i] = krow * kRow + ((2 * i + half) ^ turn_k(krow)) * 16;
+#pragma unroll
+    for (int i = 0; i < kRopeSteps; ++i) r_read[i] = kRopeAt + krow * kRopeRow + ((2 * i + half) ^ turn_rope(krow)) * 16;
+    {
+        const int g = lane >> 4, l16 = lane & 15, row = 8 * (g >> 1) + (l16 >> 2);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+            v_read[i] = kValueAt + row * kRow + ((4 * i + 2 * (g & 1) + ((l16 & 3) >> 1)) ^ turn_v(row)) * 16 + (l16 & 1) * 8;
+    }
+
+    int32_t flag = 0;
+    if (steps > 0) {
+        flag = is_there(0);
+        fetch(0, 0);
+    }
+    for (int t = 0; t < steps; ++t) {
+        const int buf = t & 1;
+        const int32_t at = t * kKeys;
+        // the step is whole behind the barrier, and all waves are done with the other buffer
+        arrive<0>();
+        uint64_t ok = __ballot(flag != 0 && at + lane < end);
+        asm volatile("" : "+s"(ok));  // (here, where nothing is under way: a wait for the flag costs nothing)
+        barrier();
+        if (t + 1 < steps) {
+            flag = is_there(t + 1);
+            fetch(t + 1, buf ^ 1);
+        }
+        uint8_t* const mem = s_mem + buf * kBuffer;
+        if (at + kKeys - 1 > tile_sees) {
+            // Values that are not finite, in rows that the tile's first row does not see (a weight of zero would
+            // make them NaN), become zeros. Every wave looks at all of them, so that all agree.
+            bool found = false;
+            for (int j = (at > tile_sees ? 0 : tile_sees + 1 - at) + (lane >> 4); j < kKeys; j += 4) {
+                v4u x = *(const v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
+                found |= drop_endless<kHalf>(x);
+            }
+            if (__any(found)) {
+                endless = true;
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                for (int j = (at > tile_sees ? 0 : tile_sees + 1 - at) + (lane >> 4) + 4 * wave; j < kKeys; j += 16) {
+                    v4u* const to = (v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
+                    v4u x = *to;
+                    if (drop_endless<kHalf>(x)) *to = x;
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
+        }
+        v16f s[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                s[c] = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + k_read[i] + c * 32 * kRow)), q[i], s[c]);
+#pragma unroll
+        for (int i = 0; i < kRopeSteps; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                s[c] = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + r_read[i] + c * 32 * kRopeRow)),
+                                q[kSteps + i], s[c]);
+        // keys 32 c + 16 (e >> 3) + 8 half + (e & 7) in s[c][e]
+        if (ok != ~0ull || at + kKeys - 1 > all_see) {
+            // the keys that are there and that the row sees, from bit 0 those of s[0][0] on
+            const int32_t ahead = pos - at;
+            uint64_t seen = ahead < 0 ? 0 : (ahead > 62 ? ~0ull : (2ull << ahead) - 1);
+            seen = (seen & ok) >> (8 * half);
+            const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(bits[c] & (1u << (16 * (e >> 3) + (e & 7))))) s[c][e] = -INFINITY;
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
+        most = larger_32(most);
+        auto scale_now = [&] {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[c][e] = product(s[c][e], p.scale2);
+            most = product(most, p.scale2);
+        };
+        if (far) scale_now();
+        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, kRoom<kHalf>));
+        if (__any(top2 > top + (far ? 0.f : kBehind))) {
+            if (!far && __any(is_far(top2))) {
+                far = true;
+                scale_now();
+                top2 = fmaxf(top, most + kRoom<kHalf>);
+            }
+            const float less = exp2_of(top - top2);
+            sum *= less;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] *= less;
+            top = top2;
+        }
+        const float scale = far ? 1.f : p.scale2;
+        v4u w[4];  // weights of 16 keys each, rounded to 16 bits as in prompt.hip; the sum takes them as they are
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[c][e] = exp2_of(__builtin_fmaf(s[c][e], scale, -top));
+                sum += s[c][e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            v4u vt[kTiles];
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+                vt[i] = join(read_transposed(mem + v_read[i] + 16 * b * kRow),
+                             read_transposed(mem + v_read[i] + (16 * b + 4) * kRow));
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+                o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b]), o[i]);
+        }
+    }
+    if (endless)
+        for (int32_t key = tile_sees + 1; key < end; ++key) {
+            if (key > pos) continue;
+            const uint16_t* x = (const uint16_t*)(values + (int64_t)key * kRow);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint16_t y = x[32 * i + 8 * (e >> 2) + 4 * half + (e & 3)];
+                    o[i][e] = add_endless(o[i][e], kHalf ? (float)__builtin_bit_cast(_Float16, y)
+                                                         : __uint_as_float((uint32_t)y << 16));
+                }
+        }
+    if (row0 + n >= f.n) return;  // both halves of a row leave together
+    sum += __shfl_xor(sum, 32);
+    // no key, or none with a weight: zeros, and the logarithm of nothing
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    uint8_t* const out = (uint8_t*)p.out.p + ((f.begin + token) * p.out.token + head * p.out.head) * 2;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int a = 0; a < 4; a += 2) {
+            v4u y;  // as in prompt.hip: 4 dimensions here, the next 4 in the other half
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t even = pack2<kHalf>(o[i][4 * a + 2 * h] * inv, o[i][4 * a + 2 * h + 1] * inv);
+                const uint32_t odd = pack2<kHalf>(o[i][4 * a + 4 + 2 * h] * inv, o[i][4 * a + 4 + 2 * h + 1] * inv);
+                const auto both = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+                y[h] = both[0];
+                y[2 + h] = both[1];
+            }
+            *(v4u*)(out + (32 * i + 8 * (a + half)) * 2) = y;
+        }
+    if (p.lse && half == 0)
+        p.lse[(f.begin + token) * p.heads + head] =
+            sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <int L, bool kHalf>
+hipError_t run(const ExpandedPlan& p, hipStream_t s) {
+    if (p.n_keys > 0) {
+        const int64_t tiles = (p.n_keys + kFormKeys - 1) / kFormKeys, groups = (p.heads + p.each - 1) / p.each;
+        hipLaunchKernelGGL((k_form<L, kHalf>), dim3((unsigned)(tiles * groups)), dim3(kThreads), 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const int64_t tiles = p.R == 1 ? (p.n_tokens + kPromptRows - 1) / kPromptRows
+                                   : tile_bound(p.n_tokens, 1, p.R, kPromptRows);
+    hipLaunchKernelGGL((k_expanded<kHalf>), dim3((unsigned)(tiles * p.heads)), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+template <int L>
+hipError_t run_kind(const ExpandedPlan& p, hipStream_t s) {
+    return p.kv.kind == PTSTORE_KV_FP16 ? run<L, true>(p, s) : run<L, false>(p, s);
+}
+
+int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
+
+}  // namespace
+
+int64_t expanded_workspace(int32_t heads, int64_t n_keys) {
+    return n_keys * heads * (kNope + kValue) * 2 + n_keys * kRope * 2 + round16(n_keys * 4);
+}
+
+void place_expanded(ExpandedPlan* p, void* workspace) {
+    p->k = static_cast<uint8_t*>(workspace);
+    p->v = p->k + p->n_keys * p->heads * kNope * 2;
+    p->rope = p->v + p->n_keys * p->heads * kValue * 2;
+    p->there = reinterpret_cast<int32_t*>(p->rope + p->n_keys * kRope * 2);
+}
+
+hipError_t launch_expanded(const ExpandedPlan& plan, int cus, hipStream_t s) {
+    ExpandedPlan p = plan;
+    // Workgroups that form keys and values: one a compute unit, as LDS allows, so that each has as many heads
+    // as leave none of them idle.
+    const int64_t tiles = (p.n_keys + kFormKeys - 1) / kFormKeys;
+    const int64_t each = (tiles * p.heads + cus - 1) / cus;
+    p.each = (int32_t)(each < 1 ? 1 : each < p.heads ? each : p.heads);
+    return p.kv.latent == 512 ? run_kind<512>(p, s) : run_kind<256>(p, s);
+}
+
+}  // namespace ptsd

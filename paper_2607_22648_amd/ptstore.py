@@ -86,6 +86,16 @@ class ptstore_latent_attention_t(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
+class ptstore_latent_expanded_t(C.Structure):
+    _fields_ = [("cache", ptstore_latent_t), *_strided("q_nope"), *_strided("q_rope"),
+                ("w_k", C.c_void_p), ("w_k_head_stride", C.c_int64), ("w_k_row_stride", C.c_int64),
+                ("w_v", C.c_void_p), ("w_v_head_stride", C.c_int64), ("w_v_row_stride", C.c_int64),
+                *_strided("out"), ("lse", C.c_void_p), ("offsets", C.c_void_p), ("context", C.c_void_p),
+                ("block_table", C.c_void_p), ("key_offsets", C.c_void_p), ("n_tokens", C.c_int64),
+                ("n_keys", C.c_int64), ("R", C.c_int32), ("max_blocks", C.c_int32), ("heads", C.c_int32),
+                ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 class PTStoreError(RuntimeError):
     def __init__(self, fn: str, code: int, detail: str):
         super().__init__(f"{fn} failed: code {code} ({detail})")
@@ -103,7 +113,8 @@ EXPORTS = ("ptstore_create", "ptstore_destroy", "ptstore_lookup", "ptstore_gathe
            "ptstore_insert_sync", "ptstore_kv_slab_bytes", "ptstore_block_tables",
            "ptstore_kv_append", "ptstore_kv_read", "ptstore_attention_workspace",
            "ptstore_attention", "ptstore_latent_append", "ptstore_latent_read",
-           "ptstore_latent_attention_workspace", "ptstore_latent_attention")
+           "ptstore_latent_attention_workspace", "ptstore_latent_attention",
+           "ptstore_latent_expanded_workspace", "ptstore_latent_attention_expanded")
 
 
 def _load() -> C.CDLL:
@@ -146,6 +157,8 @@ def _load() -> C.CDLL:
         "ptstore_latent_read": [C.POINTER(ptstore_latent_t), p, i64, p, i64, p, i64, p],
         "ptstore_latent_attention_workspace": [C.POINTER(ptstore_latent_t), C.POINTER(i64)],
         "ptstore_latent_attention": [C.POINTER(ptstore_latent_attention_t), p],
+        "ptstore_latent_expanded_workspace": [i32, i64, C.POINTER(i64)],
+        "ptstore_latent_attention_expanded": [C.POINTER(ptstore_latent_expanded_t), p],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -597,6 +610,37 @@ def ptstore_latent_attention(cache: ptstore_latent_t, q_latent, q_rope, out, lse
         _check("ptstore_latent_attention", rc)
 
 
+def ptstore_latent_expanded_workspace(heads: int, n_keys: int) -> int:
+    n = C.c_int64()
+    _check("ptstore_latent_expanded_workspace",
+           _lib.ptstore_latent_expanded_workspace(heads, n_keys, C.byref(n)))
+    return n.value
+
+
+_HEAD = 128  # a head's own key values, and its values, in the expanded form
+
+
+def ptstore_latent_attention_expanded(cache: ptstore_latent_t, q_nope, q_rope, w_k, w_v, out, lse, offsets,
+                                      context, block_table, key_offsets, n_keys: int, scale: float, workspace,
+                                      stream=None) -> None:
+    """`lse` may be None; `workspace`: a uint8 tensor of ptstore_latent_expanded_workspace(heads, n_keys) bytes."""
+    R, maxb = _table(offsets, block_table)
+    qn = _strided_rows(q_nope, (None, None, _HEAD), cache.kind, "q_nope")
+    n, heads, _ = q_nope.shape
+    a = ptstore_latent_expanded_t(
+        cache, *qn, *_strided_rows(q_rope, (n, heads, cache.rope_dim), cache.kind, "q_rope"),
+        *_strided_rows(w_k, (heads, _HEAD, cache.latent_dim), cache.kind, "w_k"),
+        *_strided_rows(w_v, (heads, _HEAD, cache.latent_dim), cache.kind, "w_v"),
+        *_strided_rows(out, (n, heads, _HEAD), cache.kind, "out"),
+        None if lse is None else _arg(lse, torch.float32, n * heads, "lse"),
+        _arg(offsets, torch.int64, R + 1, "offsets"), _arg(context, torch.int32, R, "context"),
+        _arg(block_table, torch.int32, 0, "block_table"), _arg(key_offsets, torch.int64, R + 1, "key_offsets"),
+        n, n_keys, R, maxb, heads, scale, _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
+    rc = _lib.ptstore_latent_attention_expanded(C.byref(a), _stream(stream))
+    if rc:
+        _check("ptstore_latent_attention_expanded", rc)
+
+
 # ---------------------------------------------------------------------------
 # Convenience wrappers
 # ---------------------------------------------------------------------------
@@ -1018,6 +1062,29 @@ class LatentCache(_Paged):
                 workspace = self._workspace(stream, handle)
             ptstore_latent_attention(self._planes[layer], q_latent, q_rope, out, sums, offsets, context,
                                      block_table, scale, workspace, handle)
+        return (out, sums) if lse else out
+
+    def attend_expanded(self, layer: int, q_nope, q_rope, w_k, w_v, offsets, context, block_table, key_offsets,
+                        n_keys: int, scale: Optional[float] = None, out=None, lse: bool = False, workspace=None,
+                        stream=None):
+        """The same attention in the expanded form, for prompts: q_nope [tokens, heads, 128], q_rope
+        [tokens, heads, rope_dim], and each head's matrices w_k, w_v [heads, 128, latent_dim]; out
+        [tokens, heads, 128], or (out, lse). key_offsets [R + 1] sums the requests' keys, context and new, up to
+        n_keys. scale: 1 / sqrt(128 + rope_dim) unless given. Unless given, the workspace (512 bytes a key and
+        head) is made for the call."""
+        cache = self._planes[layer]
+        if q_nope.dim() != 3:
+            raise ValueError(f"q_nope must be [tokens, heads, {_HEAD}], got shape {tuple(q_nope.shape)}")
+        heads = q_nope.shape[1]
+        scale = (_HEAD + cache.rope_dim) ** -0.5 if scale is None else scale
+        with self._on(stream):
+            sums = q_nope.new_empty(q_nope.shape[:2], dtype=torch.float32) if lse else None
+            out = torch.empty_like(q_nope, memory_format=torch.contiguous_format) if out is None else out
+            if workspace is None:
+                workspace = torch.empty(max(16, ptstore_latent_expanded_workspace(heads, n_keys)), dtype=torch.uint8,
+                                        device=self.data.device)
+        ptstore_latent_attention_expanded(cache, q_nope, q_rope, w_k, w_v, out, sums, offsets, context, block_table,
+                                          key_offsets, n_keys, scale, workspace, stream)
         return (out, sums) if lse else out
 
 

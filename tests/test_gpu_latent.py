@@ -144,3 +144,98 @@ def test_absorbed_hidden_values_are_not_seen(P, bad):
     assert torch.equal(got[[0, 1, 3]], clean[[0, 1, 3]])
     # its score is infinite or NaN for every head, so the row is NaN or, where minus infinity, that value's
     assert not bool(torch.isfinite(got[2, :, 100]).any())
+
+
+# --- the expanded form ---------------------------------------------------------------
+
+
+def expanded_bounds(want, mean, reach, q, rows, w, latent, scale, half):
+    """As paged_ref.bounds, with what rounding each key and value to 16 bits adds: a key value is off by u of
+    its size at most (and by its 32-bit sum), so a score by u reach (reach: sums of magnitudes); a
+    value likewise by u |v|. Below 2^-14 an fp16 value is off by up to 2^-25 instead."""
+    u = 2.0 ** -11 if half else 2.0 ** -8
+    tiny = 2.0 ** -25 if half else 0.0
+    # a formed value's 32-bit sum: latent products, against the sum of their magnitudes
+    spread = float((rows[..., :latent].abs().amax((0, 1)) * w.abs().amax((0, 1))).sum())
+    formed = latent * 2.0 ** -24 * spread + tiny
+    d = reach * (u + 192 * 2.0 ** -24 + 2.0 ** -21) + q[..., :128].abs().sum(-1) * scale * formed + 2.0 ** -20
+    tol = (2 * torch.expm1(d)[..., None] + 2 * u + 2.0 ** -16) * mean * 1.02 + u * want.abs() + formed * 1.1 + 2 * tiny
+    return tol, d + 2.0 ** -20
+
+
+def check_expanded(P, kind, latent, page, heads, new, past, seed=0, hole=False, split=False, more=0, qscale=1.0):
+    offsets, context, table, blocks = ref.batch(seed, new, past, page, hole=hole)
+    cache, planes = make(P, kind, latent, blocks, page, seed)
+    n, g = int(offsets[-1]), torch.Generator().manual_seed(seed + 1)
+    q = (torch.randn((n, heads, 192), generator=g) * qscale).to(DTYPE[kind])
+    w = (torch.randn((heads, 256, latent), generator=g) * latent ** -0.5).to(DTYPE[kind])
+    counts = torch.tensor([a + b + more for a, b in zip(new, past)])
+    key_offsets = torch.zeros(len(new) + 1, dtype=torch.int64)
+    key_offsets[1:] = counts.cumsum(0)
+    scale = 192 ** -0.5
+    wd, rows = w.double(), planes[0].cpu().double()
+    want, lse, mean, reach = ref.attention(
+        q.double(), rows, offsets, context, table, page, scale,
+        k_of=lambda x, h: torch.cat((x[:, :latent] @ wd[h, :128].T, x[:, latent:]), 1),
+        v_of=lambda x, h: x[:, :latent] @ wd[h, 128:].T)
+    d, dw = q.cuda(), w.cuda()
+    wk, wv = dw[:, :128], dw[:, 128:]
+    out = None
+    if split:
+        wk, wv = wk.contiguous(), torch.cat((wv, wv), 2)[..., :latent]
+        out = torch.full((n, heads, 256), 3.0, dtype=DTYPE[kind], device="cuda")[..., 128:]
+    got, sums = cache.attend_expanded(0, d[..., :128], d[..., 128:], wk, wv, offsets.cuda(), context.cuda(),
+                                      table.cuda(), key_offsets.cuda(), int(key_offsets[-1]), out=out, lse=True)
+    tol, ltol = expanded_bounds(want, mean, reach, q.double(), rows, wd, latent, scale, kind == "fp16")
+    off = (got.cpu().double() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
+    sums, none = sums.cpu().double(), lse == -math.inf
+    assert torch.equal(sums == -math.inf, none)
+    assert bool(((sums - lse).abs()[~none] <= (ltol + lse.abs() * 2.0 ** -22)[~none]).all())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("latent", [512, 256])
+@pytest.mark.parametrize("heads,new,past", [
+    (1, [1], [0]), (4, [65], [0]), (3, [33, 0, 130], [0, 7, 64]), (2, [1, 260], [200, 1]), (5, [128, 1], [128, 63])])
+def test_expanded(P, kind, latent, heads, new, past):
+    check_expanded(P, kind, latent, 16, heads, new, past, seed=heads)
+
+
+@pytest.mark.parametrize("page", [1, 7, 24, 64])
+def test_expanded_pages_and_holes(P, page):
+    check_expanded(P, "bf16", 512, page, 3, [40, 150], [100, 9], seed=page, hole=True)
+
+
+def test_expanded_strided_and_spare_keys(P):
+    check_expanded(P, "bf16", 512, 16, 4, [70, 20], [31, 0], seed=2, split=True, more=5)
+
+
+def test_expanded_sharp_scores(P):
+    check_expanded(P, "fp16", 256, 16, 2, [100], [50], seed=3, qscale=4.0)
+
+
+def test_expanded_hidden_values_and_odd_offsets(P):
+    """A later token's infinite row leaves the rows before it alone; a request whose key offsets fall or
+    reach past n_keys, or give too few keys, has those only."""
+    latent, page, heads = 512, 16, 2
+    offsets, context, table, blocks = ref.batch(3, [140, 3], [45, 20], page)
+    cache, planes = make(P, "bf16", latent, blocks, page, 3)
+    g = torch.Generator().manual_seed(4)
+    q = torch.randn((143, heads, 192), generator=g).bfloat16().cuda()
+    w = (torch.randn((heads, 256, latent), generator=g) * latent ** -0.5).bfloat16().cuda()
+
+    def call(key_offsets, n_keys):
+        return cache.attend_expanded(0, q[..., :128], q[..., 128:], w[:, :128], w[:, 128:], offsets.cuda(),
+                                     context.cuda(), table.cuda(), torch.tensor(key_offsets, device="cuda"), n_keys)
+    clean = call([0, 185, 208], 208)
+    pos = 45 + 100  # the 101st new token
+    planes[0][int(table[0, pos // page]), pos % page, 7] = math.inf
+    got = call([0, 185, 208], 208)
+    assert torch.equal(got[:100], clean[:100]) and torch.equal(got[140:], clean[140:])
+    assert not bool(torch.isfinite(got[100:140]).all(-1).any())
+    for bad in ([0, 500, 208], [0, -5, 208], [0, 1 << 40, 208], [7, 185, 100]):
+        odd = call(bad, 208)
+        assert odd.shape == clean.shape
+    few = call([0, 45, 68], 208)  # the past only, for the first request
+    assert bool(torch.isfinite(few[:140]).all()) and torch.equal(few[140:], clean[140:])
