@@ -665,7 +665,7 @@ int ptstore_latent_attention(const ptstore_latent_attention_t *args, void *strea
 
 /*
  * The same attention in the expanded form, for prompts: each head's keys and values are formed from the
- * rows by the head's matrices, in the cache's type, and
+ * rows by the head's matrices, in 32 bits, kept as two values of the cache's type each, and
  *   k_hj = (w_k[h] c_j, p_j),  v_hj = w_v[h] c_j,
  *   out[t][h] = sum_j w_j v_hj / sum_j w_j,  w_j = exp(scale * (q_nope[t][h], q_rope[t][h]) . k_hj).
  * Keys have 128 values of a head's own beside the rope_dim shared ones, values 128. Request r has
@@ -706,7 +706,7 @@ typedef struct {
     int64_t workspace_bytes;
 } ptstore_latent_expanded_t;
 
-/* Bytes of workspace for n_keys keys, 16-byte aligned: 512 a key and head, and 132 a key. Host only.
+/* Bytes of workspace for n_keys keys, 16-byte aligned: 1,024 a key and head, and 132 a key. Host only.
  * Errors: INVALID. */
 int ptstore_latent_expanded_workspace(int32_t heads, int64_t n_keys, int64_t *bytes);
 

@@ -55,7 +55,7 @@ struct ExpandedPlan {
     int32_t R, max_blocks, heads;
     int32_t group, few_rows;  // rows of a token: one a head; no limit
     float scale2;
-    uint8_t *k, *v;   // [head][key][128]
+    uint8_t *k, *v;   // [head][key]: 128 nearest 16-bit values, 128 of what is left
     uint8_t* rope;    // [key][64]
     int32_t* there;   // [key] whether its page exists
     int32_t each;     // heads of a workgroup that forms keys and values

@@ -1,16 +1,19 @@
 // Attention of prompts over a latent cache in the expanded form: keys and values of every head are formed
-// from the rows first, and attention then takes 2 (192 + 128) operations a (row, key) instead of
-// the latent space's 2 (576 + 512).
+// from the rows first, and attention over them takes fewer operations a (row, key) than in the latent space.
+//
+// A formed value lies between the 16-bit ones that products take. Rounded to one of them it would
+// make scores, and the logarithms of their sums, as coarse; so it is kept as two, the nearest and what
+// is left, 2^-16 (2^-22) of it off. Scores take 2 (128 + 128 + 64) operations a (row, key), the outputs
+// 2 (128 + 128), where the latent space has 2 (576 + 512).
 //
 // Forming them is a matrix product: 128 keys and all of their latent values stay in LDS while a workgroup goes
 // through the matrices of several heads, which its waves read from L2 into registers, 64 of a head's 256 rows
-// each. What comes out is packed by head, in the cache's type: a rounding that a model which
-// forms keys and values itself has, too.
+// each. What comes out is packed by head.
 //
-// The attention is that of prompt.hip, with keys of 128 + 64 and values of 128: 128 tokens of a head a
-// workgroup, 32 a wave, 64 keys a step, S^T = K Q^T and O^T = V^T P^T. Keys lie next to each other and
-// need no conversion, so they go to LDS without passing registers, into one of two buffers while the other
-// is computed from. Two workgroups share a compute unit.
+// The attention is that of prompt.hip: 128 tokens of a head a workgroup, 32 a wave, S^T = K Q^T and
+// O^T = V^T P^T. Keys lie next to each other and need no conversion, so they go to LDS without passing
+// registers, 32 a step, into one of two buffers while the other is computed from. Two workgroups share a
+// compute unit.
 #include <type_traits>
 
 #include "attend.hpp"
@@ -23,7 +26,8 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kFormKeys = 128;  // of a workgroup that forms keys and values
-constexpr int kKeys = 64;       // of a step of the attention
+constexpr int kKeys = 32;       // of a step of the attention
+constexpr int kRow = 512;       // bytes of a formed key, or value: 128 nearest values, 128 of what is left
 
 // The packed key x: its request (the last that begins at or before it), and its row's place in units of 16 bytes.
 __device__ inline bool row_of(const ExpandedPlan& p, int64_t x, uint32_t& at) {
@@ -45,13 +49,24 @@ __device__ inline bool row_of(const ExpandedPlan& p, int64_t x, uint32_t& at) {
     return true;
 }
 
+// Two floats to their nearest 16-bit values, and what is left of them to two more (nothing of one that is not
+// finite, or becomes so).
+template <bool kHalf>
+__device__ inline uint32_t split2(float a, float b, uint32_t& left) {
+    const uint32_t near = pack2<kHalf>(a, b);
+    const typename Elem<kHalf>::v2 two = __builtin_bit_cast(typename Elem<kHalf>::v2, near);
+    const float x = a - (float)two[0], y = b - (float)two[1];
+    left = pack2<kHalf>(__builtin_isfinite(x) ? x : 0.f, __builtin_isfinite(y) ? y : 0.f);
+    return near;
+}
+
 template <int L, bool kHalf>
 __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
     using E = Elem<kHalf>;
     using V8 = typename E::v8;
-    constexpr int kRow = L * 2 + 16;  // bytes in LDS: 16 lanes that read one column of 16 rows need 16 places
+    constexpr int kLine = L * 2 + 16;  // bytes in LDS: 16 lanes that read one column of 16 rows need 16 places
     constexpr int kTiles = kFormKeys / 32;
-    __shared__ __attribute__((aligned(256))) uint8_t s_rows[kFormKeys * kRow];
+    __shared__ __attribute__((aligned(256))) uint8_t s_rows[kFormKeys * kLine];
     __shared__ uint32_t s_at[kFormKeys];
     __shared__ int32_t s_there[kFormKeys];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -71,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
     for (int i = 0; i < kFormKeys / kWaves; ++i) {
         const int j = wave * (kFormKeys / kWaves) + i;
         const uint8_t* const row = p.kv.rows + ((uint64_t)__builtin_amdgcn_readfirstlane(s_at[j]) << 4);
-        if (L == 512 || lane < L / 8) fetch16(row, (uint32_t)lane * 16, lds + j * kRow);
+        if (L == 512 || lane < L / 8) fetch16(row, (uint32_t)lane * 16, lds + j * kLine);
     }
     if (group == 0) {
         // the shared parts, 8 lanes a row
@@ -86,7 +101,7 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
     __syncthreads();
     // rows that are not there are zeros
     for (int j = wave; j < kFormKeys; j += kWaves)
-        if (!s_there[j] && lane < L / 8) *(v4u*)(s_rows + j * kRow + lane * 16) = v4u{0u, 0u, 0u, 0u};
+        if (!s_there[j] && lane < L / 8) *(v4u*)(s_rows + j * kLine + lane * 16) = v4u{0u, 0u, 0u, 0u};
     __syncthreads();
 
     const int last = group * p.each + p.each < p.heads ? group * p.each + p.each : p.heads;
@@ -123,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
                 V8 c[kTiles];
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
-                    c[t] = __builtin_bit_cast(V8, *(const v4u*)(s_rows + (t * 32 + n) * kRow + k * 128 + half * 64 + s * 16));
+                    c[t] = __builtin_bit_cast(V8, *(const v4u*)(s_rows + (t * 32 + n) * kLine + k * 128 + half * 64 + s * 16));
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -131,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
                         o[a][t] = E::mma32(__builtin_bit_cast(V8, now[a * 4 + s]), c[t], o[a][t]);
             }
         }
-        uint8_t* const out = (value ? p.v : p.k) + ((int64_t)head * p.n_keys + key0) * (kNope * 2) + (wave & 1) * 128;
+        uint8_t* const out = (value ? p.v : p.k) + ((int64_t)head * p.n_keys + key0) * kRow + (wave & 1) * 128;
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             if (key0 + t * 32 + n >= p.n_keys) continue;  // both halves of a key
@@ -140,16 +155,23 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
 #pragma unroll
                 for (int a = 0; a < 4; a += 2) {
                     // 4 values here, the next 4 in the other half: trade, and write 8 a lane
-                    v4u y;
+                    v4u y, z;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint32_t even = pack2<kHalf>(o[i][t][4 * a + 2 * h], o[i][t][4 * a + 2 * h + 1]);
-                        const uint32_t odd = pack2<kHalf>(o[i][t][4 * a + 4 + 2 * h], o[i][t][4 * a + 4 + 2 * h + 1]);
-                        const auto both = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
-                        y[h] = both[0];
-                        y[2 + h] = both[1];
+                        uint32_t near[2], left[2];
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+                            near[b] = split2<kHalf>(o[i][t][4 * (a + b) + 2 * h], o[i][t][4 * (a + b) + 2 * h + 1], left[b]);
+                        const auto x = __builtin_amdgcn_permlane32_swap(near[0], near[1], false, false);
+                        y[h] = x[0];
+                        y[2 + h] = x[1];
+                        const auto w = __builtin_amdgcn_permlane32_swap(left[0], left[1], false, false);
+                        z[h] = w[0];
+                        z[2 + h] = w[1];
                     }
-                    *(v4u*)(out + (int64_t)(t * 32 + n) * (kNope * 2) + (32 * i + 8 * (a + half)) * 2) = y;
+                    uint8_t* const to = out + (int64_t)(t * 32 + n) * kRow + (32 * i + 8 * (a + half)) * 2;
+                    *(v4u*)to = y;
+                    *(v4u*)(to + kRow / 2) = z;
                 }
         }
     }
@@ -159,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
 // 16 rows, one column; V by 32 lanes of 4 rows, 64 consecutive bytes each.
 __device__ inline int turn_k(int row) { return row & 15; }
 __device__ inline int turn_rope(int row) { return (row >> 1) & 7; }
-__device__ inline int turn_v(int row) { return (row & 3) << 2; }
+__device__ inline int turn_v(int row) { return (row & 3) << 2; }  // (of a row's 32 columns, each 16 by themselves)
 
 // As in prompt.hip: a running maximum that is behind by up to this much (in powers of two) is kept.
 constexpr float kBehind = 8.f;
@@ -171,10 +193,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
     using E = Elem<kHalf>;
     using V8 = typename E::v8;
     constexpr int kSteps = kNope / 16, kRopeSteps = kRope / 16, kTiles = kValue / 32;
-    constexpr int kRow = 256, kRopeRow = kRope * 2;  // bytes in LDS
+    constexpr int kRopeRow = kRope * 2;  // bytes
     constexpr int kRopeAt = kKeys * kRow, kValueAt = kRopeAt + kKeys * kRopeRow, kBuffer = kValueAt + kKeys * kRow;
-    static_assert(kNope * 2 == kRow && kValue * 2 == kRow, "rows of keys and of values are alike");
-    // all that two workgroups of a compute unit have: 80 KiB each
+    static_assert(kNope * 4 == kRow && kValue * 4 == kRow, "rows of keys and of values are alike");
     __shared__ __attribute__((aligned(256))) uint8_t s_mem[2 * kBuffer];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
@@ -224,27 +245,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
     bool endless = false;  // a value that is not finite lies behind the first row's last key
 
     const uint32_t lds = lds_of(s_mem);
-    // A step's rows 16 wave .. + 15 into LDS, keys past the end as the last one.
+    // A step's rows 8 wave .. + 7 into LDS, keys past the end as the last one.
     auto fetch = [&](int t, int buffer) {
         const int32_t at = t * kKeys, last = end - 1 - at;
         const uint32_t to = lds + buffer * kBuffer;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j0 = 16 * wave + 4 * i, j = j0 + (lane >> 4), key = j < last ? j : last;
-            fetch16(keys + (int64_t)at * kRow, (uint32_t)(key * kRow + ((lane & 15) ^ turn_k(j)) * 16), to + j0 * kRow);
-            fetch16(values + (int64_t)at * kRow, (uint32_t)(key * kRow + ((lane & 15) ^ turn_v(j)) * 16),
+        for (int i = 0; i < 4; ++i) {  // two rows of 512 bytes
+            const int j0 = 8 * wave + 2 * i, j = j0 + half, key = j < last ? j : last;
+            fetch16(keys + (int64_t)at * kRow, (uint32_t)(key * kRow + (n ^ turn_k(j)) * 16), to + j0 * kRow);
+            fetch16(values + (int64_t)at * kRow, (uint32_t)(key * kRow + (n ^ turn_v(j)) * 16),
                     to + kValueAt + j0 * kRow);
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int j0 = 16 * wave + 8 * i, j = j0 + (lane >> 3), key = j < last ? j : last;
-            fetch16(shared + (int64_t)at * kRopeRow, (uint32_t)(key * kRopeRow + ((lane & 7) ^ turn_rope(j)) * 16),
-                    to + kRopeAt + j0 * kRopeRow);
-        }
+        const int j0 = 8 * wave, j = j0 + (lane >> 3), key = j < last ? j : last;
+        fetch16(shared + (int64_t)at * kRopeRow, (uint32_t)(key * kRopeRow + ((lane & 7) ^ turn_rope(j)) * 16),
+                to + kRopeAt + j0 * kRopeRow);
     };
     // whether a lane's key of a step is there
     auto is_there = [&](int t) {
-        const int32_t key = t * kKeys + lane;
+        const int32_t key = t * kKeys + n;
         return p.there[first + (key < end ? key : end - 1)];
     };
     // LDS places of a lane: see prompt.hip
@@ -271,7 +289,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
         const int32_t at = t * kKeys;
         // the step is whole behind the barrier, and all waves are done with the other buffer
         arrive<0>();
-        uint64_t ok = __ballot(flag != 0 && at + lane < end);
+        uint32_t ok = (uint32_t)__ballot(flag != 0 && at + n < end);
         asm volatile("" : "+s"(ok));  // (here, where nothing is under way: a wait for the flag costs nothing)
         barrier();
         if (t + 1 < steps) {
@@ -283,14 +301,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
             // Values that are not finite, in rows that the tile's first row does not see (a weight of zero would
             // make them NaN), become zeros. Every wave looks at all of them, so that all agree.
             bool found = false;
-            for (int j = (at > tile_sees ? 0 : tile_sees + 1 - at) + (lane >> 4); j < kKeys; j += 4) {
+            const int j0 = at > tile_sees ? 0 : tile_sees + 1 - at;
+            for (int j = j0 + (lane >> 4); j < kKeys; j += 4) {
                 v4u x = *(const v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
                 found |= drop_endless<kHalf>(x);
             }
             if (__any(found)) {
                 endless = true;
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                for (int j = (at > tile_sees ? 0 : tile_sees + 1 - at) + (lane >> 4) + 4 * wave; j < kKeys; j += 16) {
+                for (int j = j0 + (lane >> 4) + 4 * wave; j < kKeys; j += 16) {
                     v4u* const to = (v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
                     v4u x = *to;
                     if (drop_endless<kHalf>(x)) *to = x;
@@ -298,46 +317,33 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
         }
-        v16f s[2];
+        v16f s;
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                s[c] = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + k_read[i] + c * 32 * kRow)), q[i], s[c]);
+        for (int i = 0; i < 2 * kSteps; ++i)
+            s = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + k_read[i % kSteps] + i / kSteps * (kRow / 2))),
+                         q[i % kSteps], s);
 #pragma unroll
         for (int i = 0; i < kRopeSteps; ++i)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                s[c] = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + r_read[i] + c * 32 * kRopeRow)),
-                                q[kSteps + i], s[c]);
-        // keys 32 c + 16 (e >> 3) + 8 half + (e & 7) in s[c][e]
-        if (ok != ~0ull || at + kKeys - 1 > all_see) {
-            // the keys that are there and that the row sees, from bit 0 those of s[0][0] on
+            s = E::mma32(__builtin_bit_cast(V8, *(const v4u*)(mem + r_read[i])), q[kSteps + i], s);
+        // keys 16 (e >> 3) + 8 half + (e & 7) in s[e]
+        if (ok != ~0u || at + kKeys - 1 > all_see) {
+            // the keys that are there and that the row sees, from bit 0 those of s[0] on
             const int32_t ahead = pos - at;
-            uint64_t seen = ahead < 0 ? 0 : (ahead > 62 ? ~0ull : (2ull << ahead) - 1);
+            uint32_t seen = ahead < 0 ? 0 : (ahead > 30 ? ~0u : (2u << ahead) - 1);
             seen = (seen & ok) >> (8 * half);
-            const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!(bits[c] & (1u << (16 * (e >> 3) + (e & 7))))) s[c][e] = -INFINITY;
+            for (int e = 0; e < 16; ++e)
+                if (!(seen & (1u << (16 * (e >> 3) + (e & 7))))) s[e] = -INFINITY;
         }
         float most = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[c][e]);
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, s[e]);
         most = larger_32(most);
         auto scale_now = [&] {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[c][e] = product(s[c][e], p.scale2);
+            for (int e = 0; e < 16; ++e) s[e] = product(s[e], p.scale2);
             most = product(most, p.scale2);
         };
         if (far) scale_now();
@@ -357,28 +363,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
             top = top2;
         }
         const float scale = far ? 1.f : p.scale2;
-        v4u w[4];  // weights of 16 keys each, rounded to 16 bits as in prompt.hip; the sum takes them as they are
+        v4u w[2];  // weights of 16 keys each, rounded to 16 bits as in prompt.hip; the sum takes them as they are
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[c][e] = exp2_of(__builtin_fmaf(s[c][e], scale, -top));
-                sum += s[c][e];
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                w[2 * c + (e >> 2)][e & 3] = pack2<kHalf>(s[c][2 * e], s[c][2 * e + 1]);
+        for (int e = 0; e < 16; ++e) {
+            s[e] = exp2_of(__builtin_fmaf(s[e], scale, -top));
+            sum += s[e];
         }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
+        for (int e = 0; e < 8; ++e) w[e >> 2][e & 3] = pack2<kHalf>(s[2 * e], s[2 * e + 1]);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {  // 16 keys; the nearest values, then what is left
+            const uint32_t c = (b >> 1) * 16 * kRow + (b & 1) * (kRow / 2);
             v4u vt[kTiles];
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
-                vt[i] = join(read_transposed(mem + v_read[i] + 16 * b * kRow),
-                             read_transposed(mem + v_read[i] + (16 * b + 4) * kRow));
+                vt[i] = join(read_transposed(mem + v_read[i] + c), read_transposed(mem + v_read[i] + c + 4 * kRow));
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
-                o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b]), o[i]);
+                o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b >> 1]), o[i]);
         }
     }
     if (endless)
@@ -443,13 +445,13 @@ int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
 }  // namespace
 
 int64_t expanded_workspace(int32_t heads, int64_t n_keys) {
-    return n_keys * heads * (kNope + kValue) * 2 + n_keys * kRope * 2 + round16(n_keys * 4);
+    return n_keys * heads * 2 * kRow + n_keys * kRope * 2 + round16(n_keys * 4);
 }
 
 void place_expanded(ExpandedPlan* p, void* workspace) {
     p->k = static_cast<uint8_t*>(workspace);
-    p->v = p->k + p->n_keys * p->heads * kNope * 2;
-    p->rope = p->v + p->n_keys * p->heads * kValue * 2;
+    p->v = p->k + p->n_keys * p->heads * kRow;
+    p->rope = p->v + p->n_keys * p->heads * kRow;
     p->there = reinterpret_cast<int32_t*>(p->rope + p->n_keys * kRope * 2);
 }
 

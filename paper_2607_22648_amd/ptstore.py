@@ -1070,7 +1070,7 @@ class LatentCache(_Paged):
         """The same attention in the expanded form, for prompts: q_nope [tokens, heads, 128], q_rope
         [tokens, heads, rope_dim], and each head's matrices w_k, w_v [heads, 128, latent_dim]; out
         [tokens, heads, 128], or (out, lse). key_offsets [R + 1] sums the requests' keys, context and new, up to
-        n_keys. scale: 1 / sqrt(128 + rope_dim) unless given. Unless given, the workspace (512 bytes a key and
+        n_keys. scale: 1 / sqrt(128 + rope_dim) unless given. Unless given, the workspace (1,024 bytes a key and
         head) is made for the call."""
         cache = self._planes[layer]
         if q_nope.dim() != 3:

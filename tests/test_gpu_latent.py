@@ -150,16 +150,17 @@ def test_absorbed_hidden_values_are_not_seen(P, bad):
 
 
 def expanded_bounds(want, mean, reach, q, rows, w, latent, scale, half):
-    """As paged_ref.bounds, with what rounding each key and value to 16 bits adds: a key value is off by u of
-    its size at most (and by its 32-bit sum), so a score by u reach (reach: sums of magnitudes); a
-    value likewise by u |v|. Below 2^-14 an fp16 value is off by up to 2^-25 instead."""
+    """As paged_ref.bounds, with what forming keys and values adds: the sum of `latent` products in 32 bits is off
+    by latent 2^-24 of the sum of their magnitudes, and two 16-bit values leave u u of it (of an fp16 pair at
+    least 2^-25 where the second is that small). Scores move by u u reach and by the keys' sums, outputs by
+    u u |v| and the values'."""
     u = 2.0 ** -11 if half else 2.0 ** -8
     tiny = 2.0 ** -25 if half else 0.0
-    # a formed value's 32-bit sum: latent products, against the sum of their magnitudes
     spread = float((rows[..., :latent].abs().amax((0, 1)) * w.abs().amax((0, 1))).sum())
     formed = latent * 2.0 ** -24 * spread + tiny
-    d = reach * (u + 192 * 2.0 ** -24 + 2.0 ** -21) + q[..., :128].abs().sum(-1) * scale * formed + 2.0 ** -20
-    tol = (2 * torch.expm1(d)[..., None] + 2 * u + 2.0 ** -16) * mean * 1.02 + u * want.abs() + formed * 1.1 + 2 * tiny
+    d = reach * (u * u + 320 * 2.0 ** -24 + 2.0 ** -21) + q[..., :128].abs().sum(-1) * scale * formed + 2.0 ** -20
+    tol = ((2 * torch.expm1(d)[..., None] + u + u * u + 2.0 ** -16) * mean * 1.02 + u * want.abs() + formed * 1.1
+           + 2 * tiny)
     return tol, d + 2.0 ** -20
 
 
