@@ -715,6 +715,116 @@ int ptstore_latent_expanded_workspace(int32_t heads, int64_t n_keys, int64_t *by
 int ptstore_latent_attention_expanded(const ptstore_latent_expanded_t *args, void *stream);
 
 /* ======================================================================
+ * Eviction from a paged or latent cache by accumulated attention weight: a request
+ * that has grown past its budget keeps the tokens that were attended to most. Conventions as for
+ * the paged cache's operators above.
+ *
+ * A layer's weights are floats [cache_blocks][kv_heads][block_tokens] (a latent cache has one head),
+ * a number for each slot of the cache and KV head. Slots of pages that several requests of a call share
+ * hold one request's sums, whichever; their rows must not be evicted in place.
+ * ====================================================================== */
+
+/*
+ * Add to each cached token's weight what a batch's queries gave it: with key j of request r in slot s
+ * and KV head g, over the query rows (token t, head h of g) that see it as in ptstore_attention,
+ *   weights[s][g] = (j < weighed[r] ? weights[s][g] : 0) + sum_t,h exp(scale * q[t][h] . k_j - lse[t][h]).
+ * lse is the attention's own: a row whose lse is minus infinity adds nothing, one whose lse is NaN makes
+ * what it sees NaN. weighed NULL: context, so that new tokens start from nothing; smaller where
+ * tokens behind a loaded prefix have no weights yet. Slots of other tokens are not touched. Weights
+ * are 32-bit sums throughout, off by the rounding of lse and of scores, 2^-23 of their size. The
+ * same inputs give the same bits.
+ */
+typedef struct {
+    ptstore_kv_t kv;
+    const void *q;              /* [n_tokens][q_heads][head_dim], 16-byte aligned rows */
+    int64_t q_token_stride;     /* in elements, multiples of 8 */
+    int64_t q_head_stride;
+    const float *lse;           /* [n_tokens][q_heads] */
+    const int64_t *offsets;     /* [R + 1] */
+    const int32_t *context;     /* [R] */
+    const int32_t *weighed;     /* [R], or NULL */
+    const int32_t *block_table; /* [R][max_blocks] */
+    int64_t n_tokens;
+    int32_t R;
+    int32_t max_blocks;
+    int32_t q_heads;
+    float scale;                /* positive, the attention's */
+    float *weights;             /* [cache_blocks][kv_heads][block_tokens] */
+    void *workspace;            /* as for ptstore_attention */
+    int64_t workspace_bytes;
+} ptstore_weigh_t;
+
+/* The same over a latent cache, with the queries of ptstore_latent_attention. */
+typedef struct {
+    ptstore_latent_t cache;
+    const void *q_latent; /* [n_tokens][heads][latent_dim], 16-byte aligned rows */
+    int64_t q_latent_token_stride;
+    int64_t q_latent_head_stride;
+    const void *q_rope;   /* [n_tokens][heads][rope_dim] */
+    int64_t q_rope_token_stride;
+    int64_t q_rope_head_stride;
+    const float *lse;
+    const int64_t *offsets;
+    const int32_t *context;
+    const int32_t *weighed;
+    const int32_t *block_table;
+    int64_t n_tokens;
+    int32_t R;
+    int32_t max_blocks;
+    int32_t heads;
+    float scale;
+    float *weights;       /* [cache_blocks][block_tokens] */
+    void *workspace;
+    int64_t workspace_bytes;
+} ptstore_latent_weigh_t;
+
+/* Bytes of workspace that weighing a cache of kv_heads heads (a latent one: 1) needs on this device,
+ * 16-byte aligned (about 2 MB): one serves every call. Host only. Errors: INVALID, HIP. */
+int ptstore_weigh_workspace(int32_t kv_heads, int64_t *bytes);
+
+/* Errors: INVALID (as ptstore_attention; 2^22 KV heads or more), HIP. */
+int ptstore_kv_weigh(const ptstore_weigh_t *args, void *stream);
+int ptstore_latent_weigh(const ptstore_latent_weigh_t *args, void *stream);
+
+/*
+ * Keep m = min(n, keep[r], max_keep) of the n = context[r] tokens of each request: in each layer and KV head
+ * by itself the last min(recent, m), and of the others those of largest weight, of equal ones the
+ * first (NaN counts as largest). Their rows, K and V, and weights go, in order, to positions 0 .. m - 1
+ * of the pages of to_table; context_out[r] = m. All else is left as it was. Each entry of to_table that
+ * gets tokens is that of the same column of block_table (in place), or a block that no request of the
+ * call names elsewhere. A token whose page does not exist counts as of least weight and moves nowhere, as does
+ * one whose place in to_table does not exist. `layers` layers alike begin layer_bytes apart (a layer's
+ * V plane follows its K plane, as in ptstore_kv_t).
+ */
+typedef struct {
+    int32_t layers;
+    int32_t R;
+    int32_t max_blocks;
+    int32_t max_keep;           /* at least every keep[r] that is to count; the workspace follows from it */
+    int32_t recent;             /* 0 or more */
+    int64_t layer_bytes;        /* a multiple of 16 */
+    float *weights;             /* [layers][cache_blocks][kv_heads][block_tokens] */
+    const int32_t *context;     /* [R] tokens in the cache */
+    const int32_t *keep;        /* [R] */
+    int32_t *context_out;       /* [R]; not context, nor keep */
+    const int32_t *block_table; /* [R][max_blocks] */
+    const int32_t *to_table;    /* [R][max_blocks]; may be block_table */
+    void *workspace;            /* as for ptstore_attention */
+    int64_t workspace_bytes;
+} ptstore_evict_t;
+
+/* Bytes of workspace: 4 a layer, request, KV head and token that may stay, rounded to 16. Host only.
+ * Errors: INVALID. */
+int ptstore_evict_workspace(int32_t layers, int32_t R, int32_t kv_heads, int32_t max_keep,
+                            int64_t *bytes);
+
+/* `kv`, `cache`: the first layer. Errors: INVALID (sizes out of range; max_blocks * block_tokens > 2^30;
+ * more than 2^23 workgroups: layers * R * kv_heads * planes * 128-byte pieces of a row; a NULL pointer;
+ * a workspace too small), HIP. */
+int ptstore_kv_evict(const ptstore_kv_t *kv, const ptstore_evict_t *args, void *stream);
+int ptstore_latent_evict(const ptstore_latent_t *cache, const ptstore_evict_t *args, void *stream);
+
+/* ======================================================================
  * Tuning and diagnostics: not store operations. Counters, timing, the
  * store's buffers for tests, copy launch shapes, and a bandwidth probe.
  * ====================================================================== */

@@ -16,7 +16,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libptstore.so")
 SOURCES = ["api.hip", "lookup.hip", "copy.hip", "insert.hip", "evict.hip", "probe.hip",
            "paged_api.hip", "tables.hip", "append.hip", "decode.hip", "prompt.hip",
-           "latent_api.hip", "latent_rows.hip", "latent_attend.hip", "latent_prompt.hip"]
+           "latent_api.hip", "latent_rows.hip", "latent_attend.hip", "latent_prompt.hip",
+           "weight_api.hip", "weigh.hip", "keep.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -7,7 +7,6 @@
 #pragma once
 
 #include "paged.hpp"
-#include "ptstore.h"
 
 namespace ptsd {
 

@@ -12,6 +12,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "ptstore.h"
+
 namespace ptsd {
 
 constexpr int kGroup = 32;          // elements that share one exponent
@@ -104,6 +106,7 @@ inline int64_t tile_bound(int64_t n_tokens, int32_t group, int32_t R, int rows) 
     return n_tokens * group / rows + R;
 }
 
+const char* planes_of(const ptstore_kv_t* kv, Planes* out);  // or why not
 hipError_t launch_tables(const TablesPlan& p, hipStream_t s);
 hipError_t launch_append(const Planes& kv, const Rows& k, const Rows& v, const int64_t* slots, int64_t n,
                          hipStream_t s);

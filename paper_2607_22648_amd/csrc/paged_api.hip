@@ -9,15 +9,9 @@
 #include "paged.hpp"
 #include "ptstore.h"
 
-using namespace ptsd;
+namespace ptsd {
 
-namespace {
-
-constexpr int64_t kMaxUnits = kMaxItems / 256 - 8192;  // (tile, KV head) pairs of prompt.hip, and room for
-                                                       // parts of the last ones
-constexpr int64_t kMaxHeads = kMaxItems / 512;         // decode.hip: a workgroup a head at least, 512 threads
-
-int64_t slab_bytes(int32_t kind, int32_t heads, int32_t dim, int32_t page) {
+static int64_t slab_bytes(int32_t kind, int32_t heads, int32_t dim, int32_t page) {
     if (heads < 1 || (dim != 64 && dim != 128) || page < 1 || page > 64) return -1;
     const int64_t rows = (int64_t)heads * page;
     int64_t n;
@@ -50,6 +44,16 @@ const char* planes_of(const ptstore_kv_t* kv, Planes* out) {
     out->kind = kv->kind;
     return nullptr;
 }
+
+}  // namespace ptsd
+
+using namespace ptsd;
+
+namespace {
+
+constexpr int64_t kMaxUnits = kMaxItems / 256 - 8192;  // (tile, KV head) pairs of prompt.hip, and room for
+                                                       // parts of the last ones
+constexpr int64_t kMaxHeads = kMaxItems / 512;         // decode.hip: a workgroup a head at least, 512 threads
 
 // Whether a call's rows go 128 to a tile, or 16. The host knows the average
 // request alone. Behind 4,000 keys, 8 KV heads of 4 query heads (us, joins included):

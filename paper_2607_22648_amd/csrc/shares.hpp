@@ -44,22 +44,22 @@ struct Shares {
     __device__ int64_t of(int64_t x) const { return ((x + 1) * count + all - 1) / all - 1; }
 };
 
-// Sums the batch's work and finds the request `r` that the first (or last) step of
-// share `share` is in, its work and its first step. Every workgroup does so for
+// Sums the batch's work, `of(r)` for each request, and finds the request `r` that the first (or last) step of
+// share `share` of `count` is in, its work and its first step. Every workgroup does so for
 // itself: thread t takes the requests from t ceil(R / threads) on.
-template <int kRows, int kWavesOf, class Plan>
-__device__ inline Shares find_step(const Plan& p, int step_keys, int64_t share, bool last, int& r, Work& f,
-                                   int64_t& first) {
+template <int kWavesOf, class W, class Of>
+__device__ inline Shares find_share(int R, int64_t count, const Of& of, int64_t share, bool last, int& r, W& f,
+                                    int64_t& first) {
     __shared__ int64_t s_sum[kWavesOf], s_first;
     __shared__ int s_r;
-    __shared__ Work s_work;
+    __shared__ W s_work;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int per = (p.R + kWavesOf * 64 - 1) / (kWavesOf * 64);
+    const int per = (R + kWavesOf * 64 - 1) / (kWavesOf * 64);
     const int r0 = threadIdx.x * per;
-    Work w;
+    W w;
     int64_t mine = 0;
-    for (int i = 0; i < per && r0 + i < p.R; ++i) {
-        w = work_of<kRows>(p, r0 + i, step_keys);
+    for (int i = 0; i < per && r0 + i < R; ++i) {
+        w = of(r0 + i);
         mine += w.all();
     }
     int64_t scan = mine;
@@ -69,7 +69,7 @@ __device__ inline Shares find_step(const Plan& p, int step_keys, int64_t share, 
     }
     if (lane == 63) s_sum[wave] = scan;
     __syncthreads();
-    Shares s{0, p.shares};
+    Shares s{0, count};
     int64_t before = 0;
 #pragma unroll
     for (int i = 0; i < kWavesOf; ++i) {
@@ -92,11 +92,18 @@ __device__ inline Shares find_step(const Plan& p, int step_keys, int64_t share, 
         f = s_work;
         return s;
     }
-    while (f = work_of<kRows>(p, r, step_keys), first + f.all() <= at) {
+    while (f = of(r), first + f.all() <= at) {
         first += f.all();
         ++r;
     }
     return s;
+}
+
+template <int kRows, int kWavesOf, class Plan>
+__device__ inline Shares find_step(const Plan& p, int step_keys, int64_t share, bool last, int& r, Work& f,
+                                   int64_t& first) {
+    return find_share<kWavesOf>(
+        p.R, p.shares, [&](int i) { return work_of<kRows>(p, i, step_keys); }, share, last, r, f, first);
 }
 
 }  // namespace ptsd

@@ -96,6 +96,29 @@ class ptstore_latent_expanded_t(C.Structure):
                 ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
+_WEIGHED = [("lse", C.c_void_p), ("offsets", C.c_void_p), ("context", C.c_void_p), ("weighed", C.c_void_p),
+            ("block_table", C.c_void_p), ("n_tokens", C.c_int64), ("R", C.c_int32), ("max_blocks", C.c_int32)]
+_WEIGHTS = [("scale", C.c_float), ("weights", C.c_void_p), ("workspace", C.c_void_p),
+            ("workspace_bytes", C.c_int64)]
+
+
+class ptstore_weigh_t(C.Structure):
+    _fields_ = [("kv", ptstore_kv_t), *_strided("q"), *_WEIGHED, ("q_heads", C.c_int32), *_WEIGHTS]
+
+
+class ptstore_latent_weigh_t(C.Structure):
+    _fields_ = [("cache", ptstore_latent_t), *_strided("q_latent"), *_strided("q_rope"), *_WEIGHED,
+                ("heads", C.c_int32), *_WEIGHTS]
+
+
+class ptstore_evict_t(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("R", C.c_int32), ("max_blocks", C.c_int32), ("max_keep", C.c_int32),
+                ("recent", C.c_int32), ("layer_bytes", C.c_int64), ("weights", C.c_void_p),
+                ("context", C.c_void_p), ("keep", C.c_void_p), ("context_out", C.c_void_p),
+                ("block_table", C.c_void_p), ("to_table", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_int64)]
+
+
 class PTStoreError(RuntimeError):
     def __init__(self, fn: str, code: int, detail: str):
         super().__init__(f"{fn} failed: code {code} ({detail})")
@@ -114,7 +137,9 @@ EXPORTS = ("ptstore_create", "ptstore_destroy", "ptstore_lookup", "ptstore_gathe
            "ptstore_kv_append", "ptstore_kv_read", "ptstore_attention_workspace",
            "ptstore_attention", "ptstore_latent_append", "ptstore_latent_read",
            "ptstore_latent_attention_workspace", "ptstore_latent_attention",
-           "ptstore_latent_expanded_workspace", "ptstore_latent_attention_expanded")
+           "ptstore_latent_expanded_workspace", "ptstore_latent_attention_expanded",
+           "ptstore_weigh_workspace", "ptstore_kv_weigh", "ptstore_latent_weigh",
+           "ptstore_evict_workspace", "ptstore_kv_evict", "ptstore_latent_evict")
 
 
 def _load() -> C.CDLL:
@@ -159,6 +184,12 @@ def _load() -> C.CDLL:
         "ptstore_latent_attention": [C.POINTER(ptstore_latent_attention_t), p],
         "ptstore_latent_expanded_workspace": [i32, i64, C.POINTER(i64)],
         "ptstore_latent_attention_expanded": [C.POINTER(ptstore_latent_expanded_t), p],
+        "ptstore_weigh_workspace": [i32, C.POINTER(i64)],
+        "ptstore_kv_weigh": [C.POINTER(ptstore_weigh_t), p],
+        "ptstore_latent_weigh": [C.POINTER(ptstore_latent_weigh_t), p],
+        "ptstore_evict_workspace": [i32, i32, i32, i32, C.POINTER(i64)],
+        "ptstore_kv_evict": [C.POINTER(ptstore_kv_t), C.POINTER(ptstore_evict_t), p],
+        "ptstore_latent_evict": [C.POINTER(ptstore_latent_t), C.POINTER(ptstore_evict_t), p],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -641,6 +672,80 @@ def ptstore_latent_attention_expanded(cache: ptstore_latent_t, q_nope, q_rope, w
         _check("ptstore_latent_attention_expanded", rc)
 
 
+def ptstore_weigh_workspace(kv_heads: int) -> int:
+    n = C.c_int64()
+    _check("ptstore_weigh_workspace", _lib.ptstore_weigh_workspace(kv_heads, C.byref(n)))
+    return n.value
+
+
+def _weighed(n, heads, cache, kv_heads, lse, offsets, context, weighed, block_table, scale, weights, workspace):
+    """The fields of both weighing structs that follow the queries."""
+    R, maxb = _table(offsets, block_table)
+    return (_arg(lse, torch.float32, n * heads, "lse"), _arg(offsets, torch.int64, R + 1, "offsets"),
+            _arg(context, torch.int32, R, "context"),
+            None if weighed is None else _arg(weighed, torch.int32, R, "weighed"),
+            _arg(block_table, torch.int32, 0, "block_table"), n, R, maxb, heads, scale,
+            _arg(weights, torch.float32, cache.cache_blocks * kv_heads * cache.block_tokens, "weights"),
+            _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
+
+
+def ptstore_kv_weigh(kv: ptstore_kv_t, weights, q, lse, offsets, context, block_table, scale: float, workspace,
+                     weighed=None, stream=None) -> None:
+    """`workspace`: a uint8 tensor of ptstore_weigh_workspace(kv.kv_heads) bytes."""
+    rows = _token_rows(q, kv, None, "q")
+    n, heads, _ = q.shape
+    a = ptstore_weigh_t(kv, *rows, *_weighed(n, heads, kv, kv.kv_heads, lse, offsets, context, weighed, block_table,
+                                             scale, weights, workspace))
+    _check("ptstore_kv_weigh", _lib.ptstore_kv_weigh(C.byref(a), _stream(stream)))
+
+
+def ptstore_latent_weigh(cache: ptstore_latent_t, weights, q_latent, q_rope, lse, offsets, context, block_table,
+                         scale: float, workspace, weighed=None, stream=None) -> None:
+    """`workspace`: a uint8 tensor of ptstore_weigh_workspace(1) bytes."""
+    ql = _strided_rows(q_latent, (None, None, cache.latent_dim), cache.kind, "q_latent")
+    n, heads, _ = q_latent.shape
+    a = ptstore_latent_weigh_t(cache, *ql, *_strided_rows(q_rope, (n, heads, cache.rope_dim), cache.kind, "q_rope"),
+                               *_weighed(n, heads, cache, 1, lse, offsets, context, weighed, block_table, scale,
+                                         weights, workspace))
+    _check("ptstore_latent_weigh", _lib.ptstore_latent_weigh(C.byref(a), _stream(stream)))
+
+
+def ptstore_evict_workspace(layers: int, R: int, kv_heads: int, max_keep: int) -> int:
+    n = C.c_int64()
+    _check("ptstore_evict_workspace", _lib.ptstore_evict_workspace(layers, R, kv_heads, max_keep, C.byref(n)))
+    return n.value
+
+
+def _evict(call, cache, kv_heads, layers, layer_bytes, weights, context, keep, max_keep, recent, block_table,
+           to_table, context_out, workspace, stream) -> None:
+    R, maxb = _rows(block_table, "block_table")
+    if tuple(to_table.shape) != (R, maxb):
+        raise ValueError(f"to_table has shape {tuple(to_table.shape)}, block_table {(R, maxb)}")
+    i32 = torch.int32
+    a = ptstore_evict_t(
+        layers, R, maxb, max_keep, recent, layer_bytes,
+        _arg(weights, torch.float32, layers * cache.cache_blocks * kv_heads * cache.block_tokens, "weights"),
+        _arg(context, i32, R, "context"), _arg(keep, i32, R, "keep"), _arg(context_out, i32, R, "context_out"),
+        _arg(block_table, i32, 0, "block_table"), _arg(to_table, i32, 0, "to_table"),
+        _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
+    _check(call, getattr(_lib, call)(C.byref(cache), C.byref(a), _stream(stream)))
+
+
+def ptstore_kv_evict(kv: ptstore_kv_t, layers: int, layer_bytes: int, weights, context, keep, max_keep: int,
+                     recent: int, block_table, to_table, context_out, workspace, stream=None) -> None:
+    """`workspace`: a uint8 tensor of ptstore_evict_workspace(layers, R, kv.kv_heads, max_keep) bytes."""
+    _evict("ptstore_kv_evict", kv, kv.kv_heads, layers, layer_bytes, weights, context, keep, max_keep, recent,
+           block_table, to_table, context_out, workspace, stream)
+
+
+def ptstore_latent_evict(cache: ptstore_latent_t, layers: int, layer_bytes: int, weights, context, keep,
+                         max_keep: int, recent: int, block_table, to_table, context_out, workspace,
+                         stream=None) -> None:
+    """`workspace`: a uint8 tensor of ptstore_evict_workspace(layers, R, 1, max_keep) bytes."""
+    _evict("ptstore_latent_evict", cache, 1, layers, layer_bytes, weights, context, keep, max_keep, recent,
+           block_table, to_table, context_out, workspace, stream)
+
+
 # ---------------------------------------------------------------------------
 # Convenience wrappers
 # ---------------------------------------------------------------------------
@@ -905,6 +1010,47 @@ class _Paged:
         return slots, positions, held_out, next_free
 
 
+    def weights(self, layers: Optional[Tuple[int, int]] = None) -> torch.Tensor:
+        """Weights of nothing yet, [layers, cache_blocks, kv_heads, block_tokens], for layers[0] .. layers[1] - 1
+        (None: all), which have the same KV heads: what `weigh` takes a layer of, and `evict` all."""
+        a, b = (0, len(self._planes)) if layers is None else layers
+        return torch.zeros((b - a, self.cache_blocks, self._heads_of(a, b), self.block_tokens), dtype=torch.float32,
+                           device=self.data.device)
+
+    def _weigh_workspace(self, heads: int, stream) -> torch.Tensor:
+        """A call's own (2 MB): calls of several threads, and graphs, share none."""
+        with self._on(stream):
+            return torch.empty(ptstore_weigh_workspace(heads), dtype=torch.uint8, device=self.data.device)
+
+    def _heads_of(self, a: int, b: int) -> int:
+        """The KV heads of layers a .. b - 1, which have to be alike."""
+        if not 0 <= a < b <= len(self._planes):
+            raise ValueError(f"layers {a} .. {b} of {len(self._planes)}")
+        heads = {getattr(p, "kv_heads", 1) for p in self._planes[a:b]}
+        if len(heads) > 1:
+            raise ValueError(f"layers {a} .. {b} differ in KV heads: {sorted(heads)}")
+        return heads.pop()
+
+    def evict(self, weights, context, block_table, keep, max_keep: int, recent: int = 0, to=None,
+              layers: Optional[Tuple[int, int]] = None, workspace=None, stream=None):
+        """Keep of each request the last `recent` tokens and those of largest weight, keep[r] (at most max_keep) in
+        all, by layer and KV head; their rows and weights go to the front of the pages of `to` (None: in place).
+        Returns the tokens that each request has then. weights: [layers, cache_blocks, kv_heads, block_tokens] of
+        the layers layers[0] .. layers[1] - 1 (None: all), which have the same KV heads."""
+        a, b = (0, len(self._planes)) if layers is None else layers
+        heads = self._heads_of(a, b)
+        first = self._planes[a]
+        with self._on(stream):
+            after = torch.empty_like(context)
+            if workspace is None:
+                need = ptstore_evict_workspace(b - a, block_table.shape[0], heads, max_keep)
+                workspace = torch.empty(max(16, need), dtype=torch.uint8, device=self.data.device)
+        call = ptstore_kv_evict if isinstance(first, ptstore_kv_t) else ptstore_latent_evict
+        call(first, b - a, self._layer_bytes(a), weights, context, keep, max_keep, recent, block_table,
+             block_table if to is None else to, after, workspace, stream)
+        return after
+
+
 class PagedCache(_Paged):
     """A paged cache [layer][K|V][cache block][slab] on the current device, and the
     operators on it. ``data`` is what the store's loads and ``scatter`` take; a store
@@ -951,6 +1097,10 @@ class PagedCache(_Paged):
     def _workspace_bytes(self) -> int:
         return max(ptstore_attention_workspace(kv) for kv in self._planes)
 
+    def _layer_bytes(self, layer: int) -> int:
+        kv = self._planes[layer]
+        return 2 * kv.cache_blocks * ptstore_kv_slab_bytes(kv.kind, kv.kv_heads, kv.head_dim, kv.block_tokens)
+
     def append(self, layer: int, k, v, slots, stream=None) -> None:
         """Write k, v [tokens, kv_heads, head_dim] to `slots` of a layer."""
         ptstore_kv_append(self._planes[layer], k, v, slots, stream)
@@ -996,6 +1146,18 @@ class PagedCache(_Paged):
                            offsets, context, block_table, scale, workspace, handle)
         return (out, sums) if lse else out
 
+    def weigh(self, layer: int, weights, q, lse, offsets, context, block_table, scale: Optional[float] = None,
+              weighed=None, workspace=None, stream=None):
+        """Add to `weights` [cache_blocks, kv_heads, block_tokens] (or [1, ...]) of a layer the attention weights
+        that q [tokens, q_heads, head_dim] gave to its tokens, with the lse and the scale of that attention; returns
+        them. weighed [R]: how many of a request's tokens have weights (None: those of its context)."""
+        kv = self._planes[layer]
+        if workspace is None:
+            workspace = self._weigh_workspace(kv.kv_heads, stream)
+        ptstore_kv_weigh(kv, weights, q, lse, offsets, context, block_table,
+                         self._scale if scale is None else scale, workspace, weighed, stream)
+        return weights
+
 
 class LatentCache(_Paged):
     """A paged cache of latent rows, [layer][cache block][slot][latent_dim + rope_dim], on the current
@@ -1034,6 +1196,10 @@ class LatentCache(_Paged):
 
     def _workspace_bytes(self) -> int:
         return ptstore_latent_attention_workspace(self._planes[0])
+
+    def _layer_bytes(self, layer: int) -> int:
+        c = self._planes[layer]
+        return 2 * c.cache_blocks * c.block_tokens * (c.latent_dim + c.rope_dim)
 
     def append(self, layer: int, latent, rope, slots, stream=None) -> None:
         """Write latent [tokens, latent_dim] and rope [tokens, rope_dim] to `slots` of a layer."""
@@ -1086,6 +1252,15 @@ class LatentCache(_Paged):
         ptstore_latent_attention_expanded(cache, q_nope, q_rope, w_k, w_v, out, sums, offsets, context, block_table,
                                           key_offsets, n_keys, scale, workspace, stream)
         return (out, sums) if lse else out
+
+    def weigh(self, layer: int, weights, q_latent, q_rope, lse, offsets, context, block_table, scale: float,
+              weighed=None, workspace=None, stream=None):
+        """As PagedCache.weigh, with the queries of `attend`; weights [cache_blocks, 1, block_tokens]."""
+        if workspace is None:
+            workspace = self._weigh_workspace(1, stream)
+        ptstore_latent_weigh(self._planes[layer], weights, q_latent, q_rope, lse, offsets, context, block_table,
+                             scale, workspace, weighed, stream)
+        return weights
 
 
 class _CudaArray:
