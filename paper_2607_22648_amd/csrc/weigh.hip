@@ -1,16 +1,19 @@
 // The attention weights that a batch's queries gave to each cached token, added to what it had:
 //   weight(j) += sum over rows that see key j of exp(scale q . k_j - lse).
 //
-// S = Q K^T, 32 x 32 at a time with keys as columns: a lane holds one key's scores of 16 rows, so that
+// S = Q K^T, 16 x 16 at a time with keys as columns: a lane holds one key's scores of 4 rows, so that
 // sums over rows stay in the lane, and no weight is ever rounded. Few rows are bound by reading K once;
 // many by the matrix units and the exponentials (16 cycles of a wave for 64, as long as
-// 2 dim operations of 32 rows take for dim 128), which two waves a SIMD overlap.
+// 2 dim operations of a row take for dim 128), which the waves of a SIMD overlap.
 //
 // A workgroup of four waves takes a tile of keys, 64 a wave (32 of a latent cache), as registers of the
 // second factor, and goes through the query rows that see it, 32 at a time, which pass through LDS for
-// all four. (Key tile, 32 rows) items of the batch, those above the diagonal left out, are laid end to end and
+// all four. Where 32 are all that a request has they stay there, and the waves go from tile to tile by
+// themselves. (Key tile, 32 rows) items of the batch, those above the diagonal left out, are laid end to end and
 // cut into equal shares, as decode.hip's steps; a tile of more than 16 items may be cut, and a second kernel
 // adds what its shares found, in order: the same inputs give the same bits.
+#include <type_traits>
+
 #include "attend.hpp"
 #include "lds_fetch.hpp"
 #include "shares.hpp"
@@ -47,7 +50,8 @@ struct Items {
     }
 };
 
-__device__ inline Items items_of(const WeighPlan& p, int r, int keys) {
+// (of a request that has one row tile, or several: the others have none)
+__device__ inline Items items_of(const WeighPlan& p, int r, int keys, bool stream) {
     Items w;
     int64_t a = p.offsets[r], b = p.offsets[r + 1];
     const bool ok = a >= 0 && b > a && b <= p.n_tokens;
@@ -64,6 +68,7 @@ __device__ inline Items items_of(const WeighPlan& p, int r, int keys) {
     end = w.n == 0 ? 0 : end > limit ? limit : end;
     w.tiles = (int32_t)((end + keys - 1) / keys);
     w.rows = (int32_t)(((int64_t)w.n * p.group + kRowsOf - 1) / kRowsOf);
+    if ((w.rows == 1) != stream) w.tiles = 0;
     w.seen = (int32_t)(past / keys);
     w.rise = (int64_t)(keys / kRowsOf) * p.group;
     w.late = (past % keys * p.group + kRowsOf - 1) / kRowsOf;
@@ -100,93 +105,113 @@ __device__ inline void put_weight(const WeighPlan& p, int r, int head, int32_t k
     p.weights[at] = key < had ? p.weights[at] + sum : sum;
 }
 
-// kDim: of a row; kLayout: how keys are kept.
-template <int kDim, bool kHalf, int kLayout>
-__global__ __launch_bounds__(kThreads, 2) void k_weigh(WeighPlan p) {
+// Waves of a SIMD: as many as the registers hold.
+constexpr int weigh_waves(int dim) { return dim == 576 ? 2 : 3; }
+
+// kDim: of a row; kLayout: how keys are kept; kStream: requests of one row tile, else those of several.
+template <int kDim, int kLayout>
+struct WeighShape {
+    static constexpr int kColumns = kDim / 8;  // 16-byte columns of a row
+    // Rows in LDS are padded by a column, so that 16 lanes which read one column of 16 rows find 16 places; the
+    // shared parts of latent queries, which come eight rows to a load, are turned instead.
+    static constexpr int kOwn = kLayout == kLatent ? kColumns - kRope / 8 : kColumns;  // columns before the shared part
+    static constexpr int kRow = kOwn * 16 + 16, kRopeRow = kRope * 2;
+    static constexpr int kBuffer = kRowsOf * (kRow + (kLayout == kLatent ? kRopeRow : 0));
+};
+
+template <int kDim, bool kHalf, int kLayout, bool kStream>
+__device__ inline void weigh(const WeighPlan& p, int block, uint8_t (&s_q)[2][WeighShape<kDim, kLayout>::kBuffer],
+                             float (&s_lse)[2][kRowsOf]) {
+    using Shape = WeighShape<kDim, kLayout>;
     using E = Elem<kHalf>;
     using V8 = typename E::v8;
     constexpr bool kFour = kLayout == 1;
-    constexpr int kTile = keys_of(kLayout), kChunks = kTile / kWaves / 32;
-    constexpr int kSteps = kDim / 16, kColumns = kDim / 8;  // matrix steps; 16-byte columns of a row
-    // Of a row, or of each part of a latent one, a lane takes half, so that whole lines are read: queries in LDS
-    // likewise. Rows in LDS are padded by a column, so that 16 lanes which read one column of 16 rows find 16
-    // places; the shared parts of latent queries, which come eight rows to a load, are turned instead.
-    constexpr int kOwn = kLayout == kLatent ? kSteps - kRope / 16 : kSteps;  // steps before the shared part
-    constexpr int kRow = kOwn * 32 + 16, kRopeRow = kRope * 2;
+    constexpr int kTile = keys_of(kLayout), kGroups = kTile / kWaves / 16;  // of a wave, 16 keys each
+    constexpr int kSteps = kDim / 32, kColumns = Shape::kColumns;  // matrix steps
+    constexpr int kOwn = Shape::kOwn, kRow = Shape::kRow, kRopeRow = Shape::kRopeRow;
     constexpr int kPieces = kLayout == kLatent ? 1 : kRowsOf * kColumns / kThreads;  // of queries, a thread
-    constexpr int kBuffer = kRowsOf * (kRow + (kLayout == kLatent ? kRopeRow : 0));
-    __shared__ __attribute__((aligned(16))) uint8_t s_q[2][kBuffer];
-    __shared__ float s_lse[2][kRowsOf];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % p.kv.heads, share = blockIdx.x / p.kv.heads;
+    const int n = lane & 15, h4 = lane >> 4;  // key column, quarter
+    const int head = block % p.kv.heads, share = block / p.kv.heads;
     int r;
     int64_t first;
     Items f;
     const Shares shares = find_share<kWaves>(
-        p.R, p.shares, [&](int i) { return items_of(p, i, kTile); }, share, false, r, f, first);
+        p.R, kStream ? p.streams : p.shares, [&](int i) { return items_of(p, i, kTile, kStream); }, share, false, r, f, first);
     if (share >= shares.count) return;
     const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
     for (int64_t done = share0; done < share1;) {
         while (done >= first + f.all()) {
             first += f.all();
-            f = items_of(p, ++r, kTile);
+            f = items_of(p, ++r, kTile, kStream);
         }
-        const int32_t tile = tile_of(f, done - first);
-        const int64_t tile0 = first + f.before(tile), tile1 = first + f.before(tile + 1);
-        if (f.rows <= kWhole && done > tile0) {  // the share before has all of it
+        const int32_t tile = kStream ? (int32_t)(done - first) : tile_of(f, done - first);
+        const int64_t tile0 = kStream ? done : first + f.before(tile), tile1 = kStream ? done + 1 : first + f.before(tile + 1);
+        if (!kStream && f.rows <= kWhole && done > tile0) {  // the share before has all of it
             done = tile1;
             continue;
         }
-        const int32_t row_first = f.first_row(tile);
+        const int32_t row_first = kStream ? 0 : f.first_row(tile);
         const int32_t rt0 = row_first + (int32_t)(done - tile0);
         const int64_t stop = f.rows <= kWhole || tile1 < share1 ? tile1 : share1;
         const int32_t rt1 = row_first + (int32_t)(stop - tile0);
         const bool part = done > tile0 || stop < tile1;
-        float* const to = p.parts + (2 * (int64_t)blockIdx.x + (done > tile0 ? 0 : 1)) * kTile;
+        float* const to = p.parts + (2 * (int64_t)block + (done > tile0 ? 0 : 1)) * kTile;
         done = stop;
 
         const int64_t limit64 = (int64_t)p.max_blocks * p.kv.div.page;
         const int64_t end64 = (int64_t)f.past + f.n < limit64 ? (int64_t)f.past + f.n : limit64;
         const int32_t end = (int32_t)end64;
-        const int32_t k0 = tile * kTile + wave * (32 * kChunks);
+        const int32_t k0 = tile * kTile + wave * (16 * kGroups);
         const int all_rows = f.n * p.group;
         const int32_t* const table = p.table + (int64_t)r * p.max_blocks;
+        const int32_t had = p.weighed ? p.weighed[r] : p.context[r];  // tokens that have weights
 
-        // keys: column n, kSteps columns of 8 values a lane
-        V8 k[kChunks][kSteps];
+        // Keys: column n of a group; 8 consecutive values of each 32 a lane, or (4 bits) a quarter of the row. Four
+        // lanes so read 64 bytes of a row at once.
+        auto entry_of = [&](int32_t key) {
+            return table[div_page((uint32_t)(key < end ? key : end - 1), p.kv.div)];
+        };
+        auto slot_of = [&](int32_t key) { return (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page; };
+        auto is_there = [&](int32_t entry, int32_t key) {
+            return key < end && entry >= 0 && entry < (int32_t)p.kv.blocks;
+        };
+        auto load_key = [&](V8 (&to)[kSteps], int32_t entry, int32_t key) {
+            const bool there = is_there(entry, key);
+            const uint32_t page = there ? (uint32_t)entry : 0u, slot = there ? slot_of(key) : 0u;
+            const uint32_t line = head * p.kv.div.page + slot;
+            if constexpr (kFour) {
+                const uint8_t* row = p.kv.k + (uint64_t)page * p.kv.slab + (uint64_t)line * (kDim / 2) + h4 * (kDim / 8);
+                const float step = step_of(p.kv.k[(uint64_t)page * p.kv.slab + p.kv.exponents +
+                                                  (uint64_t)line * (kDim / kGroup) + h4 * (kDim / 4) / kGroup]);
+                uint32_t codes[kSteps];
+                if constexpr (kSteps == 4)
+                    *(v4u*)codes = *(const v4u*)row;
+                else
+                    *(v2u*)codes = *(const v2u*)row;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int32_t key = k0 + 32 * c + n, last = end - 1;
-            const int32_t entry = table[div_page((uint32_t)(key < last ? key : last), p.kv.div)];
-            const bool there = key < end && entry >= 0 && entry < (int32_t)p.kv.blocks;
-            const uint32_t block = there ? (uint32_t)entry : 0u;
-            const uint32_t slot = there ? (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page : 0u;
-            if constexpr (kLayout == kLatent) {
-                const uint8_t* row = p.latent.rows + ((uint64_t)((block * p.kv.div.page + slot) * p.latent.line) << 4);
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i)
-                    k[c][i] = __builtin_bit_cast(V8, *(const v4u*)(row + (i < kOwn ? i + kOwn * half : i + kOwn + (kSteps - kOwn) * half) * 16));
+                for (int i = 0; i < kSteps; ++i) to[i] = __builtin_bit_cast(V8, widen8(codes[i], step));
             } else {
-                const uint32_t line = head * p.kv.div.page + slot;
-                if constexpr (kFour) {
-                    const uint8_t* row = p.kv.k + (uint64_t)block * p.kv.slab + (uint64_t)line * (kDim / 2) + half * (kDim / 4);
-                    const uint8_t* power = p.kv.k + (uint64_t)block * p.kv.slab + p.kv.exponents +
-                                           (uint64_t)line * (kDim / kGroup) + half * (kDim / 2 / kGroup);
+                const uint8_t* row =
+                    kLayout == kLatent
+                        ? p.latent.rows + ((uint64_t)((page * p.kv.div.page + slot) * p.latent.line) << 4)
+                        : p.kv.k + (uint64_t)page * p.kv.slab + (uint64_t)line * (kDim * 2);
 #pragma unroll
-                    for (int g = 0; g < kSteps / 4; ++g) {
-                        const v4u codes = *(const v4u*)(row + g * 16);
-                        const float step = step_of(power[g]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) k[c][4 * g + i] = __builtin_bit_cast(V8, widen8(codes[i], step));
-                    }
-                } else {
-                    const uint8_t* row = p.kv.k + (uint64_t)block * p.kv.slab + (uint64_t)line * (kDim * 2) + half * kDim;
-#pragma unroll
-                    for (int i = 0; i < kSteps; ++i) k[c][i] = __builtin_bit_cast(V8, *(const v4u*)(row + i * 16));
-                }
+                for (int i = 0; i < kSteps; ++i) to[i] = __builtin_bit_cast(V8, *(const v4u*)(row + (4 * i + h4) * 16));
             }
+        };
+        auto weight_of = [&](int32_t entry, int32_t key) {
+            return p.weights + ((int64_t)entry * p.kv.heads + head) * p.kv.div.page + slot_of(key);
+        };
+
+        V8 k[kGroups][kSteps];
+        int32_t entry[kGroups];
+        if constexpr (!kStream) {
+#pragma unroll
+            for (int c = 0; c < kGroups; ++c) entry[c] = entry_of(k0 + 16 * c + n);
+#pragma unroll
+            for (int c = 0; c < kGroups; ++c) load_key(k[c], entry[c], k0 + 16 * c + n);
         }
 
         v4u piece[kPieces];
@@ -196,12 +221,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_weigh(WeighPlan p) {
         auto load = [&](int rt, int buffer) {
             auto place = [&](int j, int& token, int& sub) {
                 const int row = rt * kRowsOf + j < all_rows ? rt * kRowsOf + j : all_rows - 1;
-                token = row / p.group;
+                token = (int)div_page((uint32_t)row, p.rows_div);
                 sub = row - token * p.group;
             };
             int token, sub;
             if constexpr (kLayout == kLatent) {
-                place(n, token, sub);
+                place(lane & 31, token, sub);
                 const int64_t own = (f.begin + token) * p.q.token + (int64_t)sub * p.q.head;
                 const int64_t shared = (f.begin + token) * p.qr.token + (int64_t)sub * p.qr.head;
                 const uint32_t to = lds_of(s_q[buffer]);
@@ -210,7 +235,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_weigh(WeighPlan p) {
                     const int j = wave * (kRowsOf / kWaves) + i;
                     const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)own, j) |
                                        (int64_t)__builtin_amdgcn_readlane((int)(own >> 32), j) << 32;
-                    if (lane < kOwn * 2) fetch16((const uint8_t*)p.q.p + at * 2, (uint32_t)lane * 16, to + j * kRow);
+                    if (lane < kOwn) fetch16((const uint8_t*)p.q.p + at * 2, (uint32_t)lane * 16, to + j * kRow);
                 }
                 const int j = wave * 8 + (lane >> 3);
                 const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * j, (int)shared) |
@@ -243,64 +268,118 @@ __global__ __launch_bounds__(kThreads, 2) void k_weigh(WeighPlan p) {
                 }
             }
             if (threadIdx.x < kRowsOf) s_lse[buffer][threadIdx.x] = lse;
-            arrive<0>();
+            if (kLayout == kLatent) arrive<0>();
         };
 
-        float total[kChunks], sum[kChunks];  // sums of sums: an error of few of them, not of all
+        // Adds to `sum` what row tile rt gives to the keys of kOf groups from `key0` on.
+        auto rows_of = [&](auto groups, const V8 (*k)[kSteps], int32_t key0, int32_t rt, int buffer, float* sum) {
+            constexpr int kOf = decltype(groups)::value;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) total[c] = sum[c] = 0.f;
-        __syncthreads();  // all are done with the tile before
-        load(rt0, 0);
-        store(0);
-        __syncthreads();
-        for (int32_t rt = rt0; rt < rt1; ++rt) {
-            const int buffer = (rt - rt0) & 1;
-            if (rt + 1 < rt1) load(rt + 1, buffer ^ 1);
-            const uint8_t* const mem = s_q[buffer] + n * kRow + half * (kOwn * 16);
-            v16f s[kChunks];
+            for (int up = 0; up < 2; ++up) {
+                const int row0 = rt * kRowsOf + 16 * up;
+                if (up && row0 >= all_rows) break;
+                const uint8_t* const mem = s_q[buffer] + (n + 16 * up) * kRow;
+                const uint8_t* const shared = s_q[buffer] + kRowsOf * kRow + (n + 16 * up) * kRopeRow;
+                v4f s[kOf];
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c)
+                for (int c = 0; c < kOf; ++c) s[c] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
+                for (int i = 0; i < kSteps; ++i) {
+                    const uint8_t* const at = 4 * i >= kOwn ? shared + ((4 * i - kOwn + h4) ^ ((n >> 1) & 7)) * 16
+                                              : mem + (kFour ? h4 * kSteps + i : 4 * i + h4) * 16;
+                    const V8 q = __builtin_bit_cast(V8, *(const v4u*)at);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const uint8_t* const at = i < kOwn ? mem + i * 16
-                                                   : s_q[buffer] + kRowsOf * kRow + n * kRopeRow +
-                                                         ((i - kOwn + (kSteps - kOwn) * half) ^ ((n >> 1) & 7)) * 16;
-                const V8 q = __builtin_bit_cast(V8, *(const v4u*)at);
+                    for (int c = 0; c < kOf; ++c) s[c] = E::mma16(q, k[c][i], s[c]);
+                }
+                // rows 4 h4 + e in s[..][e]
+                const v4f less = *(const v4f*)&s_lse[buffer][16 * up + 4 * h4];
+                const bool edge = key0 + 16 * kOf - 1 > (int64_t)f.past + div_page((uint32_t)row0, p.rows_div);  // the first row's last key
+                float w[kOf][4];
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) s[c] = E::mma32(q, k[c][i], s[c]);
-            }
-            // rows 8 (e >> 2) + 4 half + (e & 3) in s[..][e]
-            const int64_t sees = (int64_t)f.past + rt * kRowsOf / p.group;  // the first row's last key
-            const bool edge = k0 + 32 * kChunks - 1 > sees;
-            float weight[kChunks] = {};
+                for (int c = 0; c < kOf; ++c)
 #pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const v4f less = *(const v4f*)&s_lse[buffer][8 * a + 4 * half];
-                float w[kChunks][4];
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[c][e] = exp2_of(__builtin_fmaf(s[c][4 * a + e], p.scale2, -less[e]));
+                    for (int e = 0; e < 4; ++e) w[c][e] = exp2_of(__builtin_fmaf(s[c][e], p.scale2, -less[e]));
                 if (edge) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int row = rt * kRowsOf + 8 * a + 4 * half + e;
-                        const int64_t pos = (int64_t)f.past + row / p.group;
+                        const int64_t pos = (int64_t)f.past + div_page((uint32_t)(row0 + 4 * h4 + e), p.rows_div);
 #pragma unroll
-                        for (int c = 0; c < kChunks; ++c)
-                            if (k0 + 32 * c + n > pos) w[c][e] = 0.f;
+                        for (int c = 0; c < kOf; ++c)
+                            if (key0 + 16 * c + n > pos) w[c][e] = 0.f;
                     }
                 }
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) weight[c] += (w[c][0] + w[c][1]) + (w[c][2] + w[c][3]);
+                for (int c = 0; c < kOf; ++c) sum[c] += (w[c][0] + w[c][1]) + (w[c][2] + w[c][3]);
             }
+        };
+
+        float total[kGroups], sum[kGroups];  // sums of sums: an error of few of them, not of all
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) sum[c] += weight[c];
+        for (int c = 0; c < kGroups; ++c) total[c] = sum[c] = 0.f;
+        __syncthreads();  // all are done with the rows before
+        load(rt0, 0);
+        store(0);
+        __syncthreads();
+        if constexpr (kStream) {
+            // The share's tiles of this request, in halves: the next half's keys are on their way while one is
+            // computed, and page entries before them.
+            constexpr int kOf = kGroups / 2;
+            const int64_t left = first + f.all() < share1 ? first + f.all() - tile0 : share1 - tile0;
+            const int32_t halves = 2 * (int32_t)left;
+            done = tile0 + left;
+            auto key_of = [&](int32_t x) { return (tile + x / 2) * kTile + wave * (16 * kGroups) + x % 2 * (16 * kOf); };
+            V8(&half)[2][kOf][kSteps] = *reinterpret_cast<V8(*)[2][kOf][kSteps]>(&k);
+            int32_t at[3][kOf];  // page entries of three halves
+            float old[2][kOf];
+            auto look = [&](int32_t x, int32_t (&to)[kOf]) {
+#pragma unroll
+                for (int c = 0; c < kOf; ++c) to[c] = entry_of(key_of(x) + 16 * c + n);
+            };
+            auto fetch = [&](int32_t x, const int32_t (&entry)[kOf], V8 (&to)[kOf][kSteps], float (&was)[kOf]) {
+#pragma unroll
+                for (int c = 0; c < kOf; ++c) load_key(to[c], entry[c], key_of(x) + 16 * c + n);
+#pragma unroll
+                for (int c = 0; c < kOf; ++c) {
+                    const int32_t key = key_of(x) + 16 * c + n;
+                    was[c] = is_there(entry[c], key) && key < had ? *weight_of(entry[c], key) : 0.f;
+                }
+            };
+            auto turn = [&](auto b, int32_t x) {
+                constexpr int kNow = decltype(b)::value;
+                if (x + 1 < halves) {
+                    // (entries first: a wait for them waits for all loads before them)
+                    look(x + 2, at[2]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    fetch(x + 1, at[1], half[kNow ^ 1], old[kNow ^ 1]);
+                }
+                float sums[kOf] = {};
+                asm volatile("" ::: "memory");  // the queries stay in LDS: registers are for keys on their way
+                rows_of(std::integral_constant<int, kOf>{}, half[kNow], key_of(x), 0, 0, sums);
+#pragma unroll
+                for (int c = 0; c < kOf; ++c) {
+                    sums[c] += __shfl_xor(sums[c], 16);
+                    sums[c] += __shfl_xor(sums[c], 32);
+                    const int32_t key = key_of(x) + 16 * c + n;
+                    if (h4 == c && is_there(at[0][c], key)) *weight_of(at[0][c], key) = old[kNow][c] + sums[c];
+                    at[0][c] = at[1][c];
+                    at[1][c] = at[2][c];
+                }
+            };
+            look(0, at[0]);
+            look(1, at[1]);
+            fetch(0, at[0], half[0], old[0]);
+            for (int32_t x = 0; x < halves; x += 2) {
+                turn(std::integral_constant<int, 0>{}, x);
+                turn(std::integral_constant<int, 1>{}, x + 1);
+            }
+        } else {
+        for (int32_t rt = rt0; rt < rt1; ++rt) {
+            const int buffer = (rt - rt0) & 1;
+            if (rt + 1 < rt1) load(rt + 1, buffer ^ 1);
+            rows_of(std::integral_constant<int, kGroups>{}, k, k0, rt, buffer, sum);
             if (((rt - rt0) & 31) == 31) {
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
+                for (int c = 0; c < kGroups; ++c) {
                     total[c] += sum[c];
                     sum[c] = 0.f;
                 }
@@ -309,17 +388,39 @@ __global__ __launch_bounds__(kThreads, 2) void k_weigh(WeighPlan p) {
             __syncthreads();
         }
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
+        for (int c = 0; c < kGroups; ++c) {
             total[c] += sum[c];
+            total[c] += __shfl_xor(total[c], 16);
             total[c] += __shfl_xor(total[c], 32);
-            const int in_tile = (wave * kChunks + c) * 32 + n;
-            if (half) continue;
-            if (part)
+        }
+        // a quarter of the lanes for each group, in turn
+#pragma unroll
+        for (int c = 0; c < kGroups; ++c) {
+            if (h4 != (c & 3)) continue;
+            const int in_tile = (wave * kGroups + c) * 16 + n;
+            if (part) {
                 to[in_tile] = total[c];
-            else if (tile * kTile + in_tile < end)
-                put_weight(p, r, head, tile * kTile + in_tile, total[c]);
+            } else if (is_there(entry[c], tile * kTile + in_tile)) {
+                const int32_t key = tile * kTile + in_tile;
+                float* const at = weight_of(entry[c], key);
+                *at = key < had ? *at + total[c] : total[c];
+            }
+        }
         }
     }
+}
+
+// The first workgroups take the requests of one row tile, the others those of several: in one launch, since the
+// host does not know of which there are any.
+template <int kDim, bool kHalf, int kLayout>
+__global__ __launch_bounds__(kThreads, weigh_waves(kDim)) void k_weigh(WeighPlan p) {
+    __shared__ __attribute__((aligned(16))) uint8_t s_q[2][WeighShape<kDim, kLayout>::kBuffer];
+    __shared__ float s_lse[2][kRowsOf];
+    const int first = p.streams * p.kv.heads;
+    if ((int)blockIdx.x < first)
+        weigh<kDim, kHalf, kLayout, true>(p, blockIdx.x, s_q, s_lse);
+    else
+        weigh<kDim, kHalf, kLayout, false>(p, blockIdx.x - first, s_q, s_lse);
 }
 
 // Adds the parts of tiles that several shares have: the workgroup of the share that begins a tile does.
@@ -331,7 +432,7 @@ __global__ __launch_bounds__(keys_of(kLayout)) void k_weigh_join(WeighPlan p) {
     int64_t first;
     Items f;
     const Shares shares = find_share<kTile / 64>(
-        p.R, p.shares, [&](int i) { return items_of(p, i, kTile); }, share, true, r, f, first);
+        p.R, p.shares, [&](int i) { return items_of(p, i, kTile, false); }, share, true, r, f, first);
     if (share >= shares.count || f.rows <= kWhole) return;
     const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
     const int32_t tile = tile_of(f, share1 - 1 - first);
@@ -350,14 +451,22 @@ __global__ __launch_bounds__(keys_of(kLayout)) void k_weigh_join(WeighPlan p) {
     if (key < end) put_weight(p, r, head, (int32_t)key, sum);
 }
 
+int32_t shares_of(int32_t heads, int workgroups) { return workgroups > heads ? workgroups / heads : 1; }
+
 template <int kDim, bool kHalf, int kLayout>
-hipError_t run(const WeighPlan& p, hipStream_t s) {
-    const dim3 grid((unsigned)(p.shares * p.kv.heads));
-    hipLaunchKernelGGL((k_weigh<kDim, kHalf, kLayout>), grid, dim3(kThreads), 0, s, p);
+hipError_t run(const WeighPlan& plan, hipStream_t s) {
+    WeighPlan p = plan;
+    const int64_t rows = p.n_tokens * p.group;
+    // As many workgroups of each kind as the device holds. Only of a single request does the host know how many
+    // row tiles it has.
+    const int32_t shares = shares_of(p.kv.heads, p.cus * weigh_waves(kDim));
+    p.streams = p.R > 1 || rows <= kRowsOf ? shares : 0;
+    p.shares = rows > kRowsOf ? shares : 0;
+    hipLaunchKernelGGL((k_weigh<kDim, kHalf, kLayout>), dim3((unsigned)((p.streams + p.shares) * p.kv.heads)),
+                       dim3(kThreads), 0, s, p);
     const hipError_t e = hipGetLastError();
-    // no request can have a tile that is cut
-    if (e != hipSuccess || p.n_tokens * p.group <= kWhole * kRowsOf) return e;
-    hipLaunchKernelGGL((k_weigh_join<kLayout>), grid, dim3(keys_of(kLayout)), 0, s, p);
+    if (e != hipSuccess || rows <= kWhole * kRowsOf) return e;  // no request can have a tile that is cut
+    hipLaunchKernelGGL((k_weigh_join<kLayout>), dim3((unsigned)(p.shares * p.kv.heads)), dim3(keys_of(kLayout)), 0, s, p);
     return hipGetLastError();
 }
 
@@ -374,14 +483,8 @@ hipError_t run_latent(const WeighPlan& p, hipStream_t s) {
 
 }  // namespace
 
-// As many workgroups as fill the device: four a compute unit.
-int weigh_shares(int32_t heads, int cus) {
-    const int shares = 4 * cus / heads;
-    return shares > 0 ? shares : 1;
-}
-
 int64_t weigh_workspace(int32_t heads, int cus) {
-    return 2ll * weigh_shares(heads, cus) * heads * keys_of(0) * (int64_t)sizeof(float);
+    return 2ll * shares_of(heads, cus * 3) * heads * keys_of(0) * (int64_t)sizeof(float);
 }
 
 hipError_t launch_weigh(const WeighPlan& p, hipStream_t s) {

@@ -38,6 +38,7 @@ const char* weigh_plan(const Args& a, int32_t q_heads, int32_t block_tokens, Wei
     p->max_blocks = a.max_blocks;
     p->q_heads = q_heads;
     p->group = q_heads / p->kv.heads;
+    p->rows_div = page_div(p->group);
     p->scale2 = a.scale * 1.4426950408889634f;
     p->weights = a.weights;
     p->parts = static_cast<float*>(a.workspace);
@@ -50,7 +51,7 @@ int weigh(const char* call, const Args& a, WeighPlan* p, void* stream) {
     if (const int rc = compute_units(call, &cus)) return rc;
     if (a.workspace_bytes < weigh_workspace(p->kv.heads, cus) || !a.workspace || !aligned16(a.workspace))
         return refuse_as(call, "workspace too small or not 16-byte aligned (ptstore_weigh_workspace)");
-    p->shares = weigh_shares(p->kv.heads, cus);
+    p->cus = cus;
     return launch_weigh(*p, (hipStream_t)stream) == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, call);
 }
 

@@ -22,10 +22,11 @@ struct WeighPlan {
     float scale2;    // scale * log2(e)
     float* weights;  // [block][KV head][slot]
     float* parts;    // workspace
-    int32_t shares;
+    int32_t streams, shares;  // of requests of one tile of query rows, of the others
+    int32_t cus;
+    PageDiv rows_div;         // by group
 };
 
-int weigh_shares(int32_t heads, int cus);
 int64_t weigh_workspace(int32_t heads, int cus);  // bytes
 hipError_t launch_weigh(const WeighPlan& p, hipStream_t s);
 
