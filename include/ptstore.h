@@ -819,7 +819,7 @@ int ptstore_evict_workspace(int32_t layers, int32_t R, int32_t kv_heads, int32_t
                             int64_t *bytes);
 
 /* `kv`, `cache`: the first layer. Errors: INVALID (sizes out of range; max_blocks * block_tokens > 2^30;
- * more than 2^23 workgroups: layers * R * kv_heads * planes * 128-byte pieces of a row; a NULL pointer;
+ * more than 2^23 workgroups: layers * R * kv_heads * (planes * 128-byte pieces of a row + 1); a NULL pointer;
  * a workspace too small), HIP. */
 int ptstore_kv_evict(const ptstore_kv_t *kv, const ptstore_evict_t *args, void *stream);
 int ptstore_latent_evict(const ptstore_latent_t *cache, const ptstore_evict_t *args, void *stream);

@@ -66,6 +66,7 @@ int evict(const char* call, const ptstore_evict_t* a, KeepPlan* p, int64_t plane
     if (a->layer_bytes % 16 || (a->layers > 1 && a->layer_bytes < plane_bytes))
         return refuse_as(call, "layer_bytes must be a multiple of 16 and hold a layer's planes");
     p->layer = a->layer_bytes;
+    p->slab_rows = page_div(p->heads * (int)p->div.page);
     p->layers = a->layers;
     p->R = a->R;
     p->max_blocks = a->max_blocks;
@@ -91,7 +92,9 @@ int evict(const char* call, const ptstore_evict_t* a, KeepPlan* p, int64_t plane
     p->max_keep = a->max_keep;
     p->recent = a->recent;
     p->source = static_cast<int32_t*>(a->workspace);
-    return launch_keep(*p, (hipStream_t)stream) == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, call);
+    int cus = 0;
+    if (const int rc = compute_units(call, &cus)) return rc;
+    return launch_keep(*p, cus, (hipStream_t)stream) == hipSuccess ? PTSTORE_OK : set_last_error(PTSTORE_ERR_HIP, call);
 }
 
 }  // namespace

@@ -37,6 +37,7 @@ struct KeepPlan {
     int32_t layers, heads, R, max_blocks;
     PageDiv div;
     int64_t slab;        // bytes of a block in a plane
+    PageDiv slab_rows;   // division by a block's rows
     int32_t row;         // bytes of a row of values or codes, a multiple of 16
     int32_t power;       // bytes of a row's exponents: 0, 2 or 4
     int64_t powers;      // offset of a slab's exponents
@@ -50,7 +51,7 @@ struct KeepPlan {
     int32_t* source;     // workspace: [unit][max_keep] positions that stay
 };
 
-int64_t keep_workgroups(const KeepPlan& p);  // of the larger launch
-hipError_t launch_keep(const KeepPlan& p, hipStream_t s);
+int64_t keep_workgroups(const KeepPlan& p);  // at least, of the larger launch
+hipError_t launch_keep(const KeepPlan& p, int cus, hipStream_t s);
 
 }  // namespace ptsd
