@@ -57,7 +57,7 @@ struct ExpandedPlan {
     uint8_t *k, *v;   // [head][key]: 128 nearest 16-bit values, 128 of what is left
     uint8_t* rope;    // [key][64]
     int32_t* there;   // [key] whether its page exists
-    int32_t each;     // heads of a workgroup that forms keys and values
+    int32_t parts;    // of the heads, each with dies of its own
 };
 
 int64_t expanded_workspace(int32_t heads, int64_t n_keys);  // bytes

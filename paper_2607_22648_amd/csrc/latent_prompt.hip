@@ -7,8 +7,8 @@
 // 2 (128 + 128), where the latent space has 2 (576 + 512).
 //
 // Forming them is a matrix product: 128 keys and all of their latent values stay in LDS while a workgroup goes
-// through the matrices of several heads, which its waves read from L2 into registers, 64 of a head's 256 rows
-// each. What comes out is packed by head.
+// through the matrices of several heads, two at a time, which its waves read from L2 into registers, 64 of a
+// head's 256 rows each. What comes out is packed by head.
 //
 // The attention is that of prompt.hip: 128 tokens of a head a workgroup, 32 a wave, S^T = K Q^T and
 // O^T = V^T P^T. Keys lie next to each other and need no conversion, so they go to LDS without passing
@@ -26,6 +26,9 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kFormKeys = 128;  // of a workgroup that forms keys and values
+constexpr int kFormWaves = 8, kFormThreads = kFormWaves * 64;  // four for a head
+constexpr int kDies = 8;
+constexpr int kDieBytes = 2 << 20;  // of matrices that a die goes through: half of its L2
 constexpr int kKeys = 32;       // of a step of the attention
 constexpr int kRow = 512;       // bytes of a formed key, or value: 128 nearest values, 128 of what is left
 
@@ -61,36 +64,49 @@ __device__ inline uint32_t split2(float a, float b, uint32_t& left) {
 }
 
 template <int L, bool kHalf>
-__global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
+__global__ __launch_bounds__(kFormThreads) void k_form(ExpandedPlan p) {
     using E = Elem<kHalf>;
     using V8 = typename E::v8;
     constexpr int kLine = L * 2 + 16;  // bytes in LDS: 16 lanes that read one column of 16 rows need 16 places
     constexpr int kTiles = kFormKeys / 32;
     __shared__ __attribute__((aligned(256))) uint8_t s_rows[kFormKeys * kLine];
+    __shared__ __attribute__((aligned(16))) uint8_t s_out[kFormWaves][16 * 128];
     __shared__ uint32_t s_at[kFormKeys];
     __shared__ int32_t s_there[kFormKeys];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
-    const int groups = (p.heads + p.each - 1) / p.each;
-    const int64_t key0 = (int64_t)(blockIdx.x / groups) * kFormKeys;
-    const int group = blockIdx.x % groups;
+    // Workgroups of neighbouring numbers are on different dies, each with an L2 of 4 MiB, and a head's matrices
+    // take 256 KiB: a die goes through 8 heads or so, and all keys. (All heads on all dies: forming 12,800 keys of 32
+    // heads took 206 us.) Within its heads, (tile of keys, pair of heads) units, in equal shares of neighbours.
+    const int die = blockIdx.x % kDies, part = die % p.parts, all_pairs = (p.heads + 1) / 2;
+    const int first = all_pairs * part / p.parts, pairs = all_pairs * (part + 1) / p.parts - first;
+    const int workers = gridDim.x / p.parts, me = blockIdx.x / kDies * (kDies / p.parts) + die / p.parts;
+    const int64_t units = (p.n_keys + kFormKeys - 1) / kFormKeys * pairs;
+    const int64_t share1 = units * (me + 1) / workers;
+    for (int64_t unit = units * me / workers; unit < share1;) {
+    const int64_t tile = unit / pairs, key0 = tile * kFormKeys;
+    const int from = (int)(unit - tile * pairs);
+    const int until = pairs - from < share1 - unit ? pairs : from + (int)(share1 - unit);
+    const int pair0 = first + from, pair1 = first + until;
+    unit += until - from;
+    __syncthreads();  // all are done with the tile before
     if (threadIdx.x < kFormKeys) {
         uint32_t at;
         const bool there = row_of(p, key0 + threadIdx.x, at);
         s_at[threadIdx.x] = at;
         s_there[threadIdx.x] = there;
-        if (group == 0 && key0 + threadIdx.x < p.n_keys) p.there[key0 + threadIdx.x] = there;
+        if (pair0 == 0 && key0 + threadIdx.x < p.n_keys) p.there[key0 + threadIdx.x] = there;
     }
     __syncthreads();
     const uint32_t lds = lds_of(s_rows);
-    for (int i = 0; i < kFormKeys / kWaves; ++i) {
-        const int j = wave * (kFormKeys / kWaves) + i;
+    for (int i = 0; i < kFormKeys / kFormWaves; ++i) {
+        const int j = wave * (kFormKeys / kFormWaves) + i;
         const uint8_t* const row = p.kv.rows + ((uint64_t)__builtin_amdgcn_readfirstlane(s_at[j]) << 4);
         if (L == 512 || lane < L / 8) fetch16(row, (uint32_t)lane * 16, lds + j * kLine);
     }
-    if (group == 0) {
+    if (pair0 == 0) {
         // the shared parts, 8 lanes a row
-        for (int j = threadIdx.x / 8; j < kFormKeys; j += kThreads / 8) {
+        for (int j = threadIdx.x / 8; j < kFormKeys; j += kFormThreads / 8) {
             if (key0 + j >= p.n_keys) break;
             const v4u x = *(const v4u*)(p.kv.rows + (((uint64_t)s_at[j] + L / 8 + threadIdx.x % 8) << 4));
             const v4u zero = {0u, 0u, 0u, 0u};
@@ -100,19 +116,31 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
     arrive<0>();
     __syncthreads();
     // rows that are not there are zeros
-    for (int j = wave; j < kFormKeys; j += kWaves)
+    for (int j = wave; j < kFormKeys; j += kFormWaves)
         if (!s_there[j] && lane < L / 8) *(v4u*)(s_rows + j * kLine + lane * 16) = v4u{0u, 0u, 0u, 0u};
     __syncthreads();
 
-    const int last = group * p.each + p.each < p.heads ? group * p.each + p.each : p.heads;
-    const bool value = wave >= 2;  // waves 0, 1: a head's keys; 2, 3: its values
+    const int last = 2 * pair1 < p.heads ? 2 * pair1 : p.heads;
+    const bool value = wave & 2;  // of four waves the first two take a head's keys, the others its values
     const Rows& w = value ? p.wv : p.wk;
-    for (int head = group * p.each; head < last; ++head) {
+    // Rows 64 (wave & 1) .. of a head's matrix. Of each 64 latent values a lane takes 32 in a row, so that
+    // whole lines are used; the keys are read to match.
+    const int64_t next = w.token * 64;  // 32 rows on
+    v4u x[2][8];  // this and the next 64 latent values of two rows
+    auto load = [&](int head, int k, v4u (&to)[8]) {
+        const uint8_t* const rows =
+            (const uint8_t*)w.p + ((int64_t)head * w.head + (int64_t)((wave & 1) * 64 + n) * w.token + half * 32) * 2;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            to[s] = *(const v4u*)(rows + k * 128 + s * 16);
+            to[4 + s] = *(const v4u*)(rows + next + k * 128 + s * 16);
+        }
+    };
+    constexpr int kAtOnce = kFormWaves / 4;  // heads
+    const int head0 = 2 * pair0 + (wave >> 2);
+    if (head0 < last) load(head0, 0, x[0]);
+    for (int head = head0; head < last; head += kAtOnce) {
         asm volatile("" ::: "memory");  // the keys stay in LDS: all of them do not fit the registers
-        // rows 64 (wave & 1) .. of the head's matrix. Of each 64 latent values a lane takes 32 in a row, so that
-        // whole lines are used; the keys are read to match.
-        const uint8_t* const rows = (const uint8_t*)w.p + ((int64_t)head * w.head + (int64_t)((wave & 1) * 64 + n) * w.token + half * 32) * 2;
-        const int64_t next = w.token * 64;  // 32 rows on
         v16f o[2][kTiles];
 #pragma unroll
         for (int a = 0; a < 2; ++a)
@@ -120,18 +148,9 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[a][t][e] = 0.f;
-        v4u x[2][8];  // this and the next 64 latent values of two rows
-        auto load = [&](v4u (&to)[8], int k) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                to[s] = *(const v4u*)(rows + k * 128 + s * 16);
-                to[4 + s] = *(const v4u*)(rows + next + k * 128 + s * 16);
-            }
-        };
-        load(x[0], 0);
 #pragma unroll
         for (int k = 0; k < L / 64; ++k) {
-            if (k + 1 < L / 64) load(x[(k + 1) & 1], k + 1);
+            if (k + 1 < L / 64) load(head, k + 1, x[(k + 1) & 1]);
             const v4u(&now)[8] = x[k & 1];
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -146,34 +165,54 @@ __global__ __launch_bounds__(kThreads) void k_form(ExpandedPlan p) {
                         o[a][t] = E::mma32(__builtin_bit_cast(V8, now[a * 4 + s]), c[t], o[a][t]);
             }
         }
+        // the next head's first values, before the stores: a wait for loads waits for all stores before them
+        if (head + kAtOnce < last) load(head + kAtOnce, 0, x[0]);
+        // Out by way of LDS, 16 keys at a time, so that 8 lanes write a whole line of a key: straight from the
+        // products' registers it is 32 bytes a key (forming 12,800 keys of 32 heads took 250 us so).
         uint8_t* const out = (value ? p.v : p.k) + ((int64_t)head * p.n_keys + key0) * kRow + (wave & 1) * 128;
+        uint8_t* const mem = s_out[wave];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-            if (key0 + t * 32 + n >= p.n_keys) continue;  // both halves of a key
+            v4u y[2][2][2];  // [nearest, left][tile of 32 values][16 of them]: 8 a lane
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int a = 0; a < 4; a += 2) {
-                    // 4 values here, the next 4 in the other half: trade, and write 8 a lane
-                    v4u y, z;
+                for (int a = 0; a < 4; a += 2)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
+                        // 4 values here, the next 4 in the other half: trade
                         uint32_t near[2], left[2];
 #pragma unroll
                         for (int b = 0; b < 2; ++b)
                             near[b] = split2<kHalf>(o[i][t][4 * (a + b) + 2 * h], o[i][t][4 * (a + b) + 2 * h + 1], left[b]);
                         const auto x = __builtin_amdgcn_permlane32_swap(near[0], near[1], false, false);
-                        y[h] = x[0];
-                        y[2 + h] = x[1];
+                        y[0][i][a / 2][h] = x[0];
+                        y[0][i][a / 2][2 + h] = x[1];
                         const auto w = __builtin_amdgcn_permlane32_swap(left[0], left[1], false, false);
-                        z[h] = w[0];
-                        z[2 + h] = w[1];
+                        y[1][i][a / 2][h] = w[0];
+                        y[1][i][a / 2][2 + h] = w[1];
                     }
-                    uint8_t* const to = out + (int64_t)(t * 32 + n) * kRow + (32 * i + 8 * (a + half)) * 2;
-                    *(v4u*)to = y;
-                    *(v4u*)(to + kRow / 2) = z;
+#pragma unroll
+            for (int round = 0; round < 4; ++round) {
+                const int kind = round & 1, up = round >> 1;  // nearest or left; which 16 keys
+                if (n >> 4 == up) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *(v4u*)(mem + (n & 15) * 128 + (((2 * c + half) ^ (n & 7)) * 16)) = y[kind][c >> 1][c & 1];
                 }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int key = 8 * j + (lane >> 3), to = t * 32 + 16 * up + key;
+                    const v4u x = *(const v4u*)(mem + key * 128 + (((lane & 7) ^ (key & 7)) * 16));
+                    if (key0 + to < p.n_keys) 
+                        __builtin_nontemporal_store(
+                            x, (v4u*)(out + (int64_t)to * kRow + kind * (kRow / 2) + (lane & 7) * 16));
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
         }
+    }
     }
 }
 
@@ -422,10 +461,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
 }
 
 template <int L, bool kHalf>
-hipError_t run(const ExpandedPlan& p, hipStream_t s) {
+hipError_t run(const ExpandedPlan& p, int cus, hipStream_t s) {
     if (p.n_keys > 0) {
-        const int64_t tiles = (p.n_keys + kFormKeys - 1) / kFormKeys, groups = (p.heads + p.each - 1) / p.each;
-        hipLaunchKernelGGL((k_form<L, kHalf>), dim3((unsigned)(tiles * groups)), dim3(kThreads), 0, s, p);
+        // one workgroup a compute unit, as LDS allows
+        const int grid = (cus + kDies - 1) / kDies * kDies;
+        hipLaunchKernelGGL((k_form<L, kHalf>), dim3((unsigned)grid), dim3(kFormThreads), 0, s, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -436,8 +476,8 @@ hipError_t run(const ExpandedPlan& p, hipStream_t s) {
 }
 
 template <int L>
-hipError_t run_kind(const ExpandedPlan& p, hipStream_t s) {
-    return p.kv.kind == PTSTORE_KV_FP16 ? run<L, true>(p, s) : run<L, false>(p, s);
+hipError_t run_kind(const ExpandedPlan& p, int cus, hipStream_t s) {
+    return p.kv.kind == PTSTORE_KV_FP16 ? run<L, true>(p, cus, s) : run<L, false>(p, cus, s);
 }
 
 int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
@@ -457,12 +497,8 @@ void place_expanded(ExpandedPlan* p, void* workspace) {
 
 hipError_t launch_expanded(const ExpandedPlan& plan, int cus, hipStream_t s) {
     ExpandedPlan p = plan;
-    // Workgroups that form keys and values: one a compute unit, as LDS allows, so that each has as many heads
-    // as leave none of them idle.
-    const int64_t tiles = (p.n_keys + kFormKeys - 1) / kFormKeys;
-    const int64_t each = (tiles * p.heads + cus - 1) / cus;
-    p.each = (int32_t)(each < 1 ? 1 : each < p.heads ? each : p.heads);
-    return p.kv.latent == 512 ? run_kind<512>(p, s) : run_kind<256>(p, s);
+    for (p.parts = 1; p.parts < kDies && (int64_t)p.heads * 256 * p.kv.latent * 2 / p.parts > kDieBytes;) p.parts *= 2;
+    return p.kv.latent == 512 ? run_kind<512>(p, cus, s) : run_kind<256>(p, cus, s);
 }
 
 }  // namespace ptsd
