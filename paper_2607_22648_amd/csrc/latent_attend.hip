@@ -25,13 +25,14 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kKeys = 32;    // of a piece
+constexpr int kSpare = 8;    // pieces' time that a tile takes beside its keys
 constexpr int kTile = 128;   // query rows
 constexpr int kStages = 3;   // pieces in LDS: one is computed while two are on their way
 constexpr int kAhead = kStages - 1;
 constexpr int kEntries = 2 * kAhead + 2;  // pieces whose page entries are in LDS
 
 // Floats of a part in the workspace: [4 dimensions][row], then rows' maxima and sums.
-constexpr int part_floats(int latent) { return kTile * (latent + 2); }
+constexpr int part_floats(int latent, int tile) { return tile * (latent + 2); }
 
 // A piece in LDS: rows' latent parts, padded by 16 bytes, row r in place place_of(r). 16 lanes read one
 // 16-byte column of 16 rows as keys: all 16 places of 256 bytes. As values, 32 lanes read 64
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     int r;
     int64_t first;  // the request's first step
     Work f;
-    Shares shares = find_step<kTile, kWaves>(p, kKeys, share, false, r, f, first);
+    Shares shares = find_step<kTile, kWaves, kSpare>(p, kKeys, share, false, r, f, first);
     shares = {uniform(shares.all), uniform(shares.count)};
     if (share >= shares.count) return;
     first = uniform(first);
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     for (int64_t done = share0; done < share1;) {
     while (done >= first + f.all()) {  // on to the next request with work
         first += f.all();
-        f = uniform(work_of<kTile>(p, ++r, kKeys));
+        f = uniform(work_of<kTile, kSpare>(p, ++r, kKeys));
     }
     const int tile = (int)((done - first) / f.steps);
     const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
@@ -217,10 +218,12 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
         // Behind the barrier the piece is whole, and all waves are done with the one before, whose
         // place the next to be fetched takes. Left under way: this wave's part of the next piece (and, so,
         // of page entries only those fetched after it, which are used three turns later).
-        if (piece + 1 < pieces)
-            arrive<(kAhead - 1) * kFetches>();
-        else
+        if (piece + 1 >= pieces)
             arrive<0>();
+        else if (wave == 0)
+            arrive<(kAhead - 1) * (kFetches + 1)>();
+        else
+            arrive<(kAhead - 1) * kFetches>();
         barrier();
         // what follows from the lane is formed anew each time: kept, it takes two dozen registers
         int here = lane;
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     const int trow = rg * 32 + column;  // in the tile
     if (step0 > 0 || step1 < f.steps) {
         // a part: of a tile that began in an earlier share, or one that goes on
-        float* const to = p.parts + (2 * (int64_t)share + (step0 > 0 ? 0 : 1)) * part_floats(L);
+        float* const to = p.parts + (2 * (int64_t)share + (step0 > 0 ? 0 : 1)) * part_floats(L, kTile);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
@@ -413,6 +416,304 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     }
 }
 
+// Few rows: tiles of 16, and each of the eight waves takes pieces of 16 keys by itself, with all dimensions (72
+// registers of queries, 128 of outputs), 128 keys of a share at a time, and no barrier until a tile's part is done.
+// What a wave waits for memory the others fill. (As a pair of waves that trade scores and wait at barriers twice a
+// piece, 64 requests of 16 heads took 82 us, not 67, where loading alone takes 50: a wave issues an instruction
+// every five cycles or so, and a piece's chain of them was longer than its bytes take.)
+constexpr int kFewRows16 = 16;
+constexpr int kFewKeys = 16;                 // of a piece
+constexpr int kFewStep = kWaves * kFewKeys;  // of a share's step
+constexpr int kFewSpare = 2;                 // steps that a tile takes beside its keys
+
+// A piece in LDS: rows' latent parts, padded by 16 bytes, row r in place few_place(r): 16 lanes that read a
+// column of 16 rows find 16 places, and the 8 rows whose 32 bytes 32 lanes read as values are 32 bytes apart.
+__device__ inline int few_place(int row) { return 2 * (row & 7) + (row >> 3); }
+
+__device__ inline v4f mma16_few(v2u a, v2u b, v4f c, std::true_type) {
+    typedef _Float16 v4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(v4, a), __builtin_bit_cast(v4, b), c, 0, 0, 0);
+}
+__device__ inline v4f mma16_few(v2u a, v2u b, v4f c, std::false_type) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, a), __builtin_bit_cast(v4s, b), c, 0, 0, 0);
+}
+
+template <int L, bool kHalf>
+__global__ __launch_bounds__(kThreads) void k_latent_few(LatentPlan p) {
+    using E = Elem<kHalf>;
+    using V8 = typename E::v8;
+    constexpr int kTile = kFewRows16;
+    constexpr int kSteps = L / 32, kRopeSteps = kRope / 32;  // of the first product, 32 dimensions each
+    constexpr int kTiles = L / 16;                           // of the output, 16 dimensions each
+    constexpr int kRow = L * 2 + 16;                         // bytes of a latent part in LDS
+    constexpr int kPiece = kFewKeys * (kRow + kRope * 2);
+    constexpr int kOut = 256;                                // dimensions that the waves join at once
+    static_assert(kWaves * kTile * kOut * 4 <= kWaves * kPiece || L == 256, "");
+    constexpr int kMem = kWaves * (kPiece > kTile * kOut * 4 ? kPiece : kTile * kOut * 4);
+
+    __shared__ __attribute__((aligned(256))) uint8_t s_rows[kMem];
+    __shared__ float s_max[kWaves][kTile], s_sum[kWaves][kTile];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, h4 = lane >> 4;  // query column, quarter
+    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
+    const int share = blockIdx.x;
+    int r;
+    int64_t first;  // the request's first step
+    Work f;
+    Shares shares = find_step<kTile, kWaves, kFewSpare>(p, kFewStep, share, false, r, f, first);
+    shares = {uniform(shares.all), uniform(shares.count)};
+    if (share >= shares.count) return;
+    first = uniform(first);
+    f = uniform(f);
+    uint8_t* const mem = s_rows + wave * kPiece;
+    const uint32_t rows_at = lds_of(s_rows) + wave * kPiece;
+
+    const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
+    for (int64_t done = share0; done < share1;) {
+    while (done >= first + f.all()) {  // on to the next request with work
+        first += f.all();
+        f = uniform(work_of<kTile, kFewSpare>(p, ++r, kFewStep));
+    }
+    const int tile = (int)((done - first) / f.steps);
+    const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
+    const int step0 = (int)(done - tile0);
+    const int step1 = share1 - tile0 < f.steps ? (int)(share1 - tile0) : f.steps;
+    done = tile0 + step1;
+
+    // the tile's rows see keys up to `end`; those of this share are [k0, k1)
+    const int all_rows = f.n * p.group;
+    const int rows_left = all_rows - tile * kTile, rows = rows_left < kTile ? rows_left : kTile;
+    const int row = tile * kTile + (n < rows ? n : rows - 1);
+    const int token = row / p.group, head = row - token * p.group;
+    int64_t seen64 = f.past + (tile * kTile + rows - 1) / p.group + 1;
+    seen64 = seen64 < 0 ? 0 : (seen64 > limit ? limit : seen64);
+    const int32_t end = __builtin_amdgcn_readfirstlane((int32_t)seen64);
+    const int32_t k0 = step0 * kFewStep;
+    const int32_t k1 = end - k0 < (step1 - step0) * kFewStep ? end : step1 * kFewStep;
+    const int64_t pos64 = f.past + token;  // the last key this lane's query sees
+    const int32_t pos = pos64 < limit ? (int32_t)pos64 : (int32_t)limit;
+    const int64_t first64 = f.past + tile * kTile / p.group;
+    const int32_t all_see = __builtin_amdgcn_readfirstlane(first64 < limit ? (int32_t)first64 : (int32_t)limit);
+    const int32_t* const table = p.table + (int64_t)r * p.max_blocks;
+
+    // queries: column n, 8 consecutive dimensions of each 32 a lane
+    V8 q[kSteps + kRopeSteps];
+    {
+        const uint8_t* a = (const uint8_t*)p.ql.p + ((f.begin + token) * p.ql.token + head * p.ql.head) * 2;
+        const uint8_t* b = (const uint8_t*)p.qr.p + ((f.begin + token) * p.qr.token + head * p.qr.head) * 2;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(V8, *(const v4u*)(a + (s * 32 + h4 * 8) * 2));
+#pragma unroll
+        for (int s = 0; s < kRopeSteps; ++s)
+            q[kSteps + s] = __builtin_bit_cast(V8, *(const v4u*)(b + (s * 32 + h4 * 8) * 2));
+    }
+    v4f o[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) o[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    float top = kLowest, sum = 0.f;
+    bool far = false;      // scores are scaled before the maximum is taken
+    bool endless = false;  // a value that is not finite lies behind the first row's last key
+
+    auto entry_of = [&](int32_t key) {  // (past the end: the last one's)
+        const int32_t last = k1 - 1;
+        return table[div_page((uint32_t)(key < last ? key : last), p.kv.div)];
+    };
+    int32_t at = k0 + wave * kFewKeys;
+    int32_t entry = at < k1 ? entry_of(at + n) : -1;
+    for (; at < k1; at += kFewStep) {
+        int here = lane;
+        asm volatile("" : "+v"(here));  // what follows from the lane is formed anew each time
+        const int n = here & 15, h4 = here >> 4;
+        const int32_t key = at + n;
+        const bool there = key < k1 && entry >= 0 && entry < (int32_t)p.kv.blocks;
+        const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
+        const uint32_t place = there ? ((uint32_t)entry * p.kv.div.page + slot) * p.kv.line : 0u;
+        const uint32_t ok = (uint32_t)__ballot(there) & 0xFFFFu;
+#pragma unroll
+        for (int j = 0; j < kFewKeys; ++j) {
+            const uint32_t row_at = (uint32_t)__builtin_amdgcn_readlane((int)place, j);
+            if (L == 512 || here < L / 8)
+                fetch16_once(p.kv.rows + ((uint64_t)row_at << 4), (uint32_t)here * 16, rows_at + few_place(j) * kRow);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {  // the shared parts, 8 rows of 8 lanes
+            const int j = 8 * i + (here >> 3);
+            const uint32_t row_at = (uint32_t)__builtin_amdgcn_ds_bpermute(j * 4, (int)place);
+            fetch16_at(p.kv.rows + (((uint64_t)row_at + L / 8 + ((here & 7) ^ turn_rope(j))) << 4),
+                       rows_at + kFewKeys * kRow + i * 1024);
+        }
+        if (at + kFewStep < k1) entry = entry_of(at + kFewStep + n);
+        arrive<0>();
+
+        // S^T: row n of the piece as keys, 8 dimensions of each 32 a lane; keys 4 h4 + e in s[e]
+        const uint8_t* const keys = mem + few_place(n) * kRow + h4 * 16;
+        const uint8_t* const shared = mem + kFewKeys * kRow + n * (kRope * 2);
+        v4f s = {0.f, 0.f, 0.f, 0.f};
+        pipelined<3, kSteps + kRopeSteps>(
+            [&](int i) {
+                return *(const v4u*)(i < kSteps ? keys + 64 * i : shared + ((4 * (i - kSteps) + h4) ^ turn_rope(n)) * 16);
+            },
+            [&](int i, const v4u& x) { s = E::mma16(__builtin_bit_cast(V8, x), q[i], s); });
+        const bool some_hidden = ok != 0xFFFFu || at + kFewKeys - 1 > all_see;
+        if (some_hidden) {
+            const int32_t ahead = pos - at;
+            uint32_t seen = ahead < 0 ? 0 : (ahead > 14 ? ~0u : (2u << ahead) - 1);
+            seen = (seen & ok) >> (4 * h4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!(seen & (1u << e))) s[e] = -INFINITY;
+            // As values, rows that are not there become zeros, and so do values that are not finite where
+            // the tile's first row does not see them: a weight of zero would make them NaN.
+#pragma unroll 1
+            for (int j = 0; j < kFewKeys; ++j) {
+                v4u* const x = (v4u*)(mem + few_place(j) * kRow) + here;
+                if (here >= L / 8) continue;
+                if (!((ok >> j) & 1)) {
+                    *x = v4u{0u, 0u, 0u, 0u};
+                } else if (at + j > all_see) {
+                    v4u y = *x;
+                    if (drop_endless<kHalf>(y)) {
+                        endless = true;
+                        *x = y;
+                    }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        float most = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        most = larger_16_32(most);
+        auto scale_now = [&] {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = product(s[e], p.scale2);
+            most = product(most, p.scale2);
+        };
+        if (far) scale_now();
+        float top2 = fmaxf(top, __builtin_fmaf(most, far ? 1.f : p.scale2, kRoom<kHalf>));
+        if (__any(top2 > top + (far ? 0.f : kBehind))) {
+            if (!far && __any(is_far(top2))) {
+                far = true;
+                scale_now();
+                top2 = fmaxf(top, most + kRoom<kHalf>);
+            }
+            const float less = exp2_of(top - top2);
+            sum *= less;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][e] *= less;
+            top = top2;
+        }
+        const float scale = far ? 1.f : p.scale2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s[e] = exp2_of(__builtin_fmaf(s[e], scale, -top));
+            sum += s[e];
+        }
+        // rounded to 16 bits as in prompt.hip; the sum takes them as they are
+        const v2u w = {pack2<kHalf>(s[0], s[1]), pack2<kHalf>(s[2], s[3])};
+        // O^T: 16 dimensions of 4 keys a quarter of the wave, read transposed
+        const uint8_t* const values = mem + few_place(4 * h4 + (n >> 2)) * kRow + (n & 3) * 8;
+        pipelined<4, kTiles>(
+            [&](int i) {
+                const v2u x = read_transposed(values + 32 * i);
+                return v4u{x[0], x[1], 0u, 0u};
+            },
+            [&](int i, const v4u& x) {
+                o[i] = mma16_few(v2u{x[0], x[1]}, w, o[i], std::integral_constant<bool, kHalf>{});
+            });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the piece is read: the next may overwrite it
+    }
+    if (__any(endless)) {
+        for (int32_t from = k0 + wave * kFewKeys; from < k1; from += kFewStep)
+            for (int32_t key = from; key < k1 && key < from + kFewKeys; ++key) {
+                if (key <= all_see || key > pos) continue;
+                const int32_t entry = table[div_page((uint32_t)key, p.kv.div)];
+                if (entry < 0 || entry >= (int32_t)p.kv.blocks) continue;
+                const uint32_t slot = (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page;
+                int up = h4;
+                asm volatile("" : "+v"(up));  // no address is kept for this from before the pieces
+                const uint16_t* x = (const uint16_t*)(p.kv.rows +
+                    ((uint64_t)(((uint32_t)entry * p.kv.div.page + slot) * p.kv.line) << 4)) + 4 * up;
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint16_t y = x[16 * i + e];
+                        o[i][e] = add_endless(o[i][e], kHalf ? (float)__builtin_bit_cast(_Float16, y)
+                                                             : __uint_as_float((uint32_t)y << 16));
+                    }
+            }
+    }
+
+    // Join the eight waves: maxima and sums, then outputs at one scale, kOut dimensions at a time through LDS.
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    __syncthreads();  // the tile before is written
+    if (h4 == 0) {
+        s_max[wave][n] = top;
+        s_sum[wave][n] = sum;
+    }
+    __syncthreads();
+    const bool part = step0 > 0 || step1 < f.steps;
+    float* const to = p.parts + (2 * (int64_t)share + (step0 > 0 ? 0 : 1)) * part_floats(L, kTile);
+    {
+        float all = kLowest;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all = fmaxf(all, s_max[w][n]);
+        const float less = exp2_of(top - all);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] *= less;
+    }
+    float* const x = (float*)s_rows;  // [wave][dimensions / 4][row][4]
+#pragma unroll
+    for (int c = 0; c < L; c += kOut) {
+        __syncthreads();  // all are done with their pieces, or with what was joined before
+#pragma unroll
+        for (int i = 0; i < kOut / 16; ++i)
+            *(v4f*)(x + ((wave * (kOut / 4) + 4 * i + h4) * kTile + n) * 4) = o[c / 16 + i];
+        __syncthreads();
+        // a row and 8 dimensions a thread
+        const int jr = threadIdx.x % kTile, jc = threadIdx.x / kTile;
+        float all = kLowest, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all = fmaxf(all, s_max[w][jr]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) total += exp2_of(s_max[w][jr] - all) * s_sum[w][jr];
+        v4f a = {0.f, 0.f, 0.f, 0.f}, b = a;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const v4f y = *(const v4f*)(x + ((w * (kOut / 4) + 2 * jc) * kTile + jr) * 4);
+            const v4f z = *(const v4f*)(x + ((w * (kOut / 4) + 2 * jc + 1) * kTile + jr) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] += y[e];
+                b[e] += z[e];
+            }
+        }
+        if (part) {
+            // of a tile that began in an earlier share, or one that goes on
+            *(v4f*)(to + ((c / 4 + 2 * jc) * kTile + jr) * 4) = a;
+            *(v4f*)(to + ((c / 4 + 2 * jc + 1) * kTile + jr) * 4) = b;
+            if (c == 0 && jc == 0) *(v2f*)(to + kTile * L + 2 * jr) = v2f{all, total};
+        } else if (jr < rows) {
+            // no key, or none with a weight: zeros, and the logarithm of nothing
+            const float inv = total != 0.f ? 1.f / total : 0.f;
+            const int out_row = tile * kTile + jr, ot = out_row / p.group, oh = out_row - ot * p.group;
+            const v4u y = {pack2<kHalf>(a[0] * inv, a[1] * inv), pack2<kHalf>(a[2] * inv, a[3] * inv),
+                           pack2<kHalf>(b[0] * inv, b[1] * inv), pack2<kHalf>(b[2] * inv, b[3] * inv)};
+            *(v4u*)((uint8_t*)p.out.p + ((f.begin + ot) * p.out.token + oh * p.out.head + c + jc * 8) * 2) = y;
+            if (p.lse && c == 0 && jc == 0)
+                p.lse[(f.begin + ot) * p.group + oh] =
+                    total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+        }
+    }
+    __syncthreads();  // the next tile's pieces go there
+    }
+}
+
 // Joins the parts of a tile that several shares have: the workgroups of all these shares but the last, kJoinGroups
 // each, take its (row, 8 dimensions) items in turn. A lane loads eight parts at once; where a tile has
 // more, several lanes divide them, so that each has few trips to memory.
@@ -446,7 +747,7 @@ struct Joined {
     }
 };
 
-template <int L, bool kHalf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf>
 __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     constexpr int kFlight = 8;
     __shared__ v4f s_acc[2][kJoinThreads];
@@ -455,7 +756,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     int64_t first;
     Work f;
     const int share = blockIdx.x / kJoinGroups;
-    const Shares shares = find_step<kTile, kJoinThreads / 64>(p, kKeys, share, true, r, f, first);
+    const Shares shares = find_step<kTile, kJoinThreads / 64, kSpareOf>(p, kStep, share, true, r, f, first);
     if (share >= shares.count) return;
     const int64_t share1 = shares.begin(share + 1);
     const int tile = (int)((share1 - 1 - first) / f.steps);
@@ -470,8 +771,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     const int at_once = kJoinThreads / slices;
     const int slice = threadIdx.x / at_once, lane_item = threadIdx.x % at_once;
     // the first share's second part, then the first of each following
-    const float* const from = p.parts + (2 * (int64_t)share0 + 1) * part_floats(L);
-    auto part_at = [&](int i) { return from + (int64_t)(2 * i - (i > 0)) * part_floats(L); };
+    const float* const from = p.parts + (2 * (int64_t)share0 + 1) * part_floats(L, kTile);
+    auto part_at = [&](int i) { return from + (int64_t)(2 * i - (i > 0)) * part_floats(L, kTile); };
     const int me = (share - share0) * kJoinGroups + blockIdx.x % kJoinGroups, workers = (parts - 1) * kJoinGroups;
     for (int item0 = me * at_once; item0 < items; item0 += workers * at_once) {
         const int item = item0 + lane_item < items ? item0 + lane_item : items - 1;
@@ -527,13 +828,24 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     }
 }
 
-template <int L, bool kHalf>
-hipError_t run(const LatentPlan& p, hipStream_t s) {
-    hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf>
+hipError_t join(const LatentPlan& p, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_latent_join<L, kHalf>), dim3((unsigned)(p.shares * kJoinGroups)), dim3(kJoinThreads), 0, s, p);
+    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf>), dim3((unsigned)(p.shares * kJoinGroups)),
+                       dim3(kJoinThreads), 0, s, p);
     return hipGetLastError();
+}
+
+// Tiles of 16 rows where that leaves a request one of them: the host knows the average request alone.
+template <int L, bool kHalf>
+hipError_t run(const LatentPlan& p, hipStream_t s) {
+    if (p.n_tokens * p.group <= (int64_t)kFewRows16 * p.R) {
+        hipLaunchKernelGGL((k_latent_few<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
+        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare>(p, s);
+    }
+    hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
+    return join<L, kHalf, kTile, kKeys, kSpare>(p, s);
 }
 
 template <int L>
@@ -545,7 +857,7 @@ hipError_t run_kind(const LatentPlan& p, hipStream_t s) {
 
 // One workgroup a compute unit, two parts each.
 int64_t latent_workspace(int latent, int cus) {
-    return 2ll * cus * part_floats(latent) * (int64_t)sizeof(float);
+    return 2ll * cus * part_floats(latent, kTile) * (int64_t)sizeof(float);
 }
 
 hipError_t launch_latent(const LatentPlan& p, hipStream_t s) {

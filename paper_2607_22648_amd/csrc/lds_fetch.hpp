@@ -15,6 +15,11 @@ __device__ inline void fetch16(const uint8_t* base, uint32_t offset, uint32_t ld
 __device__ inline void fetch16_at(const uint8_t* at, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(lds) : "memory");
 }
+// The same for what is read once: past the caches' usual order.
+__device__ inline void fetch16_once(const uint8_t* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(base), "s"(lds)
+                 : "memory");
+}
 __device__ inline void fetch4_at(const int32_t* at, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(lds) : "memory");
 }

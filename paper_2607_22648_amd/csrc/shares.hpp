@@ -20,7 +20,9 @@ struct Work {
     __device__ int64_t all() const { return (int64_t)steps * tiles; }
 };
 
-template <int kRows, class Plan>
+// kSpare: steps without keys at each tile's end, for what a tile takes beside its keys: equal shares of short
+// requests would last longer.
+template <int kRows, int kSpare = 0, class Plan>
 __device__ inline Work work_of(const Plan& p, int r, int step_keys) {
     Work w;
     const int64_t a = p.offsets[r], b = p.offsets[r + 1];
@@ -31,7 +33,7 @@ __device__ inline Work work_of(const Plan& p, int r, int step_keys) {
     const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
     int64_t end = w.past + w.n;
     end = end < 1 ? 1 : (end > limit ? limit : end);
-    w.steps = (int32_t)((end + step_keys - 1) / step_keys);
+    w.steps = (int32_t)((end + step_keys - 1) / step_keys) + kSpare;
     w.tiles = (w.n * p.group + kRows - 1) / kRows;
     return w;
 }
@@ -39,9 +41,13 @@ __device__ inline Work work_of(const Plan& p, int r, int step_keys) {
 // The shares: share w of `count` has steps [w all / count, (w + 1) all / count).
 struct Shares {
     int64_t all, count;
-    __device__ int64_t begin(int64_t w) const { return w * all / count; }
+    __device__ int64_t begin(int64_t w) const { return divided(w * all, count); }
     // the share that has step x: the last that begins at or before it
-    __device__ int64_t of(int64_t x) const { return ((x + 1) * count + all - 1) / all - 1; }
+    __device__ int64_t of(int64_t x) const { return divided((x + 1) * count + all - 1, all) - 1; }
+    // (a division of 64 bits takes a microsecond)
+    static __device__ int64_t divided(int64_t a, int64_t b) {
+        return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+    }
 };
 
 // Sums the batch's work, `of(r)` for each request, and finds the request `r` that the first (or last) step of
@@ -99,11 +105,11 @@ __device__ inline Shares find_share(int R, int64_t count, const Of& of, int64_t 
     return s;
 }
 
-template <int kRows, int kWavesOf, class Plan>
+template <int kRows, int kWavesOf, int kSpare = 0, class Plan>
 __device__ inline Shares find_step(const Plan& p, int step_keys, int64_t share, bool last, int& r, Work& f,
                                    int64_t& first) {
     return find_share<kWavesOf>(
-        p.R, p.shares, [&](int i) { return work_of<kRows>(p, i, step_keys); }, share, last, r, f, first);
+        p.R, p.shares, [&](int i) { return work_of<kRows, kSpare>(p, i, step_keys); }, share, last, r, f, first);
 }
 
 }  // namespace ptsd
