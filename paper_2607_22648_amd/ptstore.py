@@ -1009,7 +1009,6 @@ class _Paged:
                                  next_free.data_ptr()), stream)
         return slots, positions, held_out, next_free
 
-
     def weights(self, layers: Optional[Tuple[int, int]] = None) -> torch.Tensor:
         """Weights of nothing yet, [layers, cache_blocks, kv_heads, block_tokens], for layers[0] .. layers[1] - 1
         (None: all), which have the same KV heads: what `weigh` takes a layer of, and `evict` all."""
