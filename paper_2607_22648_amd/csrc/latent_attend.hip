@@ -26,6 +26,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kKeys = 32;    // of a piece
 constexpr int kSpare = 8;    // pieces' time that a tile takes beside its keys
+constexpr int kLeast = 2;    // steps of a share at least: a cut tile's parts are written and read again
 constexpr int kTile = 128;   // query rows
 constexpr int kStages = 3;   // pieces in LDS: one is computed while two are on their way
 constexpr int kAhead = kStages - 1;
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     int r;
     int64_t first;  // the request's first step
     Work f;
-    Shares shares = find_step<kTile, kWaves, kSpare>(p, kKeys, share, false, r, f, first);
+    Shares shares = find_step<kTile, kWaves, kSpare, kLeast>(p, kKeys, share, false, r, f, first);
     shares = {uniform(shares.all), uniform(shares.count)};
     if (share >= shares.count) return;
     first = uniform(first);
@@ -747,7 +748,7 @@ struct Joined {
     }
 };
 
-template <int L, bool kHalf, int kTile, int kStep, int kSpareOf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf>
 __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     constexpr int kFlight = 8;
     __shared__ v4f s_acc[2][kJoinThreads];
@@ -756,7 +757,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     int64_t first;
     Work f;
     const int share = blockIdx.x / kJoinGroups;
-    const Shares shares = find_step<kTile, kJoinThreads / 64, kSpareOf>(p, kStep, share, true, r, f, first);
+    const Shares shares = find_step<kTile, kJoinThreads / 64, kSpareOf, kLeastOf>(p, kStep, share, true, r, f, first);
     if (share >= shares.count) return;
     const int64_t share1 = shares.begin(share + 1);
     const int tile = (int)((share1 - 1 - first) / f.steps);
@@ -828,11 +829,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     }
 }
 
-template <int L, bool kHalf, int kTile, int kStep, int kSpareOf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf>
 hipError_t join(const LatentPlan& p, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf>), dim3((unsigned)(p.shares * kJoinGroups)),
+    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf, kLeastOf>), dim3((unsigned)(p.shares * kJoinGroups)),
                        dim3(kJoinThreads), 0, s, p);
     return hipGetLastError();
 }
@@ -842,10 +843,10 @@ template <int L, bool kHalf>
 hipError_t run(const LatentPlan& p, hipStream_t s) {
     if (p.n_tokens * p.group <= (int64_t)kFewRows16 * p.R) {
         hipLaunchKernelGGL((k_latent_few<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
-        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare>(p, s);
+        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare, 1>(p, s);
     }
     hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
-    return join<L, kHalf, kTile, kKeys, kSpare>(p, s);
+    return join<L, kHalf, kTile, kKeys, kSpare, kLeast>(p, s);
 }
 
 template <int L>

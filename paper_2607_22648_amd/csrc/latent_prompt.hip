@@ -27,6 +27,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kFormKeys = 128;  // of a workgroup that forms keys and values
 constexpr int kFormWaves = 8, kFormThreads = kFormWaves * 64;  // four for a head
+constexpr int kFewKeys = 32;    // of a workgroup where there are few keys
+constexpr int kFewTurns = 4;    // workgroups of few keys a compute unit, at most
 constexpr int kDies = 8;
 constexpr int kDieBytes = 2 << 20;  // of matrices that a die goes through: half of its L2
 constexpr int kKeys = 32;       // of a step of the attention
@@ -151,6 +153,7 @@ __global__ __launch_bounds__(kFormThreads) void k_form(ExpandedPlan p) {
 #pragma unroll
         for (int k = 0; k < L / 64; ++k) {
             if (k + 1 < L / 64) load(head, k + 1, x[(k + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);  // (or the loads move down to where registers are free)
             const v4u(&now)[8] = x[k & 1];
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -213,6 +216,91 @@ __global__ __launch_bounds__(kFormThreads) void k_form(ExpandedPlan p) {
             }
         }
     }
+    }
+}
+
+// The same of few keys: a workgroup takes 32 of them and the 128 rows of a head's keys or of its values, a wave 16 rows,
+// all loads on their way at once. What such a call takes is the matrices' way to the compute units, about 40 GB/s
+// each: spread over four times as many, 28 keys of 16 heads are formed in 8 us, not 25.
+template <int L, bool kHalf>
+__global__ __launch_bounds__(kFormThreads) void k_form_few(ExpandedPlan p) {
+    using E = Elem<kHalf>;
+    using V8 = typename E::v8;
+    constexpr int kLine = L * 2 + 16;  // bytes in LDS, as above
+    constexpr int kOutLine = kRow + 16;
+    static_assert(kValue == 16 * kFormWaves && kNope == kValue, "a wave takes 16 rows of a matrix");
+    __shared__ __attribute__((aligned(256))) uint8_t s_rows[kFewKeys * kLine];
+    __shared__ __attribute__((aligned(16))) uint8_t s_out[kFewKeys * kOutLine];
+    __shared__ uint32_t s_at[kFewKeys];
+    __shared__ int32_t s_there[kFewKeys];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, h4 = lane >> 4;
+    const int units = 2 * p.heads;  // of a tile of keys
+    const int64_t key0 = (int64_t)(blockIdx.x / units) * kFewKeys;
+    const int unit = blockIdx.x % units, head = unit >> 1;
+    const bool value = unit & 1;
+    const Rows& w = value ? p.wv : p.wk;
+    const uint8_t* const matrix =
+        (const uint8_t*)w.p + ((int64_t)head * w.head + (int64_t)(wave * 16 + n) * w.token + h4 * 8) * 2;
+    v4u x[L / 32];
+#pragma unroll
+    for (int k = 0; k < L / 32; ++k) x[k] = *(const v4u*)(matrix + k * 64);
+    __builtin_amdgcn_sched_barrier(0);
+    if (threadIdx.x < kFewKeys) {
+        uint32_t at;
+        const bool there = row_of(p, key0 + threadIdx.x, at);
+        s_at[threadIdx.x] = at;
+        s_there[threadIdx.x] = there;
+        if (unit == 0 && key0 + threadIdx.x < p.n_keys) p.there[key0 + threadIdx.x] = there;
+    }
+    __syncthreads();
+    const uint32_t lds = lds_of(s_rows);
+#pragma unroll
+    for (int i = 0; i < kFewKeys / kFormWaves; ++i) {
+        const int j = wave * (kFewKeys / kFormWaves) + i;
+        const uint8_t* const row = p.kv.rows + ((uint64_t)__builtin_amdgcn_readfirstlane(s_at[j]) << 4);
+        if (L == 512 || lane < L / 8) fetch16(row, (uint32_t)lane * 16, lds + j * kLine);
+    }
+    const v4u zero = {0u, 0u, 0u, 0u};
+    const int shared_row = threadIdx.x / 8, shared_at = threadIdx.x % 8 * 16;  // the shared parts, 8 lanes a row
+    if (unit == 0 && shared_row < kFewKeys && key0 + shared_row < p.n_keys) {
+        const v4u y = *(const v4u*)(p.kv.rows + (((uint64_t)s_at[shared_row] + L / 8) << 4) + shared_at);
+        *(v4u*)(p.rope + (key0 + shared_row) * (kRope * 2) + shared_at) = s_there[shared_row] ? y : zero;
+    }
+    arrive<0>();
+    // rows that are not there are zeros
+#pragma unroll
+    for (int i = 0; i < kFewKeys / kFormWaves; ++i) {
+        const int j = wave * (kFewKeys / kFormWaves) + i;
+        if (!s_there[j] && lane < L / 8) *(v4u*)(s_rows + j * kLine + lane * 16) = zero;
+    }
+    __syncthreads();
+    v4f o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};  // [16 values][16 keys]
+#pragma unroll
+    for (int k = 0; k < L / 32; ++k)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            o[t] = E::mma16(__builtin_bit_cast(V8, x[k]),
+                            __builtin_bit_cast(V8, *(const v4u*)(s_rows + (t * 16 + n) * kLine + k * 64 + h4 * 16)), o[t]);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        v2u near, left;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t rest;
+            near[h] = split2<kHalf>(o[t][2 * h], o[t][2 * h + 1], rest);
+            left[h] = rest;
+        }
+        uint8_t* const to = s_out + (t * 16 + n) * kOutLine + wave * 32 + h4 * 8;
+        *(v2u*)to = near;
+        *(v2u*)(to + kRow / 2) = left;
+    }
+    __syncthreads();
+    uint8_t* const out = (value ? p.v : p.k) + ((int64_t)head * p.n_keys + key0) * kRow;
+#pragma unroll
+    for (int i = 0; i < kFewKeys * kRow / 16 / kFormThreads; ++i) {
+        const int at = threadIdx.x + i * kFormThreads, key = at / (kRow / 16), c = at % (kRow / 16);
+        if (key0 + key < p.n_keys) *(v4u*)(out + (int64_t)key * kRow + c * 16) = *(const v4u*)(s_out + key * kOutLine + c * 16);
     }
 }
 
@@ -463,9 +551,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
 template <int L, bool kHalf>
 hipError_t run(const ExpandedPlan& p, int cus, hipStream_t s) {
     if (p.n_keys > 0) {
-        // one workgroup a compute unit, as LDS allows
-        const int grid = (cus + kDies - 1) / kDies * kDies;
-        hipLaunchKernelGGL((k_form<L, kHalf>), dim3((unsigned)grid), dim3(kFormThreads), 0, s, p);
+        const int64_t few = (p.n_keys + kFewKeys - 1) / kFewKeys * 2 * p.heads;
+        if (few <= kFewTurns * cus) {
+            hipLaunchKernelGGL((k_form_few<L, kHalf>), dim3((unsigned)few), dim3(kFormThreads), 0, s, p);
+        } else {
+            // one workgroup a compute unit, as LDS allows
+            const int grid = (cus + kDies - 1) / kDies * kDies;
+            hipLaunchKernelGGL((k_form<L, kHalf>), dim3((unsigned)grid), dim3(kFormThreads), 0, s, p);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

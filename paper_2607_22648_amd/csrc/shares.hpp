@@ -52,8 +52,8 @@ struct Shares {
 
 // Sums the batch's work, `of(r)` for each request, and finds the request `r` that the first (or last) step of
 // share `share` of `count` is in, its work and its first step. Every workgroup does so for
-// itself: thread t takes the requests from t ceil(R / threads) on.
-template <int kWavesOf, class W, class Of>
+// itself: thread t takes the requests from t ceil(R / threads) on. kLeast: steps of a share, of a batch of few.
+template <int kWavesOf, int kLeast = 1, class W, class Of>
 __device__ inline Shares find_share(int R, int64_t count, const Of& of, int64_t share, bool last, int& r, W& f,
                                     int64_t& first) {
     __shared__ int64_t s_sum[kWavesOf], s_first;
@@ -82,7 +82,7 @@ __device__ inline Shares find_share(int R, int64_t count, const Of& of, int64_t 
         if (i < wave) before += s_sum[i];
         s.all += s_sum[i];
     }
-    if (s.all < s.count) s.count = s.all;
+    if (s.all < s.count * kLeast) s.count = (s.all + kLeast - 1) / kLeast;
     const int64_t lo = before + scan - mine;
     const int64_t at = share >= s.count ? -1 : last ? s.begin(share + 1) - 1 : s.begin(share);
     if (at >= lo && at < lo + mine) {
@@ -105,10 +105,10 @@ __device__ inline Shares find_share(int R, int64_t count, const Of& of, int64_t 
     return s;
 }
 
-template <int kRows, int kWavesOf, int kSpare = 0, class Plan>
+template <int kRows, int kWavesOf, int kSpare = 0, int kLeast = 1, class Plan>
 __device__ inline Shares find_step(const Plan& p, int step_keys, int64_t share, bool last, int& r, Work& f,
                                    int64_t& first) {
-    return find_share<kWavesOf>(
+    return find_share<kWavesOf, kLeast>(
         p.R, p.shares, [&](int i) { return work_of<kRows, kSpare>(p, i, step_keys); }, share, last, r, f, first);
 }
 
