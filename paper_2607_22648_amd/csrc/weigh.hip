@@ -10,7 +10,7 @@
 // second factor, and goes through the query rows that see it, 32 at a time, which pass through LDS for
 // all four. Where 32 are all that a request has they stay there, and the waves go from tile to tile by
 // themselves. (Key tile, 32 rows) items of the batch, those above the diagonal left out, are laid end to end and
-// cut into equal shares, as decode.hip's steps; a tile of more than 16 items may be cut, and a second kernel
+// cut into equal shares, as decode.hip's steps; a tile of more than 4 items may be cut, and a second kernel
 // adds what its shares found, in order: the same inputs give the same bits.
 #include <type_traits>
 
@@ -25,7 +25,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kRowsOf = 32;  // query rows of an item
-constexpr int kWhole = 16;   // items of a tile that is not cut
+constexpr int kWhole = 4;    // items of a tile that is not cut
 constexpr int kLatent = 2;   // kinds of keys: 16 bits, 4 bits, latent rows
 
 constexpr int keys_of(int layout) { return kWaves * (layout == kLatent ? 32 : 64); }  // of a tile
