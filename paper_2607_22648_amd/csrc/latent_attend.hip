@@ -27,6 +27,7 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kKeys = 32;    // of a piece
 constexpr int kSpare = 8;    // pieces' time that a tile takes beside its keys
 constexpr int kLeast = 2;    // steps of a share at least: a cut tile's parts are written and read again
+constexpr int kWhole = 4;    // pieces of a tile that is not cut: the share that it begins in takes all of it
 constexpr int kTile = 128;   // query rows
 constexpr int kStages = 3;   // pieces in LDS: one is computed while two are on their way
 constexpr int kAhead = kStages - 1;
@@ -122,8 +123,13 @@ __global__ __launch_bounds__(kThreads) void k_latent(LatentPlan p) {
     }
     const int tile = (int)((done - first) / f.steps);
     const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
+    const bool whole = f.steps <= kWhole + kSpare;
+    if (whole && done > tile0) {  // the share before has it
+        done = tile0 + f.steps;
+        continue;
+    }
     const int step0 = (int)(done - tile0);
-    const int step1 = share1 - tile0 < f.steps ? (int)(share1 - tile0) : f.steps;
+    const int step1 = whole || share1 - tile0 >= f.steps ? f.steps : (int)(share1 - tile0);
     done = tile0 + step1;
 
     // the tile's rows see keys up to `end`; those of this share are [k0, k1)
@@ -426,6 +432,7 @@ constexpr int kFewRows16 = 16;
 constexpr int kFewKeys = 16;                 // of a piece
 constexpr int kFewStep = kWaves * kFewKeys;  // of a share's step
 constexpr int kFewSpare = 2;                 // steps that a tile takes beside its keys
+constexpr int kFewWhole = 1;                 // steps of a tile that is not cut
 
 // A piece in LDS: rows' latent parts, padded by 16 bytes, row r in place few_place(r): 16 lanes that read a
 // column of 16 rows find 16 places, and the 8 rows whose 32 bytes 32 lanes read as values are 32 bytes apart.
@@ -478,8 +485,13 @@ __global__ __launch_bounds__(kThreads) void k_latent_few(LatentPlan p) {
     }
     const int tile = (int)((done - first) / f.steps);
     const int64_t tile0 = first + (int64_t)tile * f.steps;  // the tile's first step
+    const bool whole = f.steps <= kFewWhole + kFewSpare;
+    if (whole && done > tile0) {  // the share before has it
+        done = tile0 + f.steps;
+        continue;
+    }
     const int step0 = (int)(done - tile0);
-    const int step1 = share1 - tile0 < f.steps ? (int)(share1 - tile0) : f.steps;
+    const int step1 = whole || share1 - tile0 >= f.steps ? f.steps : (int)(share1 - tile0);
     done = tile0 + step1;
 
     // the tile's rows see keys up to `end`; those of this share are [k0, k1)
@@ -748,7 +760,7 @@ struct Joined {
     }
 };
 
-template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf, int kWholeOf>
 __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     constexpr int kFlight = 8;
     __shared__ v4f s_acc[2][kJoinThreads];
@@ -758,7 +770,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     Work f;
     const int share = blockIdx.x / kJoinGroups;
     const Shares shares = find_step<kTile, kJoinThreads / 64, kSpareOf, kLeastOf>(p, kStep, share, true, r, f, first);
-    if (share >= shares.count) return;
+    if (share >= shares.count || f.steps <= kWholeOf + kSpareOf) return;
     const int64_t share1 = shares.begin(share + 1);
     const int tile = (int)((share1 - 1 - first) / f.steps);
     const int64_t tile0 = first + (int64_t)tile * f.steps, tile1 = tile0 + f.steps;
@@ -829,11 +841,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     }
 }
 
-template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf, int kWholeOf>
 hipError_t join(const LatentPlan& p, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf, kLeastOf>), dim3((unsigned)(p.shares * kJoinGroups)),
+    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf, kLeastOf, kWholeOf>), dim3((unsigned)(p.shares * kJoinGroups)),
                        dim3(kJoinThreads), 0, s, p);
     return hipGetLastError();
 }
@@ -843,10 +855,10 @@ template <int L, bool kHalf>
 hipError_t run(const LatentPlan& p, hipStream_t s) {
     if (p.n_tokens * p.group <= (int64_t)kFewRows16 * p.R) {
         hipLaunchKernelGGL((k_latent_few<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
-        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare, 1>(p, s);
+        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare, 1, kFewWhole>(p, s);
     }
     hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
-    return join<L, kHalf, kTile, kKeys, kSpare, kLeast>(p, s);
+    return join<L, kHalf, kTile, kKeys, kSpare, kLeast, kWhole>(p, s);
 }
 
 template <int L>

@@ -600,20 +600,31 @@ def _strided_rows(t: torch.Tensor, shape, kind: int, name: str):
     return (t.data_ptr(), *(s if n > 1 else 0 for n, s in zip(t.shape[:-1], t.stride()[:-1])))
 
 
+def _plane_rows(t: torch.Tensor, n: int, dim: int, kind: int, name: str):
+    """_strided_rows of [n, dim], in less time where all is well."""
+    if n > 1 and t.is_cuda and t.dtype is _KV_DTYPES[kind] and t.shape == (n, dim):
+        token, one = t.stride()
+        if one == 1:
+            return t.data_ptr(), token
+    return _strided_rows(t, (n, dim), kind, name)
+
+
 def _latent_rows(cache: ptstore_latent_t, latent, rope, slots):
     n = slots.numel()
-    return (*_strided_rows(latent, (n, cache.latent_dim), cache.kind, "latent"),
-            *_strided_rows(rope, (n, cache.rope_dim), cache.kind, "rope"), _arg(slots, torch.int64, n, "slots"), n)
+    return (*_plane_rows(latent, n, cache.latent_dim, cache.kind, "latent"),
+            *_plane_rows(rope, n, cache.rope_dim, cache.kind, "rope"), _arg(slots, torch.int64, n, "slots"), n)
 
 
 def ptstore_latent_append(cache: ptstore_latent_t, latent, rope, slots, stream=None) -> None:
-    _check("ptstore_latent_append", _lib.ptstore_latent_append(
-        C.byref(cache), *_latent_rows(cache, latent, rope, slots), _stream(stream)))
+    rc = _lib.ptstore_latent_append(C.byref(cache), *_latent_rows(cache, latent, rope, slots), _stream(stream))
+    if rc:
+        _check("ptstore_latent_append", rc)
 
 
 def ptstore_latent_read(cache: ptstore_latent_t, latent, rope, slots, stream=None) -> None:
-    _check("ptstore_latent_read", _lib.ptstore_latent_read(
-        C.byref(cache), *_latent_rows(cache, latent, rope, slots), _stream(stream)))
+    rc = _lib.ptstore_latent_read(C.byref(cache), *_latent_rows(cache, latent, rope, slots), _stream(stream))
+    if rc:
+        _check("ptstore_latent_read", rc)
 
 
 def ptstore_latent_attention_workspace(cache: ptstore_latent_t) -> int:
@@ -1207,10 +1218,14 @@ class LatentCache(_Paged):
     def read(self, layer: int, slots, stream=None):
         """The rows that `slots` of a layer hold: [tokens, latent_dim], [tokens, rope_dim]."""
         c = self._planes[layer]
+        n, dim, shared = slots.numel(), c.latent_dim, c.rope_dim
         with self._on(stream):
-            latent = slots.new_empty((slots.numel(), c.latent_dim), dtype=self.dtype)
-            rope = slots.new_empty((slots.numel(), c.rope_dim), dtype=self.dtype)
-        ptstore_latent_read(c, latent, rope, slots, stream)
+            latent = slots.new_empty((n, dim), dtype=self.dtype)
+            rope = slots.new_empty((n, shared), dtype=self.dtype)
+        rc = _lib.ptstore_latent_read(C.byref(c), latent.data_ptr(), dim, rope.data_ptr(), shared,
+                                      _arg(slots, torch.int64, n, "slots"), n, _stream(stream))
+        if rc:
+            _check("ptstore_latent_read", rc)
         return latent, rope
 
     def attend(self, layer: int, q_latent, q_rope, offsets, context, block_table, scale: float, out=None,

@@ -101,6 +101,12 @@ def test_absorbed_split_requests(P):
     check(P, "bf16", 512, 16, 4, [1] * 600, [i % 50 for i in range(600)], seed=6)
 
 
+def test_absorbed_short_requests(P):
+    """Tiles that are not cut beside some that are, at the sizes where that begins."""
+    check(P, "bf16", 256, 16, 33, [2, 1, 3, 1, 2, 4], [126, 127, 128, 30, 500, 95], seed=11)
+    check(P, "fp16", 512, 16, 16, [1] * 9, [126, 127, 128, 129, 255, 0, 600, 127, 1000], seed=12)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 def test_absorbed_sharp_scores(P, kind):
     """Scores of tens to hundreds: nearly all the weight on one key, maxima that rise by much."""
@@ -201,6 +207,14 @@ def check_expanded(P, kind, latent, page, heads, new, past, seed=0, hole=False, 
     (1, [1], [0]), (4, [65], [0]), (3, [33, 0, 130], [0, 7, 64]), (2, [1, 260], [200, 1]), (5, [128, 1], [128, 63])])
 def test_expanded(P, kind, latent, heads, new, past):
     check_expanded(P, kind, latent, 16, heads, new, past, seed=heads)
+
+
+@pytest.mark.parametrize("kind,latent,heads,new,past,hole", [
+    ("bf16", 512, 7, [3, 40], [2400, 90], True), ("fp16", 256, 8, [1, 2, 0, 3], [1500, 300, 0, 500], False),
+    ("bf16", 256, 33, [1, 2], [600, 20], True), ("fp16", 512, 16, [2], [1030], False)])
+def test_expanded_many_keys(P, kind, latent, heads, new, past, hole):
+    """More than 1,024 (32 keys, head, keys or values): 128 keys and pairs of heads a workgroup."""
+    check_expanded(P, kind, latent, 16, heads, new, past, seed=heads, hole=hole)
 
 
 @pytest.mark.parametrize("page", [1, 7, 24, 64])
