@@ -12,6 +12,11 @@
 //
 // Rows go from memory to LDS without passing through registers, 32 keys a piece, three pieces in
 // turn, and are read there as they lie for the first product, transposed for the second.
+//
+// Measured: 32 requests of 128 heads, up to two tokens each behind 500 to 8,190, 72 us (39 GFLOP, 540 TFLOP/s;
+// instructions to issue and the parts' 135 MB are what bounds it) and 24 for the join; tiles of 16 rows: 64
+// requests of 16 heads behind 120 to 8,190 tokens 66 us (309 MB, 4.7 TB/s; past its fixed 20 us it reads at 6.6), one
+// of 777 tokens 14, and 12 and 6 for their joins.
 #include <type_traits>
 
 #include "attend.hpp"
@@ -27,7 +32,10 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kKeys = 32;    // of a piece
 constexpr int kSpare = 8;    // pieces' time that a tile takes beside its keys
 constexpr int kLeast = 2;    // steps of a share at least: a cut tile's parts are written and read again
-constexpr int kWhole = 4;    // pieces of a tile that is not cut: the share that it begins in takes all of it
+// Pieces of a tile that is not cut: the share that it begins in takes all of it. 2 prompts of up to 45 tokens, 16 heads,
+// 28 us a call (with none 31), 6 drafts of 64 heads 35 (40), 12 requests of 64 heads behind up to 1,025 tokens 34
+// (32; with twelve pieces 43).
+constexpr int kWhole = 4;
 constexpr int kTile = 128;   // query rows
 constexpr int kStages = 3;   // pieces in LDS: one is computed while two are on their way
 constexpr int kAhead = kStages - 1;
@@ -727,11 +735,12 @@ __global__ __launch_bounds__(kThreads) void k_latent_few(LatentPlan p) {
     }
 }
 
-// Joins the parts of a tile that several shares have: the workgroups of all these shares but the last, kJoinGroups
-// each, take its (row, 8 dimensions) items in turn. A lane loads eight parts at once; where a tile has
-// more, several lanes divide them, so that each has few trips to memory.
+// Joins the parts of a tile that several shares have: the workgroups of all these shares but the last, kGroupsOf
+// each (64 requests of 16 heads: 82 us with two, 86 with four; 32 of 128 heads 99 and 94), take its (row, 8
+// dimensions) items in turn. A lane loads eight parts at once; where a tile has more, several lanes divide
+// them, so that each has few trips to memory.
 constexpr int kJoinThreads = 512;
-constexpr int kJoinGroups = 4;
+constexpr int kJoinGroups = 4, kFewJoinGroups = 2;  // of a tile of 128, and of 16 rows
 
 // A row's parts so far: 8 dimensions of the output, the maximum, the sum.
 struct Joined {
@@ -760,7 +769,7 @@ struct Joined {
     }
 };
 
-template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf, int kWholeOf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf, int kWholeOf, int kGroupsOf>
 __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     constexpr int kFlight = 8;
     __shared__ v4f s_acc[2][kJoinThreads];
@@ -768,7 +777,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     int r;
     int64_t first;
     Work f;
-    const int share = blockIdx.x / kJoinGroups;
+    const int share = blockIdx.x / kGroupsOf;
     const Shares shares = find_step<kTile, kJoinThreads / 64, kSpareOf, kLeastOf>(p, kStep, share, true, r, f, first);
     if (share >= shares.count || f.steps <= kWholeOf + kSpareOf) return;
     const int64_t share1 = shares.begin(share + 1);
@@ -786,7 +795,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     // the first share's second part, then the first of each following
     const float* const from = p.parts + (2 * (int64_t)share0 + 1) * part_floats(L, kTile);
     auto part_at = [&](int i) { return from + (int64_t)(2 * i - (i > 0)) * part_floats(L, kTile); };
-    const int me = (share - share0) * kJoinGroups + blockIdx.x % kJoinGroups, workers = (parts - 1) * kJoinGroups;
+    const int me = (share - share0) * kGroupsOf + blockIdx.x % kGroupsOf, workers = (parts - 1) * kGroupsOf;
     for (int item0 = me * at_once; item0 < items; item0 += workers * at_once) {
         const int item = item0 + lane_item < items ? item0 + lane_item : items - 1;
         const int trow = item % rows, c = item / rows;
@@ -841,11 +850,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_latent_join(LatentPlan p) {
     }
 }
 
-template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf, int kWholeOf>
+template <int L, bool kHalf, int kTile, int kStep, int kSpareOf, int kLeastOf, int kWholeOf, int kGroupsOf>
 hipError_t join(const LatentPlan& p, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf, kLeastOf, kWholeOf>), dim3((unsigned)(p.shares * kJoinGroups)),
+    hipLaunchKernelGGL((k_latent_join<L, kHalf, kTile, kStep, kSpareOf, kLeastOf, kWholeOf, kGroupsOf>), dim3((unsigned)(p.shares * kGroupsOf)),
                        dim3(kJoinThreads), 0, s, p);
     return hipGetLastError();
 }
@@ -855,10 +864,10 @@ template <int L, bool kHalf>
 hipError_t run(const LatentPlan& p, hipStream_t s) {
     if (p.n_tokens * p.group <= (int64_t)kFewRows16 * p.R) {
         hipLaunchKernelGGL((k_latent_few<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
-        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare, 1, kFewWhole>(p, s);
+        return join<L, kHalf, kFewRows16, kFewStep, kFewSpare, 1, kFewWhole, kFewJoinGroups>(p, s);
     }
     hipLaunchKernelGGL((k_latent<L, kHalf>), dim3((unsigned)p.shares), dim3(kThreads), 0, s, p);
-    return join<L, kHalf, kTile, kKeys, kSpare, kLeast, kWhole>(p, s);
+    return join<L, kHalf, kTile, kKeys, kSpare, kLeast, kWhole, kJoinGroups>(p, s);
 }
 
 template <int L>

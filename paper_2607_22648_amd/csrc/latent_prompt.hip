@@ -14,6 +14,10 @@
 // O^T = V^T P^T. Keys lie next to each other and need no conversion, so they go to LDS without passing
 // registers, 32 a step, into one of two buffers while the other is computed from. Two workgroups share a
 // compute unit.
+//
+// Measured: 6 prompts of 33 to 3,500 tokens, 16 heads, 80 us for forming 10,599 keys (44 GFLOP) and 286 for the
+// attention (45 % of its cycles in the matrix units, the rest mostly vector instructions that they wait for); 4 requests
+// behind up to 3,584 tokens, 32 heads, 165 (12,828 keys; 420 MB written) and 241.
 #include <type_traits>
 
 #include "attend.hpp"
@@ -221,7 +225,9 @@ __global__ __launch_bounds__(kFormThreads) void k_form(ExpandedPlan p) {
 
 // The same of few keys: a workgroup takes 32 of them and the 128 rows of a head's keys or of its values, a wave 16 rows,
 // all loads on their way at once. What such a call takes is the matrices' way to the compute units, about 40 GB/s
-// each: spread over four times as many, 28 keys of 16 heads are formed in 8 us, not 25.
+// each: spread over four times as many, 28 keys of 16 heads are formed in 8 us, not 25. Up to four workgroups
+// a compute unit (3 prompts of up to 389 tokens, 16 heads, 53 us a call with both kernels, 57 by the one above; with
+// eight, 2 prompts of up to 997 tokens 91, and 80).
 template <int L, bool kHalf>
 __global__ __launch_bounds__(kFormThreads) void k_form_few(ExpandedPlan p) {
     using E = Elem<kHalf>;

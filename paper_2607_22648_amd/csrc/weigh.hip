@@ -12,6 +12,10 @@
 // themselves. (Key tile, 32 rows) items of the batch, those above the diagonal left out, are laid end to end and
 // cut into equal shares, as decode.hip's steps; a tile of more than 4 items may be cut, and a second kernel
 // adds what its shares found, in order: the same inputs give the same bits.
+//
+// Measured: a step of 64 requests of 120 to 8,190 tokens, 8 heads of 128, 121 us (562 MB, 4.6 TB/s: 16 rows of K are
+// a load, whose 64 lanes take 64-byte pieces); of 32 over latent rows 34 (4.5 TB/s); prompts of 128 to 1,500 tokens over
+// 4 bits 96 (the exponentials and products, about alike).
 #include <type_traits>
 
 #include "attend.hpp"
