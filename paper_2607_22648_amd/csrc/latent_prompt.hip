@@ -321,20 +321,24 @@ constexpr float kBehind = 8.f;
 template <bool kHalf>
 constexpr float kRoom = Elem<kHalf>::kRoom + (kHalf ? 0.f : kBehind);
 
-template <bool kHalf>
-__global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
+// kSplit: 32 tokens a workgroup, whose waves take steps of keys in turn, each with an LDS buffer of its own and
+// no barrier, and join what they found at the end: for calls that are a few steps' chain.
+template <bool kHalf, bool kSplit>
+__global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedPlan p) {
     using E = Elem<kHalf>;
     using V8 = typename E::v8;
     constexpr int kSteps = kNope / 16, kRopeSteps = kRope / 16, kTiles = kValue / 32;
     constexpr int kRopeRow = kRope * 2;  // bytes
     constexpr int kRopeAt = kKeys * kRow, kValueAt = kRopeAt + kKeys * kRopeRow, kBuffer = kValueAt + kKeys * kRow;
     static_assert(kNope * 4 == kRow && kValue * 4 == kRow, "rows of keys and of values are alike");
-    __shared__ __attribute__((aligned(256))) uint8_t s_mem[2 * kBuffer];
+    constexpr int kTileRows = kSplit ? 32 : kPromptRows;
+    __shared__ __attribute__((aligned(256))) uint8_t s_mem[(kSplit ? kWaves : 2) * kBuffer];
+    __shared__ float s_max[kWaves][32], s_sum[kWaves][32];  // of the waves, where they join
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int head = blockIdx.x % p.heads;
     // the last tiles of a request see the most keys: they go first
-    const Tile f = find_tile(p, gridDim.x / p.heads - 1 - blockIdx.x / p.heads, kPromptRows);
+    const Tile f = find_tile(p, gridDim.x / p.heads - 1 - blockIdx.x / p.heads, kTileRows);
     if (f.tile < 0) return;
 
     // the request's packed keys
@@ -343,14 +347,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
     const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
     if (first < 0 || count < 0 || first + count > p.n_keys) count = 0;
     if (count > limit) count = limit;
-    const int row0 = f.tile * kPromptRows + wave * 32;
+    const int row0 = f.tile * kTileRows + (kSplit ? 0 : wave * 32);
     const int token = row0 + n < f.n ? row0 + n : f.n - 1;
     // (a row that sees no key, and one that sees them all, are at the ends of this range)
     auto clip = [&](int64_t x) { return (int32_t)(x < -1 ? -1 : (x < count ? x : count - 1)); };
     auto uniform = [&](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };
-    const int last_row = f.tile * kPromptRows + kPromptRows < f.n ? f.tile * kPromptRows + kPromptRows - 1 : f.n - 1;
+    const int last_row = f.tile * kTileRows + kTileRows < f.n ? f.tile * kTileRows + kTileRows - 1 : f.n - 1;
     const int32_t end = uniform(clip(f.past + last_row) + 1);
-    const int32_t tile_sees = uniform(clip(f.past + f.tile * kPromptRows));
+    const int32_t tile_sees = uniform(clip(f.past + f.tile * kTileRows));
     const int32_t all_see = uniform(clip(f.past + (row0 < f.n ? row0 : f.n - 1)));
     const int32_t pos = clip(f.past + token);
     const int steps = (end + kKeys - 1) / kKeys;
@@ -378,20 +382,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
     bool endless = false;  // a value that is not finite lies behind the first row's last key
 
     const uint32_t lds = lds_of(s_mem);
-    // A step's rows 8 wave .. + 7 into LDS, keys past the end as the last one.
+    // A step's rows 8 wave .. + 7 into LDS (a wave by itself: all 32), keys past the end as the last one.
     auto fetch = [&](int t, int buffer) {
         const int32_t at = t * kKeys, last = end - 1 - at;
         const uint32_t to = lds + buffer * kBuffer;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // two rows of 512 bytes
-            const int j0 = 8 * wave + 2 * i, j = j0 + half, key = j < last ? j : last;
-            fetch16(keys + (int64_t)at * kRow, (uint32_t)(key * kRow + (n ^ turn_k(j)) * 16), to + j0 * kRow);
-            fetch16(values + (int64_t)at * kRow, (uint32_t)(key * kRow + (n ^ turn_v(j)) * 16),
-                    to + kValueAt + j0 * kRow);
+        for (int g = 0; g < (kSplit ? 4 : 1); ++g) {
+            const int first_row = 8 * (kSplit ? g : wave);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {  // two rows of 512 bytes
+                const int j0 = first_row + 2 * i, j = j0 + half, key = j < last ? j : last;
+                fetch16(keys + (int64_t)at * kRow, (uint32_t)(key * kRow + (n ^ turn_k(j)) * 16), to + j0 * kRow);
+                fetch16(values + (int64_t)at * kRow, (uint32_t)(key * kRow + (n ^ turn_v(j)) * 16),
+                        to + kValueAt + j0 * kRow);
+            }
+            const int j = first_row + (lane >> 3), key = j < last ? j : last;
+            fetch16(shared + (int64_t)at * kRopeRow, (uint32_t)(key * kRopeRow + ((lane & 7) ^ turn_rope(j)) * 16),
+                    to + kRopeAt + first_row * kRopeRow);
         }
-        const int j0 = 8 * wave, j = j0 + (lane >> 3), key = j < last ? j : last;
-        fetch16(shared + (int64_t)at * kRopeRow, (uint32_t)(key * kRopeRow + ((lane & 7) ^ turn_rope(j)) * 16),
-                to + kRopeAt + j0 * kRopeRow);
     };
     // whether a lane's key of a step is there
     auto is_there = [&](int t) {
@@ -413,21 +421,27 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
     }
 
     int32_t flag = 0;
-    if (steps > 0) {
+    if (!kSplit && steps > 0) {
         flag = is_there(0);
         fetch(0, 0);
     }
-    for (int t = 0; t < steps; ++t) {
-        const int buf = t & 1;
+    for (int t = kSplit ? wave : 0; t < steps; t += kSplit ? kWaves : 1) {
+        const int buf = kSplit ? wave : t & 1;
         const int32_t at = t * kKeys;
+        if (kSplit) {
+            flag = is_there(t);
+            fetch(t, buf);
+        }
         // the step is whole behind the barrier, and all waves are done with the other buffer
         arrive<0>();
         uint32_t ok = (uint32_t)__ballot(flag != 0 && at + n < end);
         asm volatile("" : "+s"(ok));  // (here, where nothing is under way: a wait for the flag costs nothing)
-        barrier();
-        if (t + 1 < steps) {
-            flag = is_there(t + 1);
-            fetch(t + 1, buf ^ 1);
+        if (!kSplit) {
+            barrier();
+            if (t + 1 < steps) {
+                flag = is_there(t + 1);
+                fetch(t + 1, buf ^ 1);
+            }
         }
         uint8_t* const mem = s_mem + buf * kBuffer;
         if (at + kKeys - 1 > tile_sees) {
@@ -441,13 +455,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
             }
             if (__any(found)) {
                 endless = true;
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                for (int j = j0 + (lane >> 4) + 4 * wave; j < kKeys; j += 16) {
+                if (!kSplit) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                for (int j = j0 + (lane >> 4) + (kSplit ? 0 : 4 * wave); j < kKeys; j += kSplit ? 4 : 16) {
                     v4u* const to = (v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
                     v4u x = *to;
                     if (drop_endless<kHalf>(x)) *to = x;
                 }
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                if (kSplit)
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                else
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
         }
         v16f s;
@@ -515,10 +532,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
             for (int i = 0; i < kTiles; ++i)
                 o[i] = E::mma32(__builtin_bit_cast(V8, vt[i]), __builtin_bit_cast(V8, w[b >> 1]), o[i]);
         }
+        if (kSplit) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the step is read: the next may overwrite it
     }
     if (endless)
         for (int32_t key = tile_sees + 1; key < end; ++key) {
-            if (key > pos) continue;
+            if (key > pos || (kSplit && key / kKeys % kWaves != wave)) continue;
             const uint16_t* x = (const uint16_t*)(values + (int64_t)key * kRow);
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
@@ -529,6 +547,58 @@ __global__ __launch_bounds__(kThreads, 2) void k_expanded(ExpandedPlan p) {
                                                          : __uint_as_float((uint32_t)y << 16));
                 }
         }
+    if constexpr (kSplit) {
+        sum += __shfl_xor(sum, 32);
+        if (half == 0) {
+            s_max[wave][n] = top;
+            s_sum[wave][n] = sum;
+        }
+        __syncthreads();  // all are done with their steps, too
+        float all = kLowest;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all = fmaxf(all, s_max[w][n]);
+        const float less = exp2_of(top - all);
+        float* const x = (float*)s_mem;  // [wave][dimensions / 4][row][4]
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                *(v4f*)(x + ((wave * (kValue / 4) + 8 * i + 2 * a + half) * 32 + n) * 4) =
+                    v4f{o[i][4 * a] * less, o[i][4 * a + 1] * less, o[i][4 * a + 2] * less, o[i][4 * a + 3] * less};
+        __syncthreads();
+        // a row and 16 dimensions a thread
+        const int jr = threadIdx.x % 32, jc = threadIdx.x / 32, jt = f.tile * kTileRows + jr;
+        if (jt >= f.n) return;
+        all = kLowest;
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all = fmaxf(all, s_max[w][jr]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) total += exp2_of(s_max[w][jr] - all) * s_sum[w][jr];
+        const float inv = total != 0.f ? 1.f / total : 0.f;
+        uint8_t* const out = (uint8_t*)p.out.p + ((f.begin + jt) * p.out.token + head * p.out.head + jc * 16) * 2;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v4u y;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                v4f a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const v4f part = *(const v4f*)(x + ((w * (kValue / 4) + 4 * jc + 2 * h + b) * 32 + jr) * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[e] += part[e];
+                }
+                y[2 * b] = pack2<kHalf>(a[0] * inv, a[1] * inv);
+                y[2 * b + 1] = pack2<kHalf>(a[2] * inv, a[3] * inv);
+            }
+            *(v4u*)(out + h * 16) = y;
+        }
+        if (p.lse && jc == 0)
+            p.lse[(f.begin + jt) * p.heads + head] =
+                total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+        return;
+    }
     if (row0 + n >= f.n) return;  // both halves of a row leave together
     sum += __shfl_xor(sum, 32);
     // no key, or none with a weight: zeros, and the logarithm of nothing
@@ -568,9 +638,13 @@ hipError_t run(const ExpandedPlan& p, int cus, hipStream_t s) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int64_t tiles = p.R == 1 ? (p.n_tokens + kPromptRows - 1) / kPromptRows
-                                   : tile_bound(p.n_tokens, 1, p.R, kPromptRows);
-    hipLaunchKernelGGL((k_expanded<kHalf>), dim3((unsigned)(tiles * p.heads)), dim3(kThreads), 0, s, p);
+    auto tiles = [&](int rows) { return p.R == 1 ? (p.n_tokens + rows - 1) / rows : tile_bound(p.n_tokens, 1, p.R, rows); };
+    // Tiles of 32 where those of 128 leave half of the compute units idle: 2 prompts of up to 272 tokens, 8 heads,
+    // 26 us a call (33), 500 tokens of 32 heads 53 (59); where they leave none, 1,000 tokens of 32 heads 101 (84).
+    if (2 * tiles(kPromptRows) * p.heads <= cus)
+        hipLaunchKernelGGL((k_expanded<kHalf, true>), dim3((unsigned)(tiles(32) * p.heads)), dim3(kThreads), 0, s, p);
+    else
+        hipLaunchKernelGGL((k_expanded<kHalf, false>), dim3((unsigned)(tiles(kPromptRows) * p.heads)), dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 

@@ -205,6 +205,19 @@ def test_requests_that_share_pages(P):
     assert torch.equal(b.attend(), got)
 
 
+@pytest.mark.parametrize("heads", [2, 40])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_expanded_hidden_values(P, heads, bad):
+    """A later token's infinite row leaves the rows before it alone, in tiles of 32 and of 128 tokens."""
+    b = Batch(P, [140, 3, 1, 1], [45, 20, 300, 0], heads=heads, seed=19)
+    clean = b.expanded()
+    pos = 45 + 100  # the 101st new token
+    b.rows[int(b.host[2][0, pos // 16]), pos % 16, 7] = bad
+    got = b.expanded()
+    assert torch.equal(got[:100], clean[:100]) and torch.equal(got[140:], clean[140:])
+    assert not bool(torch.isfinite(got[100:140]).all(-1).any())
+
+
 # --- planes past 32 bits -----------------------------------------------------------------
 
 
