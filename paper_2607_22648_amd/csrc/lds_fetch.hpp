@@ -1,5 +1,5 @@
 // Loads from memory to LDS that pass no registers, and the waits for them (latent_attend.hip,
-// latent_prompt.hip).
+// latent_prompt.hip, weigh.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -20,7 +20,10 @@ __device__ inline void fetch16_once(const uint8_t* base, uint32_t offset, uint32
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(base), "s"(lds)
                  : "memory");
 }
-__device__ inline void fetch4_at(const int32_t* at, uint32_t lds) {
+__device__ inline void fetch16_once_at(const uint8_t* at, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(at), "s"(lds) : "memory");
+}
+__device__ inline void fetch4_at(const void* at, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(lds) : "memory");
 }
 // Waits until at most kLeft of the wave's loads are under way; its LDS reads are done, too.

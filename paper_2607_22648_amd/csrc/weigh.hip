@@ -10,12 +10,12 @@
 // second factor, and goes through the query rows that see it, 32 at a time, which pass through LDS for
 // all four. Where 32 are all that a request has they stay there, and the waves go from tile to tile by
 // themselves. (Key tile, 32 rows) items of the batch, those above the diagonal left out, are laid end to end and
-// cut into equal shares, as decode.hip's steps; a tile of more than 4 items may be cut, and a second kernel
+// cut into equal shares, as decode.hip's steps; a tile of more than 4 (16) items may be cut, and a second kernel
 // adds what its shares found, in order: the same inputs give the same bits.
 //
-// Measured: a step of 64 requests of 120 to 8,190 tokens, 8 heads of 128, 121 us (562 MB, 4.6 TB/s: 16 rows of K are
-// a load, whose 64 lanes take 64-byte pieces); of 32 over latent rows 34 (4.5 TB/s); prompts of 128 to 1,500 tokens over
-// 4 bits 96 (the exponentials and products, about alike).
+// Measured: a step of 64 requests of 120 to 8,190 tokens, 8 heads of 128, 93 us (562 MB, 6.0 TB/s); of 32 over latent
+// rows 34 (4.5 TB/s: 16 rows are a load, whose 64 lanes take 64-byte pieces); prompts of 128 to 1,500 tokens over 4 bits
+// 96 (the exponentials and products, about alike).
 #include <type_traits>
 
 #include "attend.hpp"
@@ -29,7 +29,6 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kRowsOf = 32;  // query rows of an item
-constexpr int kWhole = 4;    // items of a tile that is not cut
 constexpr int kLatent = 2;   // kinds of keys: 16 bits, 4 bits, latent rows
 
 constexpr int keys_of(int layout) { return kWaves * (layout == kLatent ? 32 : 64); }  // of a tile
@@ -152,13 +151,13 @@ __device__ inline void weigh(const WeighPlan& p, int block, uint8_t (&s_q)[2][We
         }
         const int32_t tile = kStream ? (int32_t)(done - first) : tile_of(f, done - first);
         const int64_t tile0 = kStream ? done : first + f.before(tile), tile1 = kStream ? done + 1 : first + f.before(tile + 1);
-        if (!kStream && f.rows <= kWhole && done > tile0) {  // the share before has all of it
+        if (!kStream && f.rows <= p.whole && done > tile0) {  // the share before has all of it
             done = tile1;
             continue;
         }
         const int32_t row_first = kStream ? 0 : f.first_row(tile);
         const int32_t rt0 = row_first + (int32_t)(done - tile0);
-        const int64_t stop = f.rows <= kWhole || tile1 < share1 ? tile1 : share1;
+        const int64_t stop = f.rows <= p.whole || tile1 < share1 ? tile1 : share1;
         const int32_t rt1 = row_first + (int32_t)(stop - tile0);
         const bool part = done > tile0 || stop < tile1;
         float* const to = p.parts + (2 * (int64_t)block + (done > tile0 ? 0 : 1)) * kTile;
@@ -414,6 +413,193 @@ __device__ inline void weigh(const WeighPlan& p, int block, uint8_t (&s_q)[2][We
     }
 }
 
+// Requests of one row tile over 16-bit keys: as the other kernel's stream, but K passes through LDS, whole rows a load
+// and nothing through registers on its way; each wave has four places for 32 keys and fetches three ahead, and of
+// page entries, which places follow from, six. 64 requests of 120 to 8,190 tokens take 93 us; with keys in registers,
+// 64-byte pieces a load, 121; without the hint that rows are read once 107.
+template <int kDim, bool kHalf>
+__global__ __launch_bounds__(kThreads) void k_weigh_stream(WeighPlan p) {
+    using E = Elem<kHalf>;
+    using V8 = typename E::v8;
+    constexpr int kTile = keys_of(0), kSteps = kDim / 32, kColumns = kDim / 8;
+    constexpr int kRow = kDim * 2 + 16;                // of a query in LDS, as above
+    constexpr int kHalfKeys = 32, kPart = kHalfKeys * kDim * 2;
+    constexpr int kLines = 64 / kColumns, kFetches = kHalfKeys / kLines;  // rows of a load, loads of a half
+    constexpr int kPlaces = 4, kAhead = kPlaces - 1, kEntries = 2 * kPlaces;
+    constexpr int kOps = kFetches + 2;                 // loads of a turn: entries, rows, old weights
+    __shared__ __attribute__((aligned(256))) uint8_t s_keys[kWaves][kPlaces][kPart];
+    __shared__ int32_t s_entry[kWaves][kEntries][64];
+    __shared__ float s_old[kWaves][kPlaces][64];
+    __shared__ __attribute__((aligned(16))) uint8_t s_q[kRowsOf * kRow];
+    __shared__ __attribute__((aligned(16))) float s_lse[kRowsOf];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, h4 = lane >> 4;
+    // (a die's workgroups, every eighth, so read pages of all heads: 106 us and 113 where it had one head)
+    const int head = blockIdx.x / p.streams, share = blockIdx.x % p.streams;
+    int r;
+    int64_t first;
+    Items f;
+    const Shares shares = find_share<kWaves>(
+        p.R, p.streams, [&](int i) { return items_of(p, i, kTile, true); }, share, false, r, f, first);
+    if (share >= shares.count) return;
+    const int64_t share1 = shares.begin(share + 1);
+    for (int64_t done = shares.begin(share); done < share1;) {
+        while (done >= first + f.all()) {
+            first += f.all();
+            f = items_of(p, ++r, kTile, true);
+        }
+        const int32_t tile = (int32_t)(done - first);
+        const int64_t left = first + f.all() < share1 ? first + f.all() - done : share1 - done;
+        done += left;
+        const int32_t halves = 2 * (int32_t)left;
+        const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
+        const int32_t end = (int32_t)((int64_t)f.past + f.n < limit ? (int64_t)f.past + f.n : limit);
+        const int all_rows = f.n * p.group;
+        const int32_t* const table = p.table + (int64_t)r * p.max_blocks;
+        const int32_t had = p.weighed ? p.weighed[r] : p.context[r];  // tokens that have weights
+
+        __syncthreads();  // all are done with the rows before
+        auto place = [&](int j, int& token, int& sub) {
+            const int row = j < all_rows ? j : all_rows - 1;
+            token = (int)div_page((uint32_t)row, p.rows_div);
+            sub = row - token * p.group;
+        };
+#pragma unroll
+        for (int i = 0; i < kRowsOf * kColumns / kThreads; ++i) {
+            const int at = threadIdx.x + i * kThreads, c = at % kColumns, j = at / kColumns;
+            int token, sub;
+            place(j, token, sub);
+            *(v4u*)(s_q + j * kRow + c * 16) =
+                *(const v4u*)((const uint8_t*)p.q.p + ((f.begin + token) * p.q.token +
+                                                      (int64_t)(head * p.group + sub) * p.q.head) * 2 + c * 16);
+        }
+        if (threadIdx.x < kRowsOf) {
+            int token, sub;
+            place(threadIdx.x, token, sub);
+            const float lse = (int)threadIdx.x < all_rows
+                                  ? p.lse[(f.begin + token) * p.q_heads + head * p.group + sub] : -INFINITY;
+            // rows that saw no key, and those that do not exist, give nothing: a weight of 2^-inf
+            s_lse[threadIdx.x] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f;
+        }
+        __syncthreads();
+
+        // 16-byte columns of a row in LDS are turned, so that 16 lanes which read one of 16 rows find 16 places
+        auto turn = [](int row) { return kDim == 128 ? row & 15 : (row >> 1) & 7; };
+        auto key_of = [&](int32_t x) { return (tile + x / 2) * kTile + wave * 64 + x % 2 * kHalfKeys; };
+        auto look = [&](int32_t x) {  // entries of a half's keys (past the end: the last one's)
+            const int32_t key = key_of(x) + (lane & 31);
+            fetch4_at(table + div_page((uint32_t)(key < end ? key : end - 1), p.kv.div),
+                      lds_of(s_entry[wave][x % kEntries]));
+        };
+        // a lane's key of a half: whether it is there, and its line of the head and page
+        auto find = [&](int32_t x, int32_t& entry, uint32_t& slot) {
+            const int32_t key = key_of(x) + (lane & 31);
+            entry = s_entry[wave][x % kEntries][lane];
+            const bool there = key < end && entry >= 0 && entry < (int32_t)p.kv.blocks;
+            entry = there ? entry : 0;
+            slot = there ? (uint32_t)key - div_page((uint32_t)key, p.kv.div) * p.kv.div.page : 0u;
+            return there;
+        };
+        auto weight_of = [&](int32_t entry, uint32_t slot) {
+            return p.weights + ((int64_t)entry * p.kv.heads + head) * p.kv.div.page + slot;
+        };
+        auto fetch = [&](int32_t x) {
+            int32_t entry;
+            uint32_t slot;
+            find(x, entry, slot);
+            // in units of 16 bytes: a plane is 64 GiB at most
+            const uint32_t at = (uint32_t)entry * (p.kv.slab / 16) + ((uint32_t)head * p.kv.div.page + slot) * kColumns;
+            const uint32_t to = lds_of(s_keys[wave][x % kPlaces]);
+#pragma unroll
+            for (int i = 0; i < kFetches; ++i) {
+                const int j = i * kLines + lane / kColumns;
+                const uint32_t row = (uint32_t)__builtin_amdgcn_ds_bpermute(j * 4, (int)at);
+                fetch16_once_at(p.kv.k + ((uint64_t)(row + ((lane % kColumns) ^ turn(j))) << 4), to + i * 1024);
+            }
+            fetch4_at(weight_of(entry, slot), lds_of(s_old[wave][x % kPlaces]));
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) look(i);
+        arrive<0>();
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {  // as in the loop's turns before the first
+            look(kAhead + i);
+            if (i < halves) fetch(i);
+        }
+        float held = 0.f;  // an even half's weights: those of two are written at once
+        float* held_at = nullptr;
+        for (int32_t x = 0; x < halves; ++x) {
+            // Left under way: what the two turns before have fetched. Stores may be, too: then this waits for more.
+            if (x + kAhead - 1 < halves)
+                arrive<(kAhead - 1) * kOps>();
+            else
+                arrive<0>();
+            look(x + 2 * kAhead);
+            if (x + kAhead < halves) fetch(x + kAhead);
+            V8 k[2][kSteps];
+            const uint8_t* const mem = s_keys[wave][x % kPlaces];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i)
+                    k[c][i] = __builtin_bit_cast(V8, *(const v4u*)(mem + (16 * c + n) * (kDim * 2) +
+                                                                  ((4 * i + h4) ^ turn(n)) * 16));
+            const int32_t key0 = key_of(x);
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int up = 0; up < 2; ++up) {
+                const int row0 = 16 * up;
+                if (up && row0 >= all_rows) break;
+                v4f s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const V8 q = __builtin_bit_cast(V8, *(const v4u*)(s_q + (n + row0) * kRow + (4 * i + h4) * 16));
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) s[c] = E::mma16(q, k[c][i], s[c]);
+                }
+                // rows 4 h4 + e in s[..][e]
+                const v4f less = *(const v4f*)&s_lse[row0 + 4 * h4];
+                float w[2][4];
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[c][e] = exp2_of(__builtin_fmaf(s[c][e], p.scale2, -less[e]));
+                if (key0 + kHalfKeys - 1 > (int64_t)f.past + div_page((uint32_t)row0, p.rows_div)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t pos = (int64_t)f.past + div_page((uint32_t)(row0 + 4 * h4 + e), p.rows_div);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            if (key0 + 16 * c + n > pos) w[c][e] = 0.f;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) sum[c] += (w[c][0] + w[c][1]) + (w[c][2] + w[c][3]);
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                sum[c] += __shfl_xor(sum[c], 16);
+                sum[c] += __shfl_xor(sum[c], 32);
+            }
+            int32_t entry;
+            uint32_t slot;
+            const bool there = find(x, entry, slot);
+            const float old = key0 + (lane & 31) < had ? s_old[wave][x % kPlaces][lane] : 0.f;
+            const float now = old + (h4 & 1 ? sum[1] : sum[0]);
+            float* const now_at = there ? weight_of(entry, slot) : nullptr;
+            if (x & 1) {
+                float* const to = lane < kHalfKeys ? held_at : now_at;
+                if (to) *to = lane < kHalfKeys ? held : now;
+            }
+            held = now;
+            held_at = now_at;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the half is read: a later one may overwrite it
+        }
+        arrive<0>();  // entries that no half uses
+    }
+}
+
 // The first workgroups take the requests of one row tile, the others those of several: in one launch, since the
 // host does not know of which there are any.
 template <int kDim, bool kHalf, int kLayout>
@@ -437,7 +623,7 @@ __global__ __launch_bounds__(keys_of(kLayout)) void k_weigh_join(WeighPlan p) {
     Items f;
     const Shares shares = find_share<kTile / 64>(
         p.R, p.shares, [&](int i) { return items_of(p, i, kTile, false); }, share, true, r, f, first);
-    if (share >= shares.count || f.rows <= kWhole) return;
+    if (share >= shares.count || f.rows <= p.whole) return;
     const int64_t share0 = shares.begin(share), share1 = shares.begin(share + 1);
     const int32_t tile = tile_of(f, share1 - 1 - first);
     const int64_t tile0 = first + f.before(tile), tile1 = first + f.before(tile + 1);
@@ -461,15 +647,32 @@ template <int kDim, bool kHalf, int kLayout>
 hipError_t run(const WeighPlan& plan, hipStream_t s) {
     WeighPlan p = plan;
     const int64_t rows = p.n_tokens * p.group;
+    // Single tokens and drafts, by the average request. Items of a tile that is not cut: of these, more, since without
+    // cut tiles there is no second kernel (64 tokens 4 us less; 6 prompts of up to 92 tokens by 64 heads 20 us with 4,
+    // 34 with 16).
+    const bool few = rows <= (int64_t)kRowsOf * p.R;
+    p.whole = few ? 16 : 4;
     // As many workgroups of each kind as the device holds. Only of a single request does the host know how many
     // row tiles it has.
     const int32_t shares = shares_of(p.kv.heads, p.cus * weigh_waves(kDim));
     p.streams = p.R > 1 || rows <= kRowsOf ? shares : 0;
     p.shares = rows > kRowsOf ? shares : 0;
-    hipLaunchKernelGGL((k_weigh<kDim, kHalf, kLayout>), dim3((unsigned)((p.streams + p.shares) * p.kv.heads)),
-                       dim3(kThreads), 0, s, p);
+    if constexpr (kLayout == 0) {
+        // (beside longer requests in a launch of its own, which takes longer than it saves where those are most)
+        if (few && p.streams) {
+            p.streams = shares_of(p.kv.heads, p.cus);
+            hipLaunchKernelGGL((k_weigh_stream<kDim, kHalf>), dim3((unsigned)(p.streams * p.kv.heads)), dim3(kThreads), 0,
+                               s, p);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            p.streams = 0;
+        }
+    }
+    if (p.streams + p.shares > 0)
+        hipLaunchKernelGGL((k_weigh<kDim, kHalf, kLayout>), dim3((unsigned)((p.streams + p.shares) * p.kv.heads)),
+                           dim3(kThreads), 0, s, p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || rows <= kWhole * kRowsOf) return e;  // no request can have a tile that is cut
+    if (e != hipSuccess || rows <= p.whole * kRowsOf) return e;  // no request can have a tile that is cut
     hipLaunchKernelGGL((k_weigh_join<kLayout>), dim3((unsigned)(p.shares * p.kv.heads)), dim3(keys_of(kLayout)), 0, s, p);
     return hipGetLastError();
 }

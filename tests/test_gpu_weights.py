@@ -128,6 +128,17 @@ def test_weigh_pages_and_holes(P, page, heads, dim):
     check_weigh(P, "bf16", heads, dim, page, 4, [1, 40, 2], [130, 9, 300], seed=page, hole=True)
 
 
+@pytest.mark.parametrize("kind,heads,dim,page", [("bf16", 2, 128, 1), ("fp16", 1, 64, 7), ("bf16", 3, 64, 24), ("fp16", 2, 128, 64),
+                                                 ("mxfp4", 2, 128, 24), ("bf16", None, 256, 24)])
+def test_weigh_steps_beside_a_prompt(P, kind, heads, dim, page):
+    """Single tokens, drafts and requests without tokens, of lengths around a wave's 32 and 64 keys and a tile's 256,
+    with missing pages; one prompt among them, and none."""
+    new = [1, 1, 0, 2, 1, 1, 4, 1, 0, 1]
+    past = [0, 31, 9, 62, 63, 255, 256, 800, 0, 1500]
+    check_weigh(P, kind, heads, dim, page, 4, new, past, seed=page, hole=True)
+    check_weigh(P, kind, heads, dim, page, 4, new + [60], past + [130], seed=page + 1, hole=True, stride=True)
+
+
 @pytest.mark.parametrize("heads,dim", [(1, 128), (None, 256)])
 def test_weigh_cut_tiles(P, heads, dim):
     """Few keys and many rows: key tiles that several workgroups share."""
