@@ -109,6 +109,7 @@ int ptstore_latent_attention(const ptstore_latent_attention_t* a, void* stream) 
         !rows_ok(a->q_rope, a->q_rope_token_stride, a->q_rope_head_stride) ||
         !rows_ok(a->out, a->out_token_stride, a->out_head_stride))
         return refuse_as(call, "rows of the queries or of out null or not 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(a->lse) & 3) return refuse_as(call, "lse not 4-byte aligned");
     // no order is promised between a row's output and the reads of other rows' queries
     if (a->out == a->q_latent || a->out == a->q_rope) return refuse_as(call, "out must be neither of the queries");
     if (p.kv.blocks < 1) return refuse_as(call, "the cache has no blocks");
@@ -163,6 +164,7 @@ int ptstore_latent_attention_expanded(const ptstore_latent_expanded_t* a, void* 
     if (!rows_ok(a->w_k, a->w_k_row_stride, a->w_k_head_stride) ||
         !rows_ok(a->w_v, a->w_v_row_stride, a->w_v_head_stride))
         return refuse_as(call, "rows of w_k or w_v null or not 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(a->lse) & 3) return refuse_as(call, "lse not 4-byte aligned");
     // no order is promised between a row's output and the reads of other rows' queries
     if (a->out == a->q_nope || a->out == a->q_rope) return refuse_as(call, "out must be neither of the queries");
     if (p.kv.blocks < 1) return refuse_as(call, "the cache has no blocks");

@@ -1,8 +1,8 @@
 // New tokens' rows into the pages of a latent cache, and rows of pages back out: a copy, 16 bytes a
 // lane, consecutive lanes along a row of 72 (40) such pieces.
 //
-// Bound by memory: 2 bytes read and 2 written a value. 16,384 tokens of 576 values (38 MB) 8.6 us into pages and 5.4
-// out of them, faster than a copy's 6.6 in memory since the 256 MB cache holds what was just written; 64 tokens 2.3.
+// Bound by memory: 2 bytes read and 2 written a value. 16,384 tokens of 576 values (38 MB) take 8.7 us into pages and
+// 6.4 out of them, where the 256 MB cache still holds them (a copy from memory takes 6.6); 64 tokens 2.3.
 #include <hip/hip_runtime.h>
 
 #include "latent.hpp"

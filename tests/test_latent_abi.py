@@ -136,7 +136,7 @@ QUERIES = [(dict(q_rope=None), "null"), (dict(q_rope=AT + 8), "16-byte"), (dict(
     (dict(heads=0), "heads"), (dict(heads=-1), "heads"), (dict(q_latent=None), "null"), (dict(q_latent=AT + 2), "16-byte"),
     (dict(q_latent_token_stride=4100), "16-byte"), (dict(q_latent_head_stride=513), "16-byte"), (dict(out=None), "null"),
     (dict(out=AT + 40), "16-byte"), (dict(out_head_stride=513), "16-byte"), (dict(out=AT), "neither"),
-    (dict(out=AT + 16), "neither"), (dict(cache=latent(cache_blocks=0)), "no blocks")])
+    (dict(out=AT + 16), "neither"), (dict(lse=AT + 2), "4-byte"), (dict(cache=latent(cache_blocks=0)), "no blocks")])
 def test_attention_refused(over, word):
     refused(P.lib().ptstore_latent_attention(C.byref(attention_args(**over)), None), "ptstore_latent_attention", word)
 
@@ -145,7 +145,7 @@ def test_attention_refused(over, word):
     (dict(heads=0), "heads"), (dict(q_nope=None), "null"), (dict(q_nope=AT + 2), "16-byte"),
     (dict(q_nope_token_stride=1028), "16-byte"), (dict(out=AT), "neither"), (dict(out=AT + 16), "neither"), (dict(out=None), "null"),
     (dict(w_k=None), "w_k"), (dict(w_v=AT + 8), "w_v"), (dict(w_k_row_stride=500), "w_k"), (dict(w_v_head_stride=4), "w_v"),
-    (dict(key_offsets=None), "null"), (dict(n_keys=-1), "n_keys"), (dict(n_keys=(1 << 31) - 255), "n_keys"),
+    (dict(lse=AT + 1), "4-byte"), (dict(key_offsets=None), "null"), (dict(n_keys=-1), "n_keys"), (dict(n_keys=(1 << 31) - 255), "n_keys"),
     (dict(n_keys=1 << 30, heads=8), "tiles"), (dict(R=1 << 21, heads=8, n_tokens=2), "tiles"),
     (dict(cache=latent(cache_blocks=0)), "no blocks"), (dict(), "workspace"),
     (dict(workspace=AT + 8, workspace_bytes=1 << 40), "workspace"), (dict(workspace=AT, workspace_bytes=1000), "workspace")])
