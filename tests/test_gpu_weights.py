@@ -179,6 +179,91 @@ def test_weigh_touches_nothing_else_and_passes_nan(P):
 # --- eviction ---------------------------------------------------------------------------
 
 
+@pytest.mark.parametrize("heads,dim", [(2, 128), (1, 64), (None, 512)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_weigh_steps_do_not_see_what_is_not_theirs(P, heads, dim, bad):
+    """Single tokens and a draft: slots behind a request's last key and of missing pages hold what is not finite, and
+    so does a draft's last token; rows whose lse is minus infinity give nothing, NaN passes to what they see."""
+    new, past, page = [1, 1, 3], [45, 300, 20], 16
+    offsets, context, table, blocks = ref.batch(5, new, past, page)
+    cache = make(P, "bf16", heads, dim, blocks, page, 5)
+    kv_heads, size = heads or 1, dim if heads else dim + 64
+    rows = cache.data.view(torch.bfloat16).view(-1, blocks, kv_heads, page, size)
+    q = torch.randn((5, kv_heads * 4, size), generator=torch.Generator().manual_seed(6)).bfloat16().cuda()
+    args = (q,) if heads else (q[..., :dim], q[..., dim:])
+    batch = (offsets.cuda(), context.cuda(), table.cuda())
+    lse = torch.full((5, kv_heads * 4), 3.0, device="cuda")
+    start = cache.weights()[0]
+
+    def weigh(lse):
+        return cache.weigh(0, start.clone(), *args, lse, *batch, scale=0.05)
+    clean = weigh(lse)
+    used = torch.zeros((blocks, page), dtype=torch.bool)
+    where = [ref.keys_of(r, offsets, context, table, page, blocks)[1:] for r in range(3)]
+    for block, slot in where:
+        used[block, slot] = True
+    rows[0].transpose(1, 2)[~used.cuda()] = bad
+    assert torch.equal(weigh(lse), clean)
+    nothing = lse.clone()
+    nothing[1] = -math.inf  # the second request's token
+    block, slot = where[1]
+    want = clean.clone()
+    want[block.cuda(), :, slot.cuda()] = 0.0
+    assert torch.equal(weigh(nothing), want)
+    nothing[1] = math.nan
+    got = weigh(nothing)
+    assert bool(torch.isnan(got[block.cuda(), :, slot.cuda()]).all())
+    keep = [r for r in (0, 2)]
+    for r in keep:
+        block, slot = (x.cuda() for x in where[r])
+        assert torch.equal(got[block, :, slot], clean[block, :, slot])
+    # the draft's last token: the others' weights are as they were
+    block, slot = (x.cuda() for x in where[2])
+    rows[0][block[-1], :, slot[-1]] = bad
+    got = weigh(lse)
+    assert torch.equal(got[block[:-1], :, slot[:-1]], clean[block[:-1], :, slot[:-1]])
+
+
+@pytest.mark.parametrize("kind,dim,new", [("bf16", 128, [1, 1, 1]), ("mxfp4", 64, [1, 1, 1]), ("fp16", 64, [1, 70, 2])])
+def test_weighing_and_eviction_in_a_graph(P, kind, dim, new):
+    """Captured once, the first calls of their cache, replayed on other queries with eager work between: the same
+    weights, pages and lengths as eager calls on a copy; and the same again on a stream of its own."""
+    past, page, heads = [400, 90, 200], 16, 2
+    offsets, context, table, blocks = ref.batch(7, new, past, page)
+    cache, other = (make(P, kind, heads, dim, blocks, page, 7, layers=2) for _ in range(2))
+    other.data.copy_(cache.data)
+    n = int(offsets[-1])
+    q = torch.randn((n, heads * 4, dim), device="cuda").to(cache.dtype)
+    batch = (offsets.cuda(), context.cuda(), table.cuda())
+    length, keep = (context + torch.tensor(new, dtype=torch.int32)).cuda(), torch.tensor([300, 64, 9], dtype=torch.int32).cuda()
+    weights = cache.weights().uniform_()
+    start = weights.clone()
+    data = cache.data.clone()
+
+    def step(cache, weights, stream=None):
+        for layer in range(2):
+            _, lse = cache.attend(layer, q, *batch, lse=True, stream=stream)
+            cache.weigh(layer, weights[layer], q, lse, *batch, stream=stream)
+        return cache.evict(weights, length, batch[2], keep, 300, recent=16, stream=stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        after = step(cache, weights)
+    side = torch.cuda.Stream()
+    for i in range(4):
+        q.copy_(torch.randn_like(q))
+        for c in (cache, other):
+            c.data.copy_(data)
+        weights.copy_(start)
+        eager = start.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(other, eager, side if i % 2 else None)
+        torch.cuda.synchronize()
+        assert torch.equal(after, want)
+        assert torch.equal(weights.view(torch.int32), eager.view(torch.int32)) and torch.equal(cache.data, other.data)
+
+
 def evict_ref(weights, n, keep, recent):
     """Positions that stay of n, in order: a token's (NaN first, weight down, position) decides."""
     m = min(n, keep)
