@@ -3,7 +3,7 @@
 //
 // Two launches. The first finds what stays: a workgroup for each (layer, request, head) finds the
 // weight from which on tokens stay by three passes over the weights' bits, 11, 11 and 10 at a time, counting
-// them in LDS; then each wave goes through an eighth of the tokens, in order, once to count those that stay and once
+// them in LDS; then each wave goes through a sixteenth of the tokens, in order, once to count those that stay and once
 // to write their positions. The second moves rows and weights, bound by memory: what stays is read
 // and written once.
 //
@@ -26,10 +26,10 @@ namespace {
 
 typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 
-constexpr int kSelectThreads = 512;
+constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kReads = 8;        // weights of a lane under way
+constexpr int kReads = 4;        // weights of a lane under way
 constexpr int kCached = 12288;  // weights that stay in LDS between passes; of longer requests they are read again
 constexpr int kMoveThreads = 256;
 constexpr int kSlice = 8;       // 16-byte pieces of a row that a workgroup moves
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_keep_select(KeepPlan p) {
     int32_t* const source = p.source + (int64_t)unit * p.max_keep;
     const int32_t rest = k.n - k.recent;                   // candidates
     uint32_t want = (uint32_t)(k.m - k.recent);            // of them
-    // weights i0 + tid, .. + 512, ..: several at once, their pages first
+    // weights i0 + tid, .. + 1,024, ..: several at once, their pages first
     auto read = [&](int32_t i0, uint32_t (&x)[kReads]) {
         int32_t block[kReads];
         uint32_t slot[kReads];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_keep_select(KeepPlan p) {
             __syncthreads();
         }
     }
-    // In order, a wave an eighth of the tokens, 64 at a time: how many are above the border, and at it; then, with
+    // In order, a wave a sixteenth of the tokens, 64 at a time: how many are above the border, and at it; then, with
     // the sums of the waves before, the positions that stay.
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t each = ((k.n + 63) / 64 + kSelectWaves - 1) / kSelectWaves * 64;
@@ -416,7 +416,10 @@ hipError_t launch_keep(const KeepPlan& p, int cus, hipStream_t s) {
     const int planes = p.v ? 2 : 1, slices = slices_of(p), columns = columns_of(p);
     const PageDiv pieces = page_div(planes * columns);
     const int64_t want = (int64_t)kMovers * cus / keep_workgroups(p);
-    const int parts = want < 1 ? 1 : want < kMostParts ? (int)want : kMostParts;
+    const int kinds = planes * slices + 1;
+    const int64_t most = ((int64_t)p.max_keep + kinds * kTokens - 1) / (kinds * kTokens);  // that have tokens to move
+    int parts = want < 1 ? 1 : want < kMostParts ? (int)want : kMostParts;
+    if (parts > most) parts = most < 1 ? 1 : (int)most;
     const dim3 grid((unsigned)(keep_workgroups(p) * parts));
     if (p.power == 4)
         hipLaunchKernelGGL(k_keep_move<4>, grid, dim3(kMoveThreads), 0, s, p, planes, slices, columns, parts, pieces);
