@@ -13,9 +13,9 @@
 // request's pages are all others there is no order to keep: a unit's workgroups then take 64 tokens at a time,
 // all of their rows, whose places 64 lanes find for all.
 //
-// Measured: 16 requests of 250 to 8,000 tokens to a quarter, 2 layers of 8 heads, 18 us for the first and 58 for the
-// second (275 MB, 4.7 TB/s); one of 2,049 to half, 8 layers, 9 and 19 (chains of trips to memory; bytes take 12).
-// 512 threads instead of 256, or 16 rows of a lane under way, 38 to 51 us a call instead of 33.
+// Measured: 16 requests of 250 to 8,000 tokens to a quarter, 2 layers of 8 heads, 16 us for the first (with 512 threads
+// 18) and 59 for the second (275 MB, 4.7 TB/s); one of 2,049 to half, 8 layers, 10 and 15 (chains of trips to memory;
+// bytes take 12). Moved by 512 threads instead of 256, or with 16 rows of a lane under way, 38 to 51 us a call, not 33.
 #include <hip/hip_runtime.h>
 
 #include "lds_fetch.hpp"
