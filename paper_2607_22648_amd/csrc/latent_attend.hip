@@ -14,7 +14,7 @@
 // turn, and are read there as they lie for the first product, transposed for the second.
 //
 // Measured: 32 requests of 128 heads, up to two tokens each behind 500 to 8,190, 70 us (39 GFLOP, 560 TFLOP/s;
-// instructions to issue and the parts' 135 MB are what bounds it) and 24 for the join; tiles of 16 rows: 64
+// instructions to issue, then the parts' 80 MB, are what bounds it) and 24 for the join; tiles of 16 rows: 64
 // requests of 16 heads behind 120 to 8,190 tokens 67 us (309 MB, 4.6 TB/s; past its fixed 20 us it reads at 6.6), one
 // of 777 tokens 14, and 8 and 6 for their joins.
 #include <type_traits>
