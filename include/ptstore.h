@@ -728,8 +728,8 @@ int ptstore_latent_attention_expanded(const ptstore_latent_expanded_t *args, voi
  * Add to each cached token's weight what a batch's queries gave it: with key j of request r in slot s
  * and KV head g, over the query rows (token t, head h of g) that see it as in ptstore_attention,
  *   weights[s][g] = (j < weighed[r] ? weights[s][g] : 0) + sum_t,h exp(scale * q[t][h] . k_j - lse[t][h]).
- * lse is the attention's own: a row whose lse is minus infinity adds nothing, one whose lse is NaN makes
- * what it sees NaN. weighed NULL: context, so that new tokens start from nothing; smaller where
+ * lse is the attention's own: a row whose lse is minus infinity adds nothing (if its scores are finite),
+ * one whose lse is NaN makes what it sees NaN. weighed NULL: context, so that new tokens start from nothing; smaller where
  * tokens behind a loaded prefix have no weights yet. Slots of other tokens are not touched. Weights
  * are 32-bit sums throughout, off by the rounding of lse and of scores, 2^-23 of their size. The
  * same inputs give the same bits.
