@@ -33,6 +33,7 @@ constexpr int kFormKeys = 128;  // of a workgroup that forms keys and values
 constexpr int kFormWaves = 8, kFormThreads = kFormWaves * 64;  // four for a head
 constexpr int kFewKeys = 32;    // of a workgroup where there are few keys
 constexpr int kFewTurns = 4;    // workgroups of few keys a compute unit, at most
+constexpr int kGroupTurns = 1;  // workgroups of eight waves of the attention a compute unit, at most
 constexpr int kDies = 8;
 constexpr int kDieBytes = 2 << 20;  // of matrices that a die goes through: half of its L2
 constexpr int kKeys = 32;       // of a step of the attention
@@ -322,9 +323,10 @@ template <bool kHalf>
 constexpr float kRoom = Elem<kHalf>::kRoom + (kHalf ? 0.f : kBehind);
 
 // kSplit: 32 tokens a workgroup, whose waves take steps of keys in turn, each with an LDS buffer of its own and
-// no barrier, and join what they found at the end: for calls that are a few steps' chain.
-template <bool kHalf, bool kSplit>
-__global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedPlan p) {
+// no barrier, and join what they found at the end: for calls that are a few steps' chain. kGroups 2: eight waves,
+// the second four take every second step, in buffers of their own: for calls of one workgroup a compute unit.
+template <bool kHalf, bool kSplit, int kGroups>
+__global__ __launch_bounds__(kThreads * kGroups, kSplit || kGroups > 1 ? 1 : 2) void k_expanded(ExpandedPlan p) {
     using E = Elem<kHalf>;
     using V8 = typename E::v8;
     constexpr int kSteps = kNope / 16, kRopeSteps = kRope / 16, kTiles = kValue / 32;
@@ -332,9 +334,10 @@ __global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedP
     constexpr int kRopeAt = kKeys * kRow, kValueAt = kRopeAt + kKeys * kRopeRow, kBuffer = kValueAt + kKeys * kRow;
     static_assert(kNope * 4 == kRow && kValue * 4 == kRow, "rows of keys and of values are alike");
     constexpr int kTileRows = kSplit ? 32 : kPromptRows;
-    __shared__ __attribute__((aligned(256))) uint8_t s_mem[(kSplit ? kWaves : 2) * kBuffer];
+    __shared__ __attribute__((aligned(256))) uint8_t s_mem[(kSplit ? kWaves : 2 * kGroups) * kBuffer];
     __shared__ float s_max[kWaves][32], s_sum[kWaves][32];  // of the waves, where they join
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = all_waves % kWaves, group = all_waves / kWaves;
     const int n = lane & 31, half = lane >> 5;
     const int head = blockIdx.x % p.heads;
     // the last tiles of a request see the most keys: they go first
@@ -421,12 +424,12 @@ __global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedP
     }
 
     int32_t flag = 0;
-    if (!kSplit && steps > 0) {
-        flag = is_there(0);
-        fetch(0, 0);
+    if (!kSplit && group < steps) {
+        flag = is_there(group);
+        fetch(group, 2 * group);
     }
-    for (int t = kSplit ? wave : 0; t < steps; t += kSplit ? kWaves : 1) {
-        const int buf = kSplit ? wave : t & 1;
+    for (int t0 = kSplit ? wave : 0; t0 < steps; t0 += kSplit ? kWaves : kGroups) {
+        const int t = t0 + group, buf = kSplit ? wave : 2 * group + (t0 / kGroups & 1);
         const int32_t at = t * kKeys;
         if (kSplit) {
             flag = is_there(t);
@@ -438,25 +441,32 @@ __global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedP
         asm volatile("" : "+s"(ok));  // (here, where nothing is under way: a wait for the flag costs nothing)
         if (!kSplit) {
             barrier();
-            if (t + 1 < steps) {
-                flag = is_there(t + 1);
-                fetch(t + 1, buf ^ 1);
+            if (t + kGroups < steps) {
+                flag = is_there(t + kGroups);
+                fetch(t + kGroups, buf ^ 1);
             }
         }
         uint8_t* const mem = s_mem + buf * kBuffer;
-        if (at + kKeys - 1 > tile_sees) {
+        const int32_t last_key = (t0 + (kSplit ? 1 : kGroups)) * kKeys - 1;  // of the workgroup's steps
+        if (last_key > tile_sees) {
             // Values that are not finite, in rows that the tile's first row does not see (a weight of zero would
             // make them NaN), become zeros. Every wave looks at all of them, so that all agree.
             bool found = false;
             const int j0 = at > tile_sees ? 0 : tile_sees + 1 - at;
-            for (int j = j0 + (lane >> 4); j < kKeys; j += 4) {
-                v4u x = *(const v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
-                found |= drop_endless<kHalf>(x);
+            for (int g = 0; g < kGroups; ++g) {
+                if (t0 + g >= steps) break;
+                const int32_t from = (t0 + g) * kKeys;
+                const uint8_t* const step = kGroups > 1 ? s_mem + (2 * g + (t0 / kGroups & 1)) * kBuffer : mem;
+                const int32_t first_hidden = from > tile_sees ? 0 : tile_sees + 1 - from;
+                for (int j = (kGroups > 1 ? first_hidden : j0) + (lane >> 4); j < kKeys; j += 4) {
+                    v4u x = *(const v4u*)(step + kValueAt + j * kRow + (lane & 15) * 16);
+                    found |= drop_endless<kHalf>(x);
+                }
             }
             if (__any(found)) {
                 endless = true;
                 if (!kSplit) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                for (int j = j0 + (lane >> 4) + (kSplit ? 0 : 4 * wave); j < kKeys; j += kSplit ? 4 : 16) {
+                for (int j = j0 + (lane >> 4) + (kSplit ? 0 : 4 * wave); j < kKeys && t < steps; j += kSplit ? 4 : 16) {
                     v4u* const to = (v4u*)(mem + kValueAt + j * kRow + (lane & 15) * 16);
                     v4u x = *to;
                     if (drop_endless<kHalf>(x)) *to = x;
@@ -467,6 +477,7 @@ __global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedP
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
         }
+        if (kGroups > 1 && t >= steps) break;  // (the last turn of the second four)
         v16f s;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -536,7 +547,8 @@ __global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedP
     }
     if (endless)
         for (int32_t key = tile_sees + 1; key < end; ++key) {
-            if (key > pos || (kSplit && key / kKeys % kWaves != wave)) continue;
+            if (key > pos || (kSplit && key / kKeys % kWaves != wave) || (kGroups > 1 && key / kKeys % kGroups != group))
+                continue;
             const uint16_t* x = (const uint16_t*)(values + (int64_t)key * kRow);
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
@@ -599,6 +611,33 @@ __global__ __launch_bounds__(kThreads, kSplit ? 1 : 2) void k_expanded(ExpandedP
                 total != 0.f ? (all + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
         return;
     }
+    if constexpr (kGroups > 1) {
+        // the second four's maxima, sums and outputs through LDS, lane by lane
+        float* const x = (float*)s_mem + (wave * 64 + lane) * 4;
+        __syncthreads();  // all are done with their steps
+        if (group) {
+            ((v2f*)s_mem)[kWaves * 64 * kTiles * 8 + wave * 64 + lane] = v2f{top, sum};
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+                    *(v4f*)(x + (4 * i + a) * kWaves * 64 * 4) = v4f{o[i][4 * a], o[i][4 * a + 1], o[i][4 * a + 2], o[i][4 * a + 3]};
+        }
+        __syncthreads();
+        if (group) return;
+        const v2f other = ((const v2f*)s_mem)[kWaves * 64 * kTiles * 8 + wave * 64 + lane];
+        const float all = fmaxf(top, other[0]), less = exp2_of(top - all), other_less = exp2_of(other[0] - all);
+        sum = sum * less + other[1] * other_less;
+        top = all;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const v4f y = *(const v4f*)(x + (4 * i + a) * kWaves * 64 * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][4 * a + e] = o[i][4 * a + e] * less + y[e] * other_less;
+            }
+    }
     if (row0 + n >= f.n) return;  // both halves of a row leave together
     sum += __shfl_xor(sum, 32);
     // no key, or none with a weight: zeros, and the logarithm of nothing
@@ -641,10 +680,15 @@ hipError_t run(const ExpandedPlan& p, int cus, hipStream_t s) {
     auto tiles = [&](int rows) { return p.R == 1 ? (p.n_tokens + rows - 1) / rows : tile_bound(p.n_tokens, 1, p.R, rows); };
     // Tiles of 32 where those of 128 leave half of the compute units idle: 2 prompts of up to 272 tokens, 8 heads,
     // 26 us a call (33), 500 tokens of 32 heads 53 (59); where they leave none, 1,000 tokens of 32 heads 101 (84).
+    // Eight waves where a compute unit has one workgroup: 2,000 tokens of 16 heads 104 us (115), 1,000 of 32 79 (83);
+    // 6 prompts of 33 to 3,500 tokens, several workgroups a compute unit, 415 (371).
     if (2 * tiles(kPromptRows) * p.heads <= cus)
-        hipLaunchKernelGGL((k_expanded<kHalf, true>), dim3((unsigned)(tiles(32) * p.heads)), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((k_expanded<kHalf, true, 1>), dim3((unsigned)(tiles(32) * p.heads)), dim3(kThreads), 0, s, p);
+    else if (tiles(kPromptRows) * p.heads <= kGroupTurns * cus)
+        hipLaunchKernelGGL((k_expanded<kHalf, false, 2>), dim3((unsigned)(tiles(kPromptRows) * p.heads)),
+                           dim3(2 * kThreads), 0, s, p);
     else
-        hipLaunchKernelGGL((k_expanded<kHalf, false>), dim3((unsigned)(tiles(kPromptRows) * p.heads)), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((k_expanded<kHalf, false, 1>), dim3((unsigned)(tiles(kPromptRows) * p.heads)), dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 

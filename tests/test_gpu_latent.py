@@ -212,10 +212,11 @@ def test_expanded(P, kind, latent, heads, new, past):
 @pytest.mark.parametrize("kind,latent,heads,new,past,hole", [
     ("bf16", 512, 7, [3, 40], [2400, 90], True), ("fp16", 256, 8, [1, 2, 0, 3], [1500, 300, 0, 500], False),
     ("bf16", 256, 33, [1, 2], [600, 20], True), ("fp16", 512, 16, [2], [1030], False),
-    ("bf16", 256, 33, [1, 2, 0, 40, 7], [60, 20, 9, 0, 129], False)])
+    ("bf16", 256, 33, [1, 2, 0, 40, 7], [60, 20, 9, 0, 129], False),
+    ("fp16", 256, 33, [1, 2, 0, 40, 7, 3, 1, 130, 1], [60, 20, 9, 0, 129, 5, 0, 31, 64], True)])
 def test_expanded_many_keys(P, kind, latent, heads, new, past, hole):
-    """More than 1,024 (32 keys, head, keys or values): 128 keys and pairs of heads a workgroup. The last: more than
-    128 (128 tokens, head), tiles of 128 tokens."""
+    """More than 1,024 (32 keys, head, keys or values): 128 keys and pairs of heads a workgroup. The last two: more
+    than 128 (128 tokens, head), tiles of 128 tokens by eight waves, and more than 256, by four."""
     check_expanded(P, kind, latent, 16, heads, new, past, seed=heads, hole=hole)
 
 

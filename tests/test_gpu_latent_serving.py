@@ -205,10 +205,11 @@ def test_requests_that_share_pages(P):
     assert torch.equal(b.attend(), got)
 
 
-@pytest.mark.parametrize("heads", [2, 40])
+@pytest.mark.parametrize("heads", [2, 40, 65])
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 def test_expanded_hidden_values(P, heads, bad):
-    """A later token's infinite row leaves the rows before it alone, in tiles of 32 and of 128 tokens."""
+    """A later token's infinite row leaves the rows before it alone, in tiles of 32 tokens, and of 128 by eight waves
+    and by four."""
     b = Batch(P, [140, 3, 1, 1], [45, 20, 300, 0], heads=heads, seed=19)
     clean = b.expanded()
     pos = 45 + 100  # the 101st new token
