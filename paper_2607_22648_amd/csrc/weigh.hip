@@ -53,7 +53,8 @@ struct Items {
     }
 };
 
-// (of a request that has one row tile, or several: the others have none)
+// stream: of a request that has one row tile, and the others have none; else of the others, and where nothing else
+// takes those of one row tile, of them, too
 __device__ inline Items items_of(const WeighPlan& p, int r, int keys, bool stream) {
     Items w;
     int64_t a = p.offsets[r], b = p.offsets[r + 1];
@@ -71,7 +72,7 @@ __device__ inline Items items_of(const WeighPlan& p, int r, int keys, bool strea
     end = w.n == 0 ? 0 : end > limit ? limit : end;
     w.tiles = (int32_t)((end + keys - 1) / keys);
     w.rows = (int32_t)(((int64_t)w.n * p.group + kRowsOf - 1) / kRowsOf);
-    if ((w.rows == 1) != stream) w.tiles = 0;
+    if (stream ? w.rows != 1 : w.rows == 1 && p.apart) w.tiles = 0;
     w.seen = (int32_t)(past / keys);
     w.rise = (int64_t)(keys / kRowsOf) * p.group;
     w.late = (past % keys * p.group + kRowsOf - 1) / kRowsOf;
@@ -652,10 +653,11 @@ hipError_t run(const WeighPlan& plan, hipStream_t s) {
     // 34 with 16).
     const bool few = rows <= (int64_t)kRowsOf * p.R;
     p.whole = few ? 16 : 4;
-    // As many workgroups of each kind as the device holds. Only of a single request does the host know how many
-    // row tiles it has.
+    // As many workgroups of each kind as the device holds. Of a single request the host knows how many row tiles
+    // it has at most (rows before and behind it, and those before position 0, are not its), so it has one kind.
     const int32_t shares = shares_of(p.kv.heads, p.cus * weigh_waves(kDim));
-    p.streams = p.R > 1 || rows <= kRowsOf ? shares : 0;
+    p.apart = p.R > 1 || rows <= kRowsOf;
+    p.streams = p.apart ? shares : 0;
     p.shares = rows > kRowsOf ? shares : 0;
     if constexpr (kLayout == 0) {
         // (beside longer requests in a launch of its own, which takes longer than it saves where those are most)

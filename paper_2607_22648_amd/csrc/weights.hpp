@@ -23,6 +23,7 @@ struct WeighPlan {
     float* weights;  // [block][KV head][slot]
     float* parts;    // workspace
     int32_t streams, shares;  // of requests of one tile of query rows, of the others
+    bool apart;               // requests of one tile have workgroups of their own
     int32_t cus, whole;       // compute units; items of a tile that is not cut
     PageDiv rows_div;         // by group
 };
