@@ -670,9 +670,10 @@ int ptstore_latent_attention(const ptstore_latent_attention_t *args, void *strea
  *   out[t][h] = sum_j w_j v_hj / sum_j w_j,  w_j = exp(scale * (q_nope[t][h], q_rope[t][h]) . k_hj).
  * Keys have 128 values of a head's own beside the rope_dim shared ones, values 128. Request r has
  * key_offsets[r+1] - key_offsets[r] keys of the n_keys that the workspace has room for: at least
- * context[r] + its new tokens (keys past that do not exist); key_offsets rises from 0 to n_keys, and
- * a request for which it does not has no keys. Cost grows with all keys, past and new: behind a long
- * past and for few tokens the absorbed form is the shorter.
+ * context[r] + its new tokens (keys past that do not exist). key_offsets rises from 0 to n_keys; where it
+ * does not, a request whose own two do not rise within 0 .. n_keys has no keys, and another that shares places with
+ * a later one, or lies before an earlier one's, may find those keys or none. Cost grows with all keys, past and
+ * new: behind a long past and for few tokens the absorbed form is the shorter.
  */
 typedef struct {
     ptstore_latent_t cache;

@@ -50,8 +50,10 @@ __device__ inline bool row_of(const ExpandedPlan& p, int64_t x, uint32_t& at) {
     }
     at = 0;
     if (x >= p.n_keys || p.R < 1) return false;
-    const int64_t key = x - p.key_offsets[lo];
-    if (key < 0 || x >= p.key_offsets[lo + 1] || key >= (int64_t)p.max_blocks * p.kv.div.page) return false;
+    const int64_t first = p.key_offsets[lo];
+    if (first < 0 || first > x || x >= p.key_offsets[lo + 1]) return false;
+    const int64_t key = x - first;
+    if (key >= (int64_t)p.max_blocks * p.kv.div.page) return false;
     const uint32_t column = div_page((uint32_t)key, p.kv.div);
     const int32_t entry = p.table[(int64_t)lo * p.max_blocks + column];
     if (entry < 0 || entry >= p.kv.blocks) return false;
@@ -344,12 +346,14 @@ __global__ __launch_bounds__(kThreads * kGroups, kSplit || kGroups > 1 ? 1 : 2) 
     const Tile f = find_tile(p, gridDim.x / p.heads - 1 - blockIdx.x / p.heads, kTileRows);
     if (f.tile < 0) return;
 
-    // the request's packed keys
-    const int64_t first = p.key_offsets[f.r];
-    int64_t count = p.key_offsets[f.r + 1] - first;
-    const int64_t limit = (int64_t)p.max_blocks * p.kv.div.page;
-    if (first < 0 || count < 0 || first + count > p.n_keys) count = 0;
-    if (count > limit) count = limit;
+    // the request's packed keys: none where its offsets do not rise within 0 .. n_keys (compared before they are
+    // subtracted, which of any two numbers could overflow)
+    int64_t first = p.key_offsets[f.r], count = 0;
+    const int64_t past_last = p.key_offsets[f.r + 1], limit = (int64_t)p.max_blocks * p.kv.div.page;
+    if (first >= 0 && past_last >= first && past_last <= p.n_keys)
+        count = past_last - first < limit ? past_last - first : limit;
+    else
+        first = 0;
     const int row0 = f.tile * kTileRows + (kSplit ? 0 : wave * 32);
     const int token = row0 + n < f.n ? row0 + n : f.n - 1;
     // (a row that sees no key, and one that sees them all, are at the ends of this range)
