@@ -689,6 +689,15 @@ def ptstore_weigh_workspace(kv_heads: int) -> int:
     return n.value
 
 
+def _weights_of(t: torch.Tensor, layers: int, cache, kv_heads: int) -> int:
+    """The address of the weights of `layers` layers, those and no others: a call would take another layer's of a
+    larger tensor, and say nothing."""
+    if t.numel() != layers * cache.cache_blocks * kv_heads * cache.block_tokens:
+        raise ValueError(f"weights has shape {tuple(t.shape)}, the call takes {layers} layers of "
+                         f"{(cache.cache_blocks, kv_heads, cache.block_tokens)}")
+    return _arg(t, torch.float32, 0, "weights")
+
+
 def _weighed(n, heads, cache, kv_heads, lse, offsets, context, weighed, block_table, scale, weights, workspace):
     """The fields of both weighing structs that follow the queries."""
     R, maxb = _table(offsets, block_table)
@@ -696,7 +705,7 @@ def _weighed(n, heads, cache, kv_heads, lse, offsets, context, weighed, block_ta
             _arg(context, torch.int32, R, "context"),
             None if weighed is None else _arg(weighed, torch.int32, R, "weighed"),
             _arg(block_table, torch.int32, 0, "block_table"), n, R, maxb, heads, scale,
-            _arg(weights, torch.float32, cache.cache_blocks * kv_heads * cache.block_tokens, "weights"),
+            _weights_of(weights, 1, cache, kv_heads),
             _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
 
 
@@ -735,7 +744,7 @@ def _evict(call, cache, kv_heads, layers, layer_bytes, weights, context, keep, m
     i32 = torch.int32
     a = ptstore_evict_t(
         layers, R, maxb, max_keep, recent, layer_bytes,
-        _arg(weights, torch.float32, layers * cache.cache_blocks * kv_heads * cache.block_tokens, "weights"),
+        _weights_of(weights, layers, cache, kv_heads),
         _arg(context, i32, R, "context"), _arg(keep, i32, R, "keep"), _arg(context_out, i32, R, "context_out"),
         _arg(block_table, i32, 0, "block_table"), _arg(to_table, i32, 0, "to_table"),
         _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
