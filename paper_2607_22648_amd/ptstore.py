@@ -652,10 +652,18 @@ def ptstore_latent_attention(cache: ptstore_latent_t, q_latent, q_rope, out, lse
         _check("ptstore_latent_attention", rc)
 
 
+def _number(x: int, bits: int, name: str) -> int:
+    """A caller's number as the C call takes it: the foreign interface would drop the bits that do not fit."""
+    if not -(1 << (bits - 1)) <= x < 1 << (bits - 1):
+        raise ValueError(f"{name} is {x}, which {bits} bits do not hold")
+    return x
+
+
 def ptstore_latent_expanded_workspace(heads: int, n_keys: int) -> int:
     n = C.c_int64()
     _check("ptstore_latent_expanded_workspace",
-           _lib.ptstore_latent_expanded_workspace(heads, n_keys, C.byref(n)))
+           _lib.ptstore_latent_expanded_workspace(_number(heads, 32, "heads"), _number(n_keys, 64, "n_keys"),
+                                                  C.byref(n)))
     return n.value
 
 
@@ -677,7 +685,8 @@ def ptstore_latent_attention_expanded(cache: ptstore_latent_t, q_nope, q_rope, w
         None if lse is None else _arg(lse, torch.float32, n * heads, "lse"),
         _arg(offsets, torch.int64, R + 1, "offsets"), _arg(context, torch.int32, R, "context"),
         _arg(block_table, torch.int32, 0, "block_table"), _arg(key_offsets, torch.int64, R + 1, "key_offsets"),
-        n, n_keys, R, maxb, heads, scale, _arg(workspace, torch.uint8, 0, "workspace"), workspace.numel())
+        n, _number(n_keys, 64, "n_keys"), R, maxb, heads, scale, _arg(workspace, torch.uint8, 0, "workspace"),
+        workspace.numel())
     rc = _lib.ptstore_latent_attention_expanded(C.byref(a), _stream(stream))
     if rc:
         _check("ptstore_latent_attention_expanded", rc)
@@ -685,7 +694,7 @@ def ptstore_latent_attention_expanded(cache: ptstore_latent_t, q_nope, q_rope, w
 
 def ptstore_weigh_workspace(kv_heads: int) -> int:
     n = C.c_int64()
-    _check("ptstore_weigh_workspace", _lib.ptstore_weigh_workspace(kv_heads, C.byref(n)))
+    _check("ptstore_weigh_workspace", _lib.ptstore_weigh_workspace(_number(kv_heads, 32, "kv_heads"), C.byref(n)))
     return n.value
 
 
@@ -732,7 +741,8 @@ def ptstore_latent_weigh(cache: ptstore_latent_t, weights, q_latent, q_rope, lse
 
 def ptstore_evict_workspace(layers: int, R: int, kv_heads: int, max_keep: int) -> int:
     n = C.c_int64()
-    _check("ptstore_evict_workspace", _lib.ptstore_evict_workspace(layers, R, kv_heads, max_keep, C.byref(n)))
+    sizes = (_number(x, 32, name) for x, name in ((layers, "layers"), (R, "R"), (kv_heads, "kv_heads"), (max_keep, "max_keep")))
+    _check("ptstore_evict_workspace", _lib.ptstore_evict_workspace(*sizes, C.byref(n)))
     return n.value
 
 
@@ -743,7 +753,7 @@ def _evict(call, cache, kv_heads, layers, layer_bytes, weights, context, keep, m
         raise ValueError(f"to_table has shape {tuple(to_table.shape)}, block_table {(R, maxb)}")
     i32 = torch.int32
     a = ptstore_evict_t(
-        layers, R, maxb, max_keep, recent, layer_bytes,
+        layers, R, maxb, _number(max_keep, 32, "max_keep"), _number(recent, 32, "recent"), layer_bytes,
         _weights_of(weights, layers, cache, kv_heads),
         _arg(context, i32, R, "context"), _arg(keep, i32, R, "keep"), _arg(context_out, i32, R, "context_out"),
         _arg(block_table, i32, 0, "block_table"), _arg(to_table, i32, 0, "to_table"),

@@ -102,3 +102,25 @@ def test_evict_takes_the_weights_of_its_layers(calls, monkeypatch, layers, shape
         with pytest.raises(ValueError, match="weights"):
             evict()
         assert not calls
+
+
+@pytest.mark.parametrize("most,recent", [(1 << 32, 0), ((1 << 32) + 20, 0), (1 << 31, 0), (20, 1 << 32), (20, (1 << 32) + 3),
+                                         (20, -(1 << 32))])
+def test_evict_refuses_what_32_bits_do_not_hold(calls, monkeypatch, most, recent):
+    """A max_keep of 2^32 must not keep nothing, nor a `recent` of 2^32 no recent tokens."""
+    cache = paged()
+    monkeypatch.setattr(torch, "empty_like", lambda t, **kw: device(*t.shape, dtype=t.dtype))
+    one, table = device(1, dtype=torch.int32), device(1, 8, dtype=torch.int32)
+    with pytest.raises(ValueError, match="max_keep" if recent == 0 else "recent"):
+        cache.evict(device(4, 5, 2, 16), one, table, one, most, recent=recent, workspace=WORKSPACE)
+    assert not calls
+
+
+@pytest.mark.parametrize("call,args", [
+    ("ptstore_evict_workspace", ((1 << 32) + 1, 1, 1, 1)), ("ptstore_evict_workspace", (1, (1 << 32) + 1, 1, 1)),
+    ("ptstore_evict_workspace", (1, 1, (1 << 32) + 1, 1)), ("ptstore_evict_workspace", (1, 1, 1, (1 << 32) + 1)),
+    ("ptstore_latent_expanded_workspace", ((1 << 32) + 8, 100)), ("ptstore_latent_expanded_workspace", (8, (1 << 64) + 100)),
+    ("ptstore_weigh_workspace", ((1 << 32) + 1,))])
+def test_workspaces_of_sizes_past_the_calls_numbers(call, args):
+    with pytest.raises(ValueError, match="bits"):
+        getattr(P, call)(*args)
