@@ -708,11 +708,11 @@ typedef struct {
 } ptstore_latent_expanded_t;
 
 /* Bytes of workspace for n_keys keys, 16-byte aligned: 1,024 a key and head, and 132 a key. Host only.
- * Errors: INVALID. */
+ * Errors: INVALID (heads and n_keys that ptstore_latent_attention_expanded refuses). */
 int ptstore_latent_expanded_workspace(int32_t heads, int64_t n_keys, int64_t *bytes);
 
 /* Errors: INVALID (as ptstore_latent_attention; n_keys > 2^31 - 256; more than 2^24 - 2^13
- * (n_tokens / 128 + R) * heads or (n_keys / 128 + 1) * heads), HIP. */
+ * (n_tokens / 128 + R + 1) * heads or (n_keys / 128 + 1) * heads), HIP. */
 int ptstore_latent_attention_expanded(const ptstore_latent_expanded_t *args, void *stream);
 
 /* ======================================================================

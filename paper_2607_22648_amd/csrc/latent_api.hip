@@ -137,7 +137,8 @@ int ptstore_latent_attention(const ptstore_latent_attention_t* a, void* stream) 
 }
 
 int ptstore_latent_expanded_workspace(int32_t heads, int64_t n_keys, int64_t* bytes) {
-    if (!bytes || heads < 1 || n_keys < 0 || n_keys > kMostKeys)
+    // (of sizes that the call refuses there is no size, and the product could overflow)
+    if (!bytes || heads < 1 || n_keys < 0 || n_keys > kMostKeys || (n_keys / 128 + 1) * heads > kMaxUnits)
         return refuse("ptstore_latent_expanded_workspace: heads or n_keys out of range, or a null argument");
     *bytes = expanded_workspace(heads, n_keys);
     return PTSTORE_OK;

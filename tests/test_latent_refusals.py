@@ -124,3 +124,18 @@ def test_evict_refuses_what_32_bits_do_not_hold(calls, monkeypatch, most, recent
 def test_workspaces_of_sizes_past_the_calls_numbers(call, args):
     with pytest.raises(ValueError, match="bits"):
         getattr(P, call)(*args)
+
+
+@pytest.mark.parametrize("heads,keys", [((1 << 31) - 1, (1 << 31) - 256), (1 << 24, 1 << 30), (8, (1 << 31) - 256), (1 << 24, 0),
+                                        ((1 << 24) - (1 << 13) + 1, 1), (128, 1 << 24)])
+def test_expanded_workspaces_of_calls_that_are_refused(heads, keys):
+    """(n_keys / 128 + 1) * heads past 2^24 - 2^13, which the call refuses: no size, and no product that overflows."""
+    with pytest.raises(P.PTStoreError, match="out of range"):
+        P.ptstore_latent_expanded_workspace(heads, keys)
+
+
+@pytest.mark.parametrize("heads,keys", [((1 << 24) - (1 << 13), 127), (8, 268304383), (1, (1 << 31) - 1048577), (128, 16769023)])
+def test_expanded_workspaces_of_the_largest_calls(heads, keys):
+    assert P.ptstore_latent_expanded_workspace(heads, keys) == heads * keys * 1024 + keys * 128 + -(-keys * 4 // 16) * 16
+    with pytest.raises(P.PTStoreError):
+        P.ptstore_latent_expanded_workspace(heads, keys + 1)
