@@ -1,0 +1,33 @@
+"""What the device sources have to keep to that no compiler tells (CPU)."""
+from __future__ import annotations
+
+import glob
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_22648_amd", "csrc")
+SOURCES = sorted(glob.glob(os.path.join(CSRC, "*.h*")))
+
+
+def statements(text):
+    """Inline asm statements, whole."""
+    return re.findall(r"\basm\b[^;]*?\((?:[^;\"]|\"(?:[^\"\\]|\\.)*\")*\)\s*;", text)
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_loads_to_lds_are_given_their_register(path):
+    """A load to LDS takes its place from m0. The compiler reserves that register and takes no note of asm that writes it,
+    so that it might keep a value of its own there: the asm asks for it as an operand instead."""
+    with open(path) as f:
+        asm = statements(f.read())
+    for s in asm:
+        assert not re.search(r"s_\w+ m0\b", s), s
+        if "_load_lds_" in s:
+            assert '"{m0}"(' in s and "s_nop 0" in s, s
+
+
+def test_the_statements_are_found():
+    with open(os.path.join(CSRC, "lds_fetch.hpp")) as f:
+        assert sum("_load_lds_" in s for s in statements(f.read())) == 5
