@@ -94,6 +94,15 @@ __device__ inline v2u read_transposed(const uint8_t* lds) {
 
 __device__ inline v4u join(v2u a, v2u b) { return v4u{a[0], a[1], b[0], b[1]}; }
 
+// What a wave's lanes wrote to LDS its other lanes read behind this: a wave's LDS operations are performed in the order
+// in which it issues them, so all it takes is that the compiler moves none across (a wave barrier by itself orders
+// no memory). No instruction.
+__device__ inline void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // The 32 codes of a lane's 16 bytes: piece `i` of four, 8 elements.
 __device__ inline v4u widen8(uint32_t code, float step) {
     v4u x;

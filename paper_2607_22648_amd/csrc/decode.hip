@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                 const int key = i * (64 / kLanes) + here / kLanes;
                 *(v4u*)(lds + key * kRow + (((here % kLanes) ^ turn_k<D>(key)) * 16)) = kreg[i];
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
         }
         float kstep[kFour ? kGroups : 1];
         if constexpr (kFour) {
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                     a = *(const v4u*)(lds + key * kRow + (((4 * t + (here >> 4)) ^ turn_k<D>(key)) * 16));
                 s[g] = E::mma16(__builtin_bit_cast(typename E::v8, a), __builtin_bit_cast(typename E::v8, q[t]), s[g]);
             }
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
         const int32_t next = at + stride;
         const uint64_t ok = valid;
         place = key_row<D, kFour>(p.kv, entry, next + step_key, k1, head_row, there);
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
                     *(v4u*)(lds + key * kRow + (((here % kLanes) ^ turn_v<D, kFour>(key)) * 16)) = vreg[i];
                 }
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
             if (b == kKeys / 32 - 1) {
                 __builtin_amdgcn_sched_barrier(0);
                 load_v(place);
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_decode(AttendPlan p) {
             for (int i = 0; i < D / 16; ++i)
                 o[i] = E::mma16(__builtin_bit_cast(typename E::v8, vt[i]),
                                 __builtin_bit_cast(typename E::v8, w[b]), o[i]);
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
         }
         at = next;
     }

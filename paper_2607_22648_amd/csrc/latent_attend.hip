@@ -600,7 +600,7 @@ __global__ __launch_bounds__(kThreads) void k_latent_few(LatentPlan p) {
                     }
                 }
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
         }
         float most = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
         most = larger_16_32(most);

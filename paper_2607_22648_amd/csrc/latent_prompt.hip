@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kFormThreads) void k_form(ExpandedPlan p) {
                     for (int c = 0; c < 4; ++c)
                         *(v4u*)(mem + (n & 15) * 128 + (((2 * c + half) ^ (n & 7)) * 16)) = y[kind][c >> 1][c & 1];
                 }
-                __builtin_amdgcn_wave_barrier();
+                wave_order();
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int key = 8 * j + (lane >> 3), to = t * 32 + 16 * up + key;
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kFormThreads) void k_form(ExpandedPlan p) {
                         __builtin_nontemporal_store(
                             x, (v4u*)(out + (int64_t)to * kRow + kind * (kRow / 2) + (lane & 7) * 16));
                 }
-                __builtin_amdgcn_wave_barrier();
+                wave_order();
             }
         }
     }

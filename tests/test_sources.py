@@ -31,3 +31,13 @@ def test_loads_to_lds_are_given_their_register(path):
 def test_the_statements_are_found():
     with open(os.path.join(CSRC, "lds_fetch.hpp")) as f:
         assert sum("_load_lds_" in s for s in statements(f.read())) == 5
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_wave_barriers_order_memory(path):
+    """A wave barrier alone orders no memory: what lanes exchange through LDS stands between fences of the wave."""
+    with open(path) as f:
+        text = f.read()
+    for m in re.finditer(r"__builtin_amdgcn_wave_barrier\(\);", text):
+        assert re.search(r"__builtin_amdgcn_fence\(__ATOMIC_RELEASE, \"\w+\"\);\s*$", text[:m.start()])
+        assert re.match(r"\s*__builtin_amdgcn_fence\(__ATOMIC_ACQUIRE, \"\w+\"\);", text[m.end():])
