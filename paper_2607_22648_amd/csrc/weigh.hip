@@ -606,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void k_weigh_stream(WeighPlan p) {
 template <int kDim, bool kHalf, int kLayout>
 __global__ __launch_bounds__(kThreads, weigh_waves(kDim)) void k_weigh(WeighPlan p) {
     __shared__ __attribute__((aligned(16))) uint8_t s_q[2][WeighShape<kDim, kLayout>::kBuffer];
-    __shared__ float s_lse[2][kRowsOf];
+    __shared__ __attribute__((aligned(16))) float s_lse[2][kRowsOf];
     const int first = p.streams * p.kv.heads;
     if ((int)blockIdx.x < first)
         weigh<kDim, kHalf, kLayout, true>(p, blockIdx.x, s_q, s_lse);

@@ -41,3 +41,13 @@ def test_wave_barriers_order_memory(path):
     for m in re.finditer(r"__builtin_amdgcn_wave_barrier\(\);", text):
         assert re.search(r"__builtin_amdgcn_fence\(__ATOMIC_RELEASE, \"\w+\"\);\s*$", text[:m.start()])
         assert re.match(r"\s*__builtin_amdgcn_fence\(__ATOMIC_ACQUIRE, \"\w+\"\);", text[m.end():])
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_arrays_read_in_sixteen_bytes_are_aligned(path):
+    """A shared array of single numbers that is read four at a time is declared with the alignment of four."""
+    with open(path) as f:
+        text = f.read()
+    for name in set(re.findall(r"\(const v4[fu]\*\)&(s_\w+)", text)):
+        found = re.findall(r"__shared__ ([^;]*\b%s\[[^;]*);" % name, text)
+        assert found and all("aligned(16)" in x for x in found), (name, found)
