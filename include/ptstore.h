@@ -628,8 +628,9 @@ int ptstore_latent_read(const ptstore_latent_t *cache, void *latent, int64_t lat
  * shared part of key j,
  *   out[t][h] = sum_j w_j c_j / sum_j w_j,
  *   w_j = exp(scale * (q_latent[t][h] . c_j + q_rope[t][h] . p_j)),   lse[t][h] = log(sum_j w_j).
- * Rows that see nothing, and values that are not finite, as there. For single tokens, drafts and short
- * prompts; ptstore_latent_attention_expanded takes fewer operations for long ones.
+ * Rows that see nothing, and values that are not finite, as there. Weights enter the second product rounded to
+ * the cache's type, half a step of it off each; sums and lse take them as they are. For single tokens, drafts and
+ * short prompts; ptstore_latent_attention_expanded takes fewer operations for long ones.
  */
 typedef struct {
     ptstore_latent_t cache;
@@ -665,7 +666,8 @@ int ptstore_latent_attention(const ptstore_latent_attention_t *args, void *strea
 
 /*
  * The same attention in the expanded form, for prompts: each head's keys and values are formed from the
- * rows by the head's matrices, in 32 bits, kept as two values of the cache's type each, and
+ * rows by the head's matrices, in 32 bits, kept as two values of the cache's type each (beyond that type's
+ * largest, 65,504 of fp16, as infinities), and
  *   k_hj = (w_k[h] c_j, p_j),  v_hj = w_v[h] c_j,
  *   out[t][h] = sum_j w_j v_hj / sum_j w_j,  w_j = exp(scale * (q_nope[t][h], q_rope[t][h]) . k_hj).
  * Keys have 128 values of a head's own beside the rope_dim shared ones, values 128. Request r has
@@ -796,6 +798,9 @@ int ptstore_latent_weigh(const ptstore_latent_weigh_t *args, void *stream);
  * call names elsewhere. A token whose page does not exist counts as of least weight and moves nowhere, as does
  * one whose place in to_table does not exist. `layers` layers alike begin layer_bytes apart (a layer's
  * V plane follows its K plane, as in ptstore_kv_t).
+ * context_out counts tokens, and ptstore_block_tables numbers new ones from it: a place in the cache. It is no longer
+ * their position in the text, where the kept keys of each layer and head were rotated; a program whose keys carry
+ * positions counts those by itself, for new keys and queries both. What a query sees goes by places.
  */
 typedef struct {
     int32_t layers;

@@ -13,9 +13,12 @@
 // request's pages are all others there is no order to keep: a unit's workgroups then take 64 tokens at a time,
 // all of their rows, whose places 64 lanes find for all.
 //
-// Measured: 16 requests of 250 to 8,000 tokens to a quarter, 2 layers of 8 heads, 16 us for the first (with 512 threads
-// 18) and 59 for the second (275 MB, 4.7 TB/s); one of 2,049 to half, 8 layers, 10 and 15 (chains of trips to memory;
-// bytes take 12). Moved by 512 threads instead of 256, or with 16 rows of a lane under way, 38 to 51 us a call, not 33.
+// Measured, to other pages: 16 requests of 250 to 8,000 tokens to a quarter, 2 layers of 8 heads, 16 us for the first
+// (with 512 threads 18) and 59 for the second (275 MB, 4.7 TB/s), 78 a call; one of 2,049 to half, 8 layers, 10 and 15
+// (chains of trips to memory; bytes take 12), 27 to 29 a call. In place 139 and 96 a call: one workgroup a unit and 128
+// bytes of its rows, in order. Replayed from a graph a call takes 2 to 4 us more than its kernels; so timed, moving by 512
+// threads instead of 256, or with 16 rows of a lane under way, made the one request's call 38 to 51 us, where an earlier
+// selection and these movers took 33.
 #include <hip/hip_runtime.h>
 
 #include "lds_fetch.hpp"
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_keep_select(KeepPlan p) {
                 }
             }
             __syncthreads();
-            // thread t has the bins 2047 - 4 t .. 2044 - 4 t: the largest first
+            // thread t has the bins 2047 - 2 t and 2046 - 2 t: the largest first
             constexpr int kOf = kBins / kSelectThreads;
             uint32_t mine[kOf], sum = 0;
 #pragma unroll

@@ -13,8 +13,9 @@
 // Rows go from memory to LDS without passing through registers, 32 keys a piece, three pieces in
 // turn, and are read there as they lie for the first product, transposed for the second.
 //
-// Measured: 32 requests of 128 heads, up to two tokens each behind 500 to 8,190, 70 us (39 GFLOP, 560 TFLOP/s;
-// instructions to issue, then the parts' 80 MB, are what bounds it) and 24 for the join; tiles of 16 rows: 64
+// Measured: 32 requests of 128 heads, up to two tokens each behind 500 to 8,190, 70 us (39 GFLOP, 560 TFLOP/s; its two
+// waves a SIMD wait at barriers and for memory 40 % of their time and to issue 31 %, matrix units 22 % of the cycles; then
+// the parts' 80 MB) and 24 for the join; tiles of 16 rows: 64
 // requests of 16 heads behind 120 to 8,190 tokens 67 us (309 MB, 4.6 TB/s; past its fixed 20 us it reads at 6.6), one
 // of 777 tokens 14, and 8 and 6 for their joins.
 #include <type_traits>
@@ -736,7 +737,7 @@ __global__ __launch_bounds__(kThreads) void k_latent_few(LatentPlan p) {
 }
 
 // Joins the parts of a tile that several shares have: the workgroups of all these shares but the last, kGroupsOf
-// each (64 requests of 16 heads: 82 us with two, 86 with four; 32 of 128 heads 99 and 94), take its (row, 8
+// each (64 requests of 16 heads: 78 us a call with two, 82 with four; 32 of 128 heads 96 and 91), take its (row, 8
 // dimensions) items in turn. A lane loads eight parts at once; where a tile has more, several lanes divide
 // them, so that each has few trips to memory.
 constexpr int kJoinThreads = 512;

@@ -15,9 +15,9 @@
 // registers, 32 a step, into one of two buffers while the other is computed from. Two workgroups share a
 // compute unit.
 //
-// Measured: 6 prompts of 33 to 3,500 tokens, 16 heads, 79 us for forming 10,599 keys (44 GFLOP) and 283 for the
-// attention (45 % of its cycles in the matrix units, the rest mostly vector instructions that they wait for); 4 requests
-// behind up to 3,584 tokens, 32 heads, 165 (12,828 keys; 420 MB written) and 238.
+// Measured: 6 prompts of 33 to 3,500 tokens, 16 heads, 79 us for forming 10,599 keys (44 GFLOP) and 290 for the
+// attention (matrix units 46 % of the cycles, other vector instructions 28; with 1.6 waves a SIMD they add up); 4 requests
+// behind up to 3,584 tokens, 32 heads, 168 (12,828 keys; 420 MB written) and 246.
 #include <type_traits>
 
 #include "attend.hpp"

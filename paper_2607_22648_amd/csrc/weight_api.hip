@@ -13,8 +13,10 @@ using namespace ptsd;
 
 namespace {
 
-constexpr int64_t kMaxWeighHeads = 1ll << 22;   // a workgroup a head at least, and a few for the shares' rounding
-constexpr int64_t kMaxWorkgroups = 1ll << 23;   // of keep.hip: 512 threads each
+constexpr int64_t kMaxWeighHeads = 1ll << 22;  // a workgroup a head at least, and a few for the shares' rounding
+// Workgroups that move, of 256 threads: 2^31 work-items. A unit (layer, request, head) has three of them at least, and one
+// of 1,024 threads that chooses: fewer than 2^32 / 1.5.
+constexpr int64_t kMaxWorkgroups = 1ll << 23;
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 

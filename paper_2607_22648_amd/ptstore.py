@@ -1065,7 +1065,10 @@ class _Paged:
         """Keep of each request the last `recent` tokens and those of largest weight, keep[r] (at most max_keep) in
         all, by layer and KV head; their rows and weights go to the front of the pages of `to` (None: in place).
         Returns the tokens that each request has then. weights: [layers, cache_blocks, kv_heads, block_tokens] of
-        the layers layers[0] .. layers[1] - 1 (None: all), which have the same KV heads."""
+        the layers layers[0] .. layers[1] - 1 (None: all), which have the same KV heads.
+
+        From then on `tables` numbers new tokens by their place in the cache. A program whose keys carry positions
+        counts a request's true ones by itself: what is kept has those that it had."""
         a, b = (0, len(self._planes)) if layers is None else layers
         heads = self._heads_of(a, b)
         first = self._planes[a]
