@@ -701,7 +701,9 @@ def ptstore_weigh_workspace(kv_heads: int) -> int:
 def _weights_of(t: torch.Tensor, layers: int, cache, kv_heads: int) -> int:
     """The address of the weights of `layers` layers, those and no others: a call would take another layer's of a
     larger tensor, and say nothing."""
-    if t.numel() != layers * cache.cache_blocks * kv_heads * cache.block_tokens:
+    n = layers * cache.cache_blocks * kv_heads * cache.block_tokens
+    _need(t, n, "weights")
+    if t is not None and t.numel() != n:
         raise ValueError(f"weights has shape {tuple(t.shape)}, the call takes {layers} layers of "
                          f"{(cache.cache_blocks, kv_heads, cache.block_tokens)}")
     return _arg(t, torch.float32, 0, "weights")

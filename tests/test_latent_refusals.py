@@ -139,3 +139,14 @@ def test_expanded_workspaces_of_the_largest_calls(heads, keys):
     assert P.ptstore_latent_expanded_workspace(heads, keys) == heads * keys * 1024 + keys * 128 + -(-keys * 4 // 16) * 16
     with pytest.raises(P.PTStoreError):
         P.ptstore_latent_expanded_workspace(heads, keys + 1)
+
+
+def test_weights_are_required(calls, monkeypatch):
+    cache = paged()
+    monkeypatch.setattr(torch, "empty_like", lambda t, **kw: device(*t.shape, dtype=t.dtype))
+    one, table = device(1, dtype=torch.int32), device(1, 8, dtype=torch.int32)
+    with pytest.raises(ValueError, match="weights is required"):
+        cache.evict(None, one, table, one, 20, workspace=WORKSPACE)
+    with pytest.raises(ValueError, match="weights is required"):
+        cache.weigh(0, None, device(3, 4, 64, dtype=torch.bfloat16), device(3, 4), *batch(), workspace=WORKSPACE)
+    assert not calls
